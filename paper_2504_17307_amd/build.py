@@ -7,7 +7,9 @@ import sysconfig
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
-SRC = os.path.join(CSRC, "uccl_chunk.hip")  # the one translation unit; it includes the .hpp files beside it
+# two translation units, which include the .hpp files beside them: the chunk data path and the row operators
+SRC = os.path.join(CSRC, "uccl_chunk.hip")
+ROWS_SRC = os.path.join(CSRC, "uccl_rows.hip")
 INC = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libuccl_chunk.so")
 # aids of bench.py (dense streaming kernels) and of the tests (the report's recount, late decisions), a library of their own
@@ -19,7 +21,7 @@ PREPARED_SRC = os.path.join(CSRC, "prepared_call.c")
 PREPARED_LIB = os.path.join(PKG, "_prepared" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-fno-fast-math", "-ffp-contract=off", "-fno-gpu-flush-denormals-to-zero",
     # keep packed fp32 VALU forms out of the generated code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -28,26 +30,36 @@ HIPCC_FLAGS = [
 
 
 def sources():
-    """Every file the library is built from (kernel sources and the public header)."""
+    """Every file the library is built from (kernel sources and the public headers)."""
     files = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".hip", ".hpp")))
-    return files + [os.path.join(INC, "uccl_chunk.h")]
+    return files + [os.path.join(INC, "uccl_chunk.h"), os.path.join(INC, "uccl_rows.h")]
 
 
 def build(extra_flags=(), out=LIB, verbose=False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = out + f".tmp{os.getpid()}"
-    cmd = [hipcc, *HIPCC_FLAGS, *extra_flags, f"-I{INC}", f"-I{CSRC}", SRC, "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
-    os.replace(tmp, out)
+    objects = [f"{tmp}.{os.path.basename(src)}.o" for src in (SRC, ROWS_SRC)]   # linked in this order
+    cmds = [[hipcc, *HIPCC_FLAGS, *extra_flags, f"-I{INC}", f"-I{CSRC}", "-c", src, "-o", o] for src, o in zip((SRC, ROWS_SRC), objects)]
+    link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", tmp]
+    try:
+        if verbose:
+            print("\n".join(" ".join(c) for c in (*cmds, link)), flush=True)
+        failed = [p.args for p in [subprocess.Popen(c) for c in cmds] if p.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        subprocess.check_call(link)
+        os.replace(tmp, out)
+    finally:
+        for f in (*objects, tmp):
+            if os.path.exists(f):
+                os.remove(f)
     return out
 
 
 def build_probe(verbose=False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = PROBE_LIB + f".tmp{os.getpid()}"
-    cmd = [hipcc, *HIPCC_FLAGS, f"-I{INC}", f"-I{CSRC}", *PROBE_SRC, "-o", tmp]
+    cmd = [hipcc, *HIPCC_FLAGS, "-shared", f"-I{INC}", f"-I{CSRC}", *PROBE_SRC, "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)

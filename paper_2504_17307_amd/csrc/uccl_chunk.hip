@@ -50,6 +50,7 @@
 
 #include "uccl_chunk.h"
 
+#include "uccl_launch.hpp"
 #include "uccl_elements.hpp"
 #include "uccl_data_kernels.hpp"
 #include "uccl_feedback_kernels.hpp"
@@ -957,6 +958,16 @@ int feed_flush(uccl_feed* f) {
 
 }  // namespace
 
+int uccl_internal_failed(hipError_t e) { return launch_failed(e); }
+
+int uccl_internal_launch(const void* kernel, dim3 grid, dim3 block, hipStream_t s, void** args) {
+  const hipEvent_t t0 = t_start, t1 = t_stop;
+  t_start = t_stop = nullptr;
+  const hipError_t e = t0 != nullptr || t1 != nullptr ? hipExtLaunchKernel(kernel, grid, block, args, 0, s, t0, t1, 0)
+                                                      : hipLaunchKernel(kernel, grid, block, args, 0, s);
+  return e == hipSuccess ? UCCL_OK : launch_failed(e);
+}
+
 extern "C" {
 
 int uccl_feed_create(uccl_feed** feed, void* acc, void* out_stage, const void* recv_stage,
@@ -1199,6 +1210,7 @@ int uccl_init(void) {
   unsigned long long* at = nullptr;
   if (rc == UCCL_OK) rc = device_array(g_scratch, HIP_SYMBOL(scratch), dev, &at);
   if (rc == UCCL_OK) rc = device_array(g_regions, HIP_SYMBOL(regions), dev, &at);
+  if (rc == UCCL_OK) rc = uccl_internal_load_rows();
   return rc;
 }
 

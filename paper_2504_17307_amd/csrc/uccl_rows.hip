@@ -1,0 +1,258 @@
+// Row operators around an all-to-all dispatch, gfx950 (MI355X): norm of rows, products grouped by expert, combination
+// of rows, and their gradients.  Host side: argument checks, the choice of the kernel, the entry points of uccl_rows.h.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+#include <stdint.h>
+
+#include "uccl_rows.h"
+
+#include "uccl_launch.hpp"
+#include "uccl_product_kernels.hpp"
+#include "uccl_row_kernels.hpp"
+
+// What stands for rows and pieces that are not there: loads that must bring zeros go here.
+static __device__ __align__(256) uint32_t zeros[64];
+
+namespace {
+
+constexpr uint32_t kMost = 0x7FFFFFFFu;   // rows, columns, slots, groups
+
+bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+uint32_t element_bytes(uint32_t dtype) {
+  switch (dtype) {
+    case UCCL_F32: return 4;
+    case UCCL_BF16: case UCCL_F16: return 2;
+    case UCCL_E4M3: return 1;
+    default: return 0;
+  }
+}
+bool is_16(uint32_t dtype) { return dtype == UCCL_BF16 || dtype == UCCL_F16; }
+bool is_float(uint32_t dtype) { return dtype == UCCL_F32 || is_16(dtype); }
+bool same_shape(const uccl_rows* a, const uccl_rows* b) { return a->rows == b->rows && a->cols == b->cols; }
+
+// What holds for every matrix by itself.
+int check(const uccl_rows* m) {
+  if (m == nullptr || m->reserved != 0u || element_bytes(m->dtype) == 0u || m->rows > kMost || m->cols > kMost) return UCCL_EINVAL;
+  if ((m->dtype == UCCL_E4M3) != (m->scales != nullptr) && m->rows != 0u) return UCCL_EINVAL;
+  if (m->rows == 0u || m->cols == 0u) return UCCL_OK;
+  if (m->data == nullptr) return UCCL_EINVAL;
+  if (m->rows > 1u && m->stride < static_cast<uint64_t>(m->cols) * element_bytes(m->dtype)) return UCCL_EINVAL;   // rows would overlap
+  if (misaligned(m->data, 16) || (m->rows > 1u && m->stride % 16u != 0u)) return UCCL_EALIGN;
+  if (m->scales != nullptr && (misaligned(m->scales, 4) || (m->rows > 1u && m->scale_stride % 4u != 0u))) return UCCL_EALIGN;
+  return UCCL_OK;
+}
+template <class... M>
+int check(const uccl_rows* first, const M*... others) {
+  const int e = check(first);
+  return e != UCCL_OK ? e : check(others...);
+}
+
+Rows rows_of(const uccl_rows* m) {
+  if (m == nullptr) return Rows{nullptr, 0, nullptr, 0};
+  return Rows{static_cast<char*>(m->data), m->stride, static_cast<char*>(m->scales), m->scale_stride};
+}
+
+uint32_t blocks_for(uint64_t n, uint32_t each) { return static_cast<uint32_t>((n + each - 1) / each); }
+
+// Calls f with a value of the element type of 16- or 32-bit rows.
+template <class F>
+int with_type(uint32_t dtype, F f) {
+  return dtype == UCCL_F32 ? f(float{}) : dtype == UCCL_BF16 ? f(__bf16{}) : f(_Float16{});
+}
+
+template <class T, bool E8>
+int norm(const NormArgs& a, hipStream_t s) {
+  const uint32_t pieces = blocks_for(a.cols, Piece<T>::N);
+  const dim3 grid(a.rows);
+  if (pieces <= 64u) return enqueue(norm_kernel<T, E8, 64, 1>, grid, 64, s, a);
+  if (pieces <= 256u) return enqueue(norm_kernel<T, E8, 256, 1>, grid, 256, s, a);
+  if (pieces <= 512u) return enqueue(norm_kernel<T, E8, 256, 2>, grid, 256, s, a);
+  if (pieces <= 1024u) return enqueue(norm_kernel<T, E8, 256, 4>, grid, 256, s, a);
+  return enqueue(norm_long_kernel<T, E8>, grid, 1024, s, a);
+}
+
+constexpr uint32_t kGradGroups = 512;   // workgroups that share the rows of a norm's gradient
+
+template <class T>
+int norm_grad(const NormGradArgs& a, uint32_t groups, hipStream_t s) {
+  const uint32_t pieces = blocks_for(a.cols, Piece<T>::N);
+  if (pieces <= 256u) return enqueue(norm_grad_kernel<T, 256, 1>, dim3(groups), 256, s, a);
+  if (pieces <= 512u) return enqueue(norm_grad_kernel<T, 256, 2>, dim3(groups), 256, s, a);
+  if (pieces <= 1024u) return enqueue(norm_grad_kernel<T, 1024, 1>, dim3(groups), 1024, s, a);
+  return enqueue(norm_grad_long_kernel<T>, dim3(groups), 1024, s, a);
+}
+
+OutType out_type(const uccl_rows* m) { return m->dtype == UCCL_F32 ? kOutF32 : m->dtype == UCCL_BF16 ? kOutBf16 : kOutF16; }
+
+// Tiles that the rows of `groups` groups can make at most: every group has one that is not full, whatever the offsets.
+uint64_t most_tiles(uint32_t rows, uint32_t groups, uint32_t height) { return rows / height + static_cast<uint64_t>(groups < rows ? groups : rows); }
+
+template <Product P>
+int product(const ProductArgs& a, uint32_t dtype, hipStream_t s) {
+  const uint32_t out_cols = P == kForward ? a.wide : a.cols, across = blocks_for(out_cols, 64u);
+  const uint64_t down = P == kGradW ? static_cast<uint64_t>(a.groups) * blocks_for(a.wide, 64u) : most_tiles(a.rows, a.groups, 64u);
+  const uint64_t tiles = down * across;
+  if (tiles > 0xFFFFFFFFull / 256u) return UCCL_ETOOBIG;
+  const dim3 grid(static_cast<uint32_t>(tiles));
+  if constexpr (P == kForward)
+    if (dtype == UCCL_E4M3) return enqueue(product_plain_kernel<E4m3, P>, grid, 256, s, a);
+  if (dtype == UCCL_BF16) return enqueue(product_plain_kernel<__bf16, P>, grid, 256, s, a);
+  return enqueue(product_plain_kernel<_Float16, P>, grid, 256, s, a);
+}
+
+}  // namespace
+
+int uccl_internal_load_rows() {
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;   // another stream of the program may be under capture
+  const bool relaxed = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
+  void* at = nullptr;
+  const hipError_t e = hipGetSymbolAddress(&at, HIP_SYMBOL(zeros));
+  if (relaxed) (void)hipThreadExchangeStreamCaptureMode(&mode);
+  return e == hipSuccess ? UCCL_OK : uccl_internal_failed(e);
+}
+
+extern "C" {
+
+int uccl_norm_rows(const uccl_rows* y, const uccl_rows* h, float* rstd, const uccl_rows* x, const uccl_rows* r, const void* weight,
+                   const uccl_norm_opts* opts, void* stream) {
+  if (y == nullptr || x == nullptr || !is_float(x->dtype) || (y->dtype != x->dtype && y->dtype != UCCL_E4M3) || !same_shape(y, x)) return UCCL_EINVAL;
+  if ((h != nullptr && (h->dtype != x->dtype || !same_shape(h, x))) || (r != nullptr && (r->dtype != x->dtype || !same_shape(r, x)))) return UCCL_EINVAL;
+  if (opts == nullptr || !(opts->eps >= 0.0f) || isinf(opts->eps) || opts->reserved[0] || opts->reserved[1] || opts->reserved[2]) return UCCL_EINVAL;
+  int e = check(y, x);
+  if (e == UCCL_OK && h != nullptr) e = check(h);
+  if (e == UCCL_OK && r != nullptr) e = check(r);
+  if (e != UCCL_OK) return e;
+  if (x->rows == 0u || x->cols == 0u) return UCCL_OK;
+  if (weight == nullptr) return UCCL_EINVAL;
+  if (misaligned(weight, 16) || misaligned(rstd, 4)) return UCCL_EALIGN;
+  const float shrink = ldexpf(1.0f, -ilogbf(static_cast<float>(x->cols)) / 2);
+  const NormArgs a{rows_of(y), rows_of(h), rows_of(x), rows_of(r), static_cast<const char*>(weight), rstd, x->rows, x->cols, opts->eps, shrink,
+                   1.0f / (static_cast<float>(x->cols) * shrink * shrink)};
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  return with_type(x->dtype, [&](auto t) {
+    using T = decltype(t);
+    return y->dtype == UCCL_E4M3 ? norm<T, true>(a, s) : norm<T, false>(a, s);
+  });
+}
+
+uint64_t uccl_norm_rows_scratch(uint32_t rows, uint32_t cols) {
+  const uint64_t bytes = static_cast<uint64_t>(rows < kGradGroups ? rows : kGradGroups) * cols * sizeof(float);
+  return (bytes + 15u) / 16u * 16u;
+}
+
+int uccl_norm_rows_grad(const uccl_rows* dx, float* dweight, const uccl_rows* dy, const uccl_rows* dh, const uccl_rows* h,
+                        const float* rstd, const void* weight, void* scratch, uint64_t scratch_bytes, void* stream) {
+  if (dx == nullptr || dy == nullptr || h == nullptr || !is_float(h->dtype)) return UCCL_EINVAL;
+  if (dx->dtype != h->dtype || dy->dtype != h->dtype || !same_shape(dx, h) || !same_shape(dy, h)) return UCCL_EINVAL;
+  if (dh != nullptr && (dh->dtype != h->dtype || !same_shape(dh, h))) return UCCL_EINVAL;
+  int e = check(dx, dy, h);
+  if (e == UCCL_OK && dh != nullptr) e = check(dh);
+  if (e != UCCL_OK) return e;
+  if (h->cols == 0u) return UCCL_OK;
+  if (dweight == nullptr) return UCCL_EINVAL;
+  if (misaligned(dweight, 4)) return UCCL_EALIGN;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const uint32_t groups = h->rows < kGradGroups ? h->rows : kGradGroups;
+  if (h->rows != 0u) {
+    if (rstd == nullptr || weight == nullptr || scratch == nullptr || scratch_bytes < uccl_norm_rows_scratch(h->rows, h->cols)) return UCCL_EINVAL;
+    if (misaligned(weight, 16) || misaligned(rstd, 4) || misaligned(scratch, 16)) return UCCL_EALIGN;
+    const NormGradArgs a{rows_of(dx), rows_of(dy), rows_of(h), rows_of(dh), static_cast<const char*>(weight), rstd, static_cast<float*>(scratch), h->rows, h->cols};
+    e = with_type(h->dtype, [&](auto t) { return norm_grad<decltype(t)>(a, groups, s); });
+    if (e != UCCL_OK) return e;
+  }
+  return enqueue(column_sum_kernel, dim3(blocks_for(h->cols, 64u)), 256, s, dweight, static_cast<const float*>(scratch), groups, h->cols);
+}
+
+// What the three products have in common.  `x` of kForward and kGradW is read through the index.
+static int check_product(const uccl_rows* rows, const uccl_rows* w, const int32_t* index, const int32_t* offsets, uint32_t n_groups, uint32_t* wide) {
+  if (n_groups > kMost || (n_groups == 0u && w->rows != 0u)) return UCCL_EINVAL;
+  if (n_groups != 0u && w->rows % n_groups != 0u) return UCCL_EINVAL;
+  *wide = n_groups == 0u ? 0u : w->rows / n_groups;
+  if (n_groups != 0u && offsets == nullptr && rows->rows != 0u) return UCCL_EINVAL;
+  return misaligned(offsets, 4) || misaligned(index, 4) ? UCCL_EALIGN : UCCL_OK;
+}
+
+int uccl_group_product(const uccl_rows* y, const uccl_rows* x, const int32_t* index, const uccl_rows* w, const int32_t* offsets,
+                       uint32_t n_groups, void* stream) {
+  int e = check(y, x, w);
+  if (e != UCCL_OK) return e;
+  uint32_t wide = 0;
+  if (!is_float(y->dtype) || !(is_16(x->dtype) || x->dtype == UCCL_E4M3) || w->dtype != x->dtype || w->cols != x->cols) return UCCL_EINVAL;
+  e = check_product(y, w, index, offsets, n_groups, &wide);
+  if (e != UCCL_OK) return e;
+  if ((n_groups != 0u && y->cols != wide) || (index == nullptr && x->rows < y->rows)) return UCCL_EINVAL;
+  if (n_groups == 0u || y->rows == 0u || y->cols == 0u) return UCCL_OK;
+  const ProductArgs a{rows_of(y), rows_of(x), rows_of(w), index, offsets, n_groups, y->rows, x->rows, wide, x->cols, out_type(y)};
+  return product<kForward>(a, x->dtype, static_cast<hipStream_t>(stream));
+}
+
+int uccl_group_product_grad_x(const uccl_rows* dx, const uccl_rows* dy, const uccl_rows* w, const int32_t* offsets, uint32_t n_groups, void* stream) {
+  int e = check(dx, dy, w);
+  if (e != UCCL_OK) return e;
+  uint32_t wide = 0;
+  if (!is_float(dx->dtype) || !is_16(dy->dtype) || w->dtype != dy->dtype || w->cols != dx->cols || dx->rows != dy->rows) return UCCL_EINVAL;
+  e = check_product(dx, w, nullptr, offsets, n_groups, &wide);
+  if (e != UCCL_OK) return e;
+  if (n_groups != 0u && dy->cols != wide) return UCCL_EINVAL;
+  if (n_groups == 0u || dx->rows == 0u || dx->cols == 0u) return UCCL_OK;
+  const ProductArgs a{rows_of(dx), rows_of(dy), rows_of(w), nullptr, offsets, n_groups, dx->rows, dx->rows, wide, dx->cols, out_type(dx)};
+  return product<kGradX>(a, dy->dtype, static_cast<hipStream_t>(stream));
+}
+
+int uccl_group_product_grad_w(const uccl_rows* dw, const uccl_rows* dy, const uccl_rows* x, const int32_t* index, const int32_t* offsets,
+                              uint32_t n_groups, void* stream) {
+  int e = check(dw, dy, x);
+  if (e != UCCL_OK) return e;
+  uint32_t wide = 0;
+  if (!is_float(dw->dtype) || !is_16(dy->dtype) || x->dtype != dy->dtype || dw->cols != x->cols) return UCCL_EINVAL;
+  e = check_product(dy, dw, index, offsets, n_groups, &wide);
+  if (e != UCCL_OK) return e;
+  if ((n_groups != 0u && dy->cols != wide) || (index == nullptr && x->rows < dy->rows) || (n_groups != 0u && offsets == nullptr)) return UCCL_EINVAL;
+  if (n_groups == 0u || wide == 0u || dw->cols == 0u) return UCCL_OK;
+  const ProductArgs a{rows_of(dw), rows_of(dy), rows_of(x), index, offsets, n_groups, dy->rows, x->rows, wide, dw->cols, out_type(dw)};
+  return product<kGradW>(a, dy->dtype, static_cast<hipStream_t>(stream));
+}
+
+// pos, weights and the like of a combination.
+static int check_slots(const uccl_rows* tokens, const uccl_rows* y, const int32_t* pos, const float* weights, uint32_t slots) {
+  if (y->cols != tokens->cols || y->dtype != tokens->dtype || !is_float(y->dtype) || slots > kMost) return UCCL_EINVAL;
+  if (pos == nullptr && tokens->rows != 0u && slots != 0u) return UCCL_EINVAL;
+  return misaligned(pos, 4) || misaligned(weights, 4) ? UCCL_EALIGN : UCCL_OK;
+}
+
+int uccl_combine_rows(const uccl_rows* out, const uccl_rows* y, const int32_t* pos, const float* weights, uint32_t slots, const uccl_rows* r, void* stream) {
+  int e = check(out, y);
+  if (e == UCCL_OK && r != nullptr) e = check(r);
+  if (e != UCCL_OK) return e;
+  if (r != nullptr && (r->dtype != out->dtype || !same_shape(r, out))) return UCCL_EINVAL;
+  e = check_slots(out, y, pos, weights, slots);
+  if (e != UCCL_OK) return e;
+  if (out->rows == 0u || out->cols == 0u) return UCCL_OK;
+  return with_type(out->dtype, [&](auto t) {
+    using T = decltype(t);
+    const uint32_t blocks = blocks_for(blocks_for(out->cols, Piece<T>::N), 256u);
+    const uint64_t grid = static_cast<uint64_t>(out->rows) * blocks;
+    if (grid > 0xFFFFFFFFull / 256u) return static_cast<int>(UCCL_ETOOBIG);
+    const CombineArgs a{rows_of(out), rows_of(y), rows_of(r), pos, weights, out->rows, slots, y->rows, out->cols, blocks};
+    return enqueue(combine_kernel<T>, dim3(static_cast<uint32_t>(grid)), 256, static_cast<hipStream_t>(stream), a);
+  });
+}
+
+int uccl_combine_rows_grad(const uccl_rows* dy, float* dweights, const uccl_rows* dout, const uccl_rows* y, const int32_t* pos, const float* weights,
+                           uint32_t slots, void* stream) {
+  int e = check(dy, dout, y);
+  if (e != UCCL_OK) return e;
+  if (dy->dtype != y->dtype || !same_shape(dy, y)) return UCCL_EINVAL;
+  e = check_slots(dout, y, pos, weights, slots);
+  if (e != UCCL_OK) return e;
+  if (misaligned(dweights, 4)) return UCCL_EALIGN;
+  if (dout->rows == 0u || slots == 0u) return UCCL_OK;
+  return with_type(y->dtype, [&](auto t) {
+    const CombineGradArgs a{rows_of(dy), rows_of(dout), rows_of(y), pos, weights, dweights, dout->rows, slots, y->rows, dout->cols};
+    return enqueue(combine_grad_kernel<decltype(t)>, dim3(dout->rows), 256, static_cast<hipStream_t>(stream), a);
+  });
+}
+
+}  // extern "C"
