@@ -5,6 +5,9 @@
 
 #include "uccl_row_elements.hpp"
 
+// Loads that must bring zeros go here.
+static __device__ __align__(256) uint32_t page_of_zeros[64];
+
 namespace {
 
 struct E4m3 { uint8_t bits; };
@@ -36,46 +39,84 @@ struct Group {
 
 // Offsets are taken as they can be used, whatever they hold: each is at least the one before it, at least 0 and at most
 // `rows`.  Groups never overlap then and no row outside the matrix is touched.
-// Finds the group of the `tile`th tile of `height` rows (every group's rows are cut into tiles of its own); false: there are fewer tiles.
-// All lanes of a wavefront call it; 64 groups a turn.
-__device__ __forceinline__ bool find_tile(const ProductArgs& a, uint32_t height, uint32_t tile, Group& g, uint32_t& first_row) {
-  const uint32_t lane = threadIdx.x & 63u;
-  int32_t before = 0;       // the greatest offset so far
-  uint32_t passed = 0;      // tiles of earlier groups
-  for (uint32_t at = 0; at < a.groups; at += 64u) {
-    const uint32_t mine = at + lane;
-    int32_t begin = mine <= a.groups ? a.offsets[mine] : 0, end = mine < a.groups ? a.offsets[mine + 1u] : 0;
-    int32_t most = end;
-    if (lane == 0u) most = max(max(most, begin), before);
+//
+// 64 groups' ranges, a lane each, and how many tiles of `height` rows these are (every group is cut into tiles of its own)
+// up to and with the lane's.  `before`: the greatest offset of earlier groups.
+struct Ranges {
+  uint32_t begin, end, tiles, sum;
+  int32_t most;
+};
+__device__ __forceinline__ Ranges group_ranges(const ProductArgs& a, uint32_t at, int32_t before, uint32_t height) {
+  const uint32_t lane = threadIdx.x & 63u, mine = at + lane;
+  const int32_t begin = mine <= a.groups ? a.offsets[mine] : 0, end = mine < a.groups ? a.offsets[mine + 1u] : 0;
+  const int32_t limit = static_cast<int32_t>(a.rows);
+  Ranges r;
+  r.most = lane == 0u ? max(max(end, begin), before) : end;
 #pragma unroll
-    for (uint32_t d = 1; d < 64u; d <<= 1) {
-      const int32_t other = __shfl_up(most, d);
-      if (lane >= d) most = max(most, other);
-    }
-    const int32_t limit = static_cast<int32_t>(a.rows);
-    const int32_t previous = __shfl_up(most, 1);
-    const uint32_t b = static_cast<uint32_t>(min(max(lane == 0u ? max(begin, before) : previous, 0), limit));
-    const uint32_t e = static_cast<uint32_t>(min(max(most, 0), limit));
-    const uint32_t tiles = mine < a.groups ? (e - b + height - 1u) / height : 0u;
-    uint32_t sum = tiles;
+  for (uint32_t d = 1; d < 64u; d <<= 1) {
+    const int32_t other = __shfl_up(r.most, d);
+    if (lane >= d) r.most = max(r.most, other);
+  }
+  const int32_t previous = __shfl_up(r.most, 1);
+  r.begin = static_cast<uint32_t>(min(max(lane == 0u ? max(begin, before) : previous, 0), limit));
+  r.end = static_cast<uint32_t>(min(max(r.most, 0), limit));
+  r.tiles = mine < a.groups ? (r.end - r.begin + height - 1u) / height : 0u;
+  r.sum = r.tiles;
 #pragma unroll
-    for (uint32_t d = 1; d < 64u; d <<= 1) {
-      const uint32_t other = __shfl_up(sum, d);
-      if (lane >= d) sum += other;
+  for (uint32_t d = 1; d < 64u; d <<= 1) {
+    const uint32_t other = __shfl_up(r.sum, d);
+    if (lane >= d) r.sum += other;
+  }
+  return r;
+}
+
+// Workgroups of a launch go round the eight XCDs in turn.  Each XCD gets a contiguous eighth of the n tiles, so that tiles
+// with the same rows or the same weights, which are neighbours, share an L2.  False: there is no tile for this workgroup.
+__device__ __forceinline__ bool tile_of_xcd(uint32_t block, uint32_t n, uint32_t& tile) {
+  const uint32_t each = (n + 7u) / 8u, place = block / 8u;
+  tile = block % 8u * each + place;
+  return place < each && tile < n;
+}
+
+// The tiles of an XCD are taken in bands of 4 rows of tiles, column by column: the 32 that its compute units work on at a time
+// are 4 x 8 and read 12 panels of rows and weights, where a row of 32 would read 33.
+constexpr uint32_t kBand = 4;
+__device__ __forceinline__ void place_in_band(uint32_t& tile, uint32_t down, uint32_t across, uint32_t& place) {
+  const uint32_t band = tile / (kBand * across), high = min(kBand, down - band * kBand), at = tile - band * kBand * across;
+  place = at / high;
+  tile = band * kBand + at % high;
+}
+
+// The workgroup's tile of the products by rows: its group, its first row and its place across.  All lanes of a wavefront call
+// it.  The launch has a workgroup for every tile that there could be; which there are is known here only.
+__device__ __forceinline__ bool find_tile(const ProductArgs& a, uint32_t height, uint32_t across, Group& g, uint32_t& first_row, uint32_t& place) {
+  Ranges r = group_ranges(a, 0, 0, height);
+  uint32_t total = __builtin_amdgcn_readlane(r.sum, 63);
+  if (a.groups > 64u) {
+    int32_t before = __builtin_amdgcn_readlane(r.most, 63);
+    for (uint32_t at = 64; at < a.groups; at += 64u) {
+      const Ranges next = group_ranges(a, at, before, height);
+      before = __builtin_amdgcn_readlane(next.most, 63);
+      total += __builtin_amdgcn_readlane(next.sum, 63);
     }
-    const uint64_t holds = __ballot(passed + sum > tile);
+  }
+  uint32_t tile;
+  if (!tile_of_xcd(blockIdx.x, total * across, tile)) return false;
+  place_in_band(tile, total, across, place);
+  uint32_t passed = 0;
+  for (uint32_t at = 0;; at += 64u) {
+    const uint64_t holds = __ballot(passed + r.sum > tile);
     if (holds != 0u) {
       const int l = __ffsll(static_cast<unsigned long long>(holds)) - 1;
       g.index = at + static_cast<uint32_t>(l);
-      g.begin = __builtin_amdgcn_readlane(b, l);
-      g.end = __builtin_amdgcn_readlane(e, l);
-      first_row = g.begin + (tile - passed - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(tiles, l))) * height;
+      g.begin = __builtin_amdgcn_readlane(r.begin, l);
+      g.end = __builtin_amdgcn_readlane(r.end, l);
+      first_row = g.begin + (tile - passed - (__builtin_amdgcn_readlane(r.sum, l) - __builtin_amdgcn_readlane(r.tiles, l))) * height;
       return true;
     }
-    passed += __builtin_amdgcn_readlane(sum, 63);
-    before = __builtin_amdgcn_readlane(most, 63);
+    passed += __builtin_amdgcn_readlane(r.sum, 63);
+    r = group_ranges(a, at + 64u, __builtin_amdgcn_readlane(r.most, 63), height);
   }
-  return false;
 }
 
 // The rows of group g, by the same rule.
@@ -90,92 +131,342 @@ __device__ __forceinline__ Group group_rows(const ProductArgs& a, uint32_t g) {
   return Group{g, static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(min(most, limit))), static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(min(next, limit)))};
 }
 
-__device__ __forceinline__ void store_out(const ProductArgs& a, uint64_t row, uint32_t col, float v) {
-  char* at = a.out.data + row * a.out.stride;
-  if (a.out_type == kOutF32) reinterpret_cast<float*>(at)[col] = v;
-  else if (a.out_type == kOutBf16) reinterpret_cast<__bf16*>(at)[col] = static_cast<__bf16>(v);
-  else reinterpret_cast<_Float16*>(at)[col] = static_cast<_Float16>(v);
+// The same for either kind of product: tiles of `height` output rows, `across` to a row of tiles.
+template <Product P>
+__device__ __forceinline__ bool find_output(const ProductArgs& a, uint32_t height, uint32_t across, Group& g, uint32_t& first_row, uint32_t& place) {
+  if constexpr (P != kGradW) return find_tile(a, height, across, g, first_row, place);
+  const uint32_t down = (a.wide + height - 1u) / height;
+  uint32_t tile;
+  if (!tile_of_xcd(blockIdx.x, a.groups * down * across, tile)) return false;
+  place_in_band(tile, a.groups * down, across, place);
+  g = group_rows(a, tile / down);
+  first_row = tile % down * height;
+  return true;
 }
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// The plainest form: tiles of 64 x 64, 32 deep, both operands through the LDS element by element.  8-bit operands are
-// widened to bf16 and multiplied exactly: the matrix instructions for 8 bits drop what is below about 2^-13 of the largest
-// of the products that they add at a time.
-template <class T, Product P>
-__global__ __launch_bounds__(256) void product_plain_kernel(ProductArgs a) {
-  using M = std::conditional_t<sizeof(T) == 1, __bf16, T>;
-  constexpr uint32_t DEEP = 32, PITCH = DEEP + 8;
-  __shared__ __align__(16) M ta[64][PITCH], tb[64][PITCH];
-  const uint32_t out_cols = P == kForward ? a.wide : a.cols, across = (out_cols + 63u) / 64u;
-  const uint32_t c0 = blockIdx.x % across * 64u;
-  Group g;
-  uint32_t r0;
-  if constexpr (P == kGradW) {
-    const uint32_t down = (a.wide + 63u) / 64u, t = blockIdx.x / across;
-    g = group_rows(a, t / down);
-    r0 = t % down * 64u;
+// 32 rows x 32 columns from `first` on: a lane has of its row (lane % 32; `there`: it is stored) the columns first + i / 4 * 8 +
+// lane / 32 * 4 + i % 4.  16-bit rows: the lane's other half hands it the 4 columns that make 8, so that 16 bytes are stored.
+__device__ __forceinline__ void store_block(const ProductArgs& a, uint64_t row, bool there, uint32_t first, uint32_t cols, f32x16 v) {
+  char* at = a.out.data + row * a.out.stride;
+  const uint32_t half = threadIdx.x % 64u / 32u;
+  if (a.out_type == kOutF32) {
+#pragma unroll
+    for (uint32_t i = 0; i < 4u; ++i) {
+      const uint32_t c = first + i * 8u + half * 4u;
+      const Piece<float> p{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+      if (there && c < cols) store_piece(at, c / 4u, p, cols - c);
+    }
+    return;
+  }
+  uint32_t w[8];
+#pragma unroll
+  for (uint32_t i = 0; i < 8u; ++i) {
+    if (a.out_type == kOutBf16) w[i] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(v[2 * i]), static_cast<__bf16>(v[2 * i + 1])});
+    else w[i] = __builtin_bit_cast(uint32_t, f16x2{static_cast<_Float16>(v[2 * i]), static_cast<_Float16>(v[2 * i + 1])});
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < 8u; i += 4u) {
+    const u32x2 s0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(w[i], w[i + 2], false, false));
+    const u32x2 s1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(w[i + 1], w[i + 3], false, false));
+    const uint32_t c = first + i * 4u + half * 8u;
+    const Piece<uint16_t> p = __builtin_bit_cast(Piece<uint16_t>, u32x4{s0.x, s1.x, s0.y, s1.y});
+    if (there && c < cols) store_piece(at, c / 8u, p, cols - c);
+  }
+}
+
+// ---- tiles through the LDS --------------------------------------------------------------------------
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+enum Arithmetic : uint32_t { kBf16, kF16, kWidened, kNative8 };   // kWidened: 8-bit operands as bf16
+
+// A stage is 64 bytes along the sum: 32 steps of 16 bits or 64 of 8.  Four of them are in the LDS: one is worked on, and up
+// to three are on their way.
+constexpr uint32_t kStageBytes = 64, kStages = 4;
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) char*)(p)));
+}
+
+// 64 lanes' 16 bytes from memory into the LDS at `to` (the same in every lane), lane by lane.  The compiler does not see the
+// write: wait_for_stage() orders it before the reads.
+__device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from));
+}
+// Every wavefront has at most its newest `N` loads under way and has read what it asked of the LDS.  (Other loads of the
+// wavefront that are counted too only make this stricter: they return in order.)
+template <uint32_t N>
+__device__ __forceinline__ void wait_for_stage() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
+
+// Operands lie in the LDS in 16-byte pieces as they come from memory, in another order within a row so that the lanes of a
+// read meet different banks (64 of 4 bytes, 16 lanes at a time): along the sum, piece p of row r is at p ^ (r / 4 % 4); across
+// it (rows of a tile's width), pairs of pieces are at pair ^ turn(r).
+__device__ __forceinline__ uint32_t turn(uint32_t r) { return (r & 1u) * 2u ^ (r >> 1 & 1u) * 5u; }
+
+template <Arithmetic M>
+__device__ __forceinline__ f32x16 multiply(u32x4 x, u32x4 y, f32x16 acc) {
+  if constexpr (M == kBf16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
   } else {
-    if (!find_tile(a, 64u, blockIdx.x / across, g, r0)) return;
+    static_assert(M == kF16);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), acc, 0, 0, 0);
   }
+}
+struct Widened { u32x4 low, high; };
+__device__ __forceinline__ Widened widen_e4m3(u32x4 v) {
+  const u32x2 a = widen_e4m3(v.x), b = widen_e4m3(v.y), c = widen_e4m3(v.z), d = widen_e4m3(v.w);
+  return Widened{u32x4{a.x, a.y, b.x, b.y}, u32x4{c.x, c.y, d.x, d.y}};
+}
+
+// One operand of a tile: SIDE rows (ALONG: rows of the matrix lie along the sum) or SIDE columns (rows of the matrix are steps
+// of the sum), loaded a stage at a time by THREADS threads.
+template <bool ALONG, uint32_t SIDE, uint32_t THREADS>
+struct Operand {
+  static constexpr uint32_t LOADS = SIDE * kStageBytes / 16u / THREADS, PITCH = ALONG ? kStageBytes / 16u : SIDE / 8u;   // pieces
+  static_assert(SIDE * kStageBytes / 16u % THREADS == 0);
+  const char* at[LOADS];     // the thread's next pieces; of an operand across the sum through an index: the piece in row 0
+  uint32_t step[LOADS];      // along the sum: how far it is to the next piece; through an index: the next row
+
+  static __device__ __forceinline__ uint32_t row(uint32_t i) { return (i * THREADS + threadIdx.x) / PITCH; }
+  static __device__ __forceinline__ uint32_t piece(uint32_t i) {
+    const uint32_t slot = threadIdx.x % PITCH, r = row(i);
+    return ALONG ? slot ^ (r >> 2 & 3u) : slot ^ (turn(r) << 1);
+  }
+  static __device__ __forceinline__ uint32_t place(uint32_t stage, uint32_t i) {   // the wavefront's part of load i
+    return __builtin_amdgcn_readfirstlane(stage + (i * THREADS + (threadIdx.x & ~63u)) * 16u);
+  }
+  // 16 bytes of part j (of 2) of the stage for the lane's row / column of the 32 from `first` on; half the wavefront has the
+  // first 16 bytes of the part, the other half the other ones
+  static __device__ __forceinline__ u32x4 fragment(const char* stage, uint32_t first, uint32_t j) {
+    const uint32_t lane = threadIdx.x & 63u, half = lane / 32u;
+    if constexpr (ALONG) {
+      const uint32_t r = first + lane % 32u;
+      return *reinterpret_cast<const u32x4*>(stage + r * kStageBytes + (((j * 2u + half) ^ (r >> 2 & 3u)) << 4));
+    } else {
+      // 16 lanes bring a block of 4 steps x 16 columns and get it transposed: a lane its column's 4 steps
+      const uint32_t step = j * 16u + half * 8u + lane % 16u / 4u, pair = (first + lane / 16u % 2u * 16u) / 16u;
+      const char* p = stage + step * PITCH * 16u + ((pair ^ turn(step)) << 5) + lane % 4u * 8u;
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)));
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4u * PITCH * 16u)));
+      return u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+  }
+};
+
+// What a wavefront multiplies at a time: 16 bytes a lane, or both parts of a stage for the matrix instruction for 8 bits.
+template <Arithmetic M, class O>
+__device__ __forceinline__ auto fragment_of(const char* stage, uint32_t first, uint32_t j) {
+  const u32x4 x = O::fragment(stage, first, j);
+  if constexpr (M == kNative8) return __builtin_bit_cast(i32x8, __builtin_shufflevector(x, O::fragment(stage, first, 1), 0, 1, 2, 3, 4, 5, 6, 7));
+  else return x;
+}
+
+// A workgroup computes BM x BN of the output, WR x WC wavefronts a part each.  While the matrix cores work on one stage, the
+// next fragments are read from the LDS and loads straight into the LDS bring later stages, a few between every two of a
+// wavefront's multiplications: loads that are issued together hold up what comes after them.  The matrix instruction has the
+// output's columns as its rows, so that a lane holds 4 neighbouring columns of one row.
+template <Arithmetic M, Product P, uint32_t BM, uint32_t BN, uint32_t WR, uint32_t WC>
+__global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs a) {
+  constexpr uint32_t THREADS = WR * WC * 64u, E = M == kWidened || M == kNative8 ? 1u : 2u, DEEP = kStageBytes / E;
+  constexpr uint32_t NA = BM / WR / 32u, NB = BN / WC / 32u, STAGE = (BM + BN) * kStageBytes, PARTS = M == kNative8 ? 1u : 2u;
+  constexpr bool A_ALONG = P != kGradW, B_ALONG = P == kForward;
+  using A = Operand<A_ALONG, BM, THREADS>;
+  using B = Operand<B_ALONG, BN, THREADS>;
+  constexpr uint32_t LOADS = A::LOADS + B::LOADS, LOADS_A_PART = LOADS / PARTS;   // a thread's
+  static_assert(LOADS % PARTS == 0);
+  __shared__ __align__(1024) char lds[kStages * STAGE];
+  const char* const zeros = reinterpret_cast<const char*>(page_of_zeros);
+  const uint32_t out_cols = P == kForward ? a.wide : a.cols, across = (out_cols + BN - 1u) / BN;
+  Group g;
+  uint32_t r0, c0;
+  if (!find_output<P>(a, BM, across, g, r0, c0)) return;
+  c0 *= BN;
   const uint64_t w0 = static_cast<uint64_t>(g.index) * a.wide;
+  const uint32_t out_rows = P == kGradW ? a.wide : g.end;   // its rows end here
   const uint32_t depth = P == kForward ? a.cols : P == kGradX ? a.wide : g.end - g.begin;
-  auto element = [&](const Rows& m, uint64_t row, uint32_t col) {
-    const T v = reinterpret_cast<const T*>(m.data + row * m.stride)[col];
-    if constexpr (sizeof(T) == 1) return __builtin_bit_cast(bf16x2, widen_e4m3(v.bits).x).x;
-    else return v;
-  };
-  auto source = [&](uint32_t i, uint32_t& row) {   // the row that row i reads
-    row = a.index == nullptr ? i : static_cast<uint32_t>(a.index[i]);
-    return row < a.indexed_rows;
-  };
-  f32x4 acc[4] = {};
-  for (uint32_t d0 = 0; d0 < depth; d0 += DEEP) {
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < 64u * DEEP; i += 256u) {
-      const uint32_t r = P == kGradW ? i % 64u : i / DEEP, d = P == kGradW ? i / 64u : i % DEEP;
-      const uint32_t rb = P == kForward ? i / DEEP : i % 64u, db = P == kForward ? i % DEEP : i / 64u;
-      M va{}, vb{};
-      uint32_t from;
-      if constexpr (P == kForward) {
-        if (r0 + r < g.end && d0 + d < depth && source(r0 + r, from)) va = element(a.a, from, d0 + d);
-        if (c0 + rb < a.wide && d0 + db < depth) vb = element(a.b, w0 + c0 + rb, d0 + db);
-      } else if constexpr (P == kGradX) {
-        if (r0 + r < g.end && d0 + d < depth) va = element(a.a, r0 + r, d0 + d);
-        if (c0 + rb < a.cols && d0 + db < depth) vb = element(a.b, w0 + d0 + db, c0 + rb);
-      } else {
-        if (r0 + r < a.wide && d0 + d < depth) va = element(a.a, g.begin + d0 + d, r0 + r);
-        if (c0 + rb < a.cols && d0 + db < depth && source(g.begin + d0 + db, from)) vb = element(a.b, from, c0 + rb);
-      }
-      ta[r][d] = va;
-      tb[rb][db] = vb;
-    }
-    __syncthreads();
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64u;
-    const M* pa = &ta[wave * 16u + lane % 16u][lane / 16u * 8u];
+  const uint32_t steps = (depth + DEEP - 1u) / DEEP;
+
+  // Where the thread's pieces are.  Rows and columns past the tile's end stand for its last ones: what they make is not stored.
+  A la;
+  B lb;
 #pragma unroll
-    for (uint32_t n = 0; n < 4; ++n) {
-      const M* pb = &tb[n * 16u + lane % 16u][lane / 16u * 8u];
-      if constexpr (__is_same(M, __bf16)) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(pa), *reinterpret_cast<const bf16x8*>(pb), acc[n], 0, 0, 0);
-      else acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8*>(pa), *reinterpret_cast<const f16x8*>(pb), acc[n], 0, 0, 0);
+  for (uint32_t i = 0; i < A::LOADS; ++i) {
+    if constexpr (A_ALONG) {
+      uint32_t r = min(r0 + A::row(i), out_rows - 1u);
+      if (P == kForward && a.index != nullptr) r = static_cast<uint32_t>(a.index[r]);
+      la.at[i] = a.a.data + r * a.a.stride + A::piece(i) * 16u;
+      la.step[i] = kStageBytes;
+      if (P == kForward && r >= a.indexed_rows) {           // zeros from the first stage to the last
+        la.at[i] = zeros;
+        la.step[i] = 0u;
+      }
+    } else {
+      la.at[i] = a.a.data + min(r0 / 8u + A::piece(i), (a.wide - 1u) / 8u) * 16ull + (static_cast<uint64_t>(g.begin) + A::row(i)) * a.a.stride;
     }
   }
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64u;
+  // Row d of the group, read through the index by scalar loads: the rows of a wavefront's load are few.  (Vector loads would
+  // be waited for together with the loads into the LDS.)
+  auto indexed = [&](uint32_t d) -> uint32_t {
+    constexpr uint32_t ROWS = 64u / B::PITCH;
+    const uint32_t first = __builtin_amdgcn_readfirstlane(d);
+    uint32_t r = 0xFFFFFFFFu;
 #pragma unroll
-  for (uint32_t n = 0; n < 4; ++n)
-#pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-      const uint32_t r = r0 + wave * 16u + lane / 16u * 4u + i, c = c0 + n * 16u + lane % 16u;
-      if (r >= (P == kGradW ? a.wide : g.end) || c >= out_cols) continue;
-      float v = acc[n][i];
-      if constexpr (sizeof(T) == 1) {
-        uint32_t from;
-        const float sx = source(r, from) ? *reinterpret_cast<const float*>(a.a.scales + from * a.a.scale_stride) : 0.0f;
-        v = v * sx * *reinterpret_cast<const float*>(a.b.scales + (w0 + c) * a.b.scale_stride);
+    for (uint32_t i = 0; i < ROWS; ++i) {
+      const uint32_t at = first + i;
+      if (at < depth) {
+        const uint32_t v = a.index == nullptr ? g.begin + at : static_cast<uint32_t>(((const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.index))[g.begin + at]);
+        r = d == at ? v : r;
       }
-      store_out(a, P == kGradW ? w0 + r : r, c, v);
     }
+    return r;
+  };
+#pragma unroll
+  for (uint32_t i = 0; i < B::LOADS; ++i) {
+    if constexpr (B_ALONG) {
+      lb.at[i] = a.b.data + (w0 + min(c0 + B::row(i), out_cols - 1u)) * a.b.stride + B::piece(i) * 16u;
+    } else {
+      lb.at[i] = a.b.data + min(c0 / 8u + B::piece(i), (a.cols - 1u) / 8u) * 16ull;
+      if constexpr (P == kGradX) lb.at[i] += (w0 + B::row(i)) * a.b.stride;
+      else lb.step[i] = indexed(B::row(i));
+    }
+  }
+
+  // Ask for a thread's load i of stage k.  What lies behind the sum's end comes from a page of zeros.
+  const uint32_t base = lds_address(lds);
+  auto load = [&](uint32_t k, uint32_t i) {
+    const uint32_t stage = base + k % kStages * STAGE;
+    const bool last = k + 1u == steps;
+    if (i < A::LOADS) {
+      const char* from = la.at[i];
+      if constexpr (A_ALONG) {
+        if (last && k * kStageBytes + A::piece(i) * 16u >= depth * E) from = zeros;
+        la.at[i] += P == kForward ? la.step[i] : kStageBytes;
+      } else {
+        if (last && k * DEEP + A::row(i) >= depth) from = zeros;
+        la.at[i] += DEEP * a.a.stride;
+      }
+      load_to_lds(from, A::place(stage, i));
+    } else {
+      i -= A::LOADS;
+      const char* from = lb.at[i];
+      if constexpr (B_ALONG) {
+        if (last && k * kStageBytes + B::piece(i) * 16u >= depth * E) from = zeros;
+        lb.at[i] += kStageBytes;
+      } else if constexpr (P == kGradX) {
+        if (last && k * DEEP + B::row(i) >= depth) from = zeros;
+        lb.at[i] += DEEP * a.b.stride;
+      } else {
+        from = lb.step[i] < a.indexed_rows ? from + lb.step[i] * a.b.stride : zeros;
+        lb.step[i] = indexed((k + 1u) * DEEP + B::row(i));
+      }
+      load_to_lds(from, B::place(stage + BM * kStageBytes, i));
+    }
+  };
+  // Wait for stage k, of which a wavefront has asked for `N` loads less than it has under way.  The piece that the sum ends in
+  // has what is behind the row's end: that is blanked.
+  auto ready = [&](uint32_t k, auto under_way) {
+    if (k + 2u < steps) wait_for_stage<decltype(under_way)::value>();
+    else wait_for_stage<0>();
+    if ((A_ALONG || B_ALONG) && k + 1u == steps && depth * E % 16u != 0u) {
+      const uint32_t tail = depth * E % kStageBytes, p = tail / 16u;
+      char* stage = lds + k % kStages * STAGE;
+      const uint32_t from = A_ALONG ? 0u : BM, to = B_ALONG ? BM + BN : BM;
+      for (uint32_t r = from + threadIdx.x; r < to; r += THREADS) {   // B's rows follow A's
+        char* piece = stage + r * kStageBytes + ((p ^ (r >> 2 & 3u)) << 4);
+#pragma unroll
+        for (uint32_t b = 0; b < 16u; b += E)
+          if (b >= tail % 16u) {
+            if constexpr (E == 1) piece[b] = 0;
+            else *reinterpret_cast<uint16_t*>(piece + b) = 0;
+          }
+      }
+      wait_for_stage<0>();
+    }
+  };
+
+  const uint32_t wave = threadIdx.x / 64u, lane = threadIdx.x & 63u;
+  const uint32_t ra = wave / WC * (BM / WR), cb = wave % WC * (BN / WC);
+  f32x16 acc[NB][NA] = {};
+  if (steps != 0u) {
+#pragma unroll
+    for (uint32_t k = 0; k + 1u < kStages; ++k)
+      if (k < steps)
+#pragma unroll
+        for (uint32_t i = 0; i < LOADS; ++i) load(k, i);
+    ready(0, std::integral_constant<uint32_t, (kStages - 2u) * LOADS>{});
+    using Fragment = decltype(fragment_of<M, A>(lds, 0, 0));
+    Fragment fa[NA], fb[NB];
+#pragma unroll
+    for (uint32_t n = 0; n < NB; ++n) fb[n] = fragment_of<M, B>(lds + BM * kStageBytes, cb + n * 32u, 0);
+#pragma unroll
+    for (uint32_t m = 0; m < NA; ++m) fa[m] = fragment_of<M, A>(lds, ra + m * 32u, 0);
+    for (uint32_t k = 0; k < steps; ++k) {
+#pragma unroll
+      for (uint32_t j = 0; j < PARTS; ++j) {
+        const bool ends = j + 1u == PARTS;
+        if (ends && k + 1u < steps) ready(k + 1u, std::integral_constant<uint32_t, (kStages - 3u) * LOADS + (PARTS - 1u) * LOADS_A_PART>{});
+        const char* next = lds + (ends ? k + 1u : k) % kStages * STAGE;   // behind the last stage: read, and not used
+        Fragment fn[NB];
+#pragma unroll
+        for (uint32_t n = 0; n < NB; ++n) fn[n] = fragment_of<M, B>(next + BM * kStageBytes, cb + n * 32u, ends ? 0u : j + 1u);
+#pragma unroll
+        for (uint32_t m = 0; m < NA; ++m) {
+          if constexpr (M == kWidened) {
+            const Widened x = widen_e4m3(fa[m]);
+#pragma unroll
+            for (uint32_t n = 0; n < NB; ++n) {
+              const Widened w = widen_e4m3(fb[n]);
+              acc[n][m] = multiply<kBf16>(w.low, x.low, acc[n][m]);
+              acc[n][m] = multiply<kBf16>(w.high, x.high, acc[n][m]);
+            }
+          } else {
+#pragma unroll
+            for (uint32_t n = 0; n < NB; ++n) {
+              if constexpr (M == kNative8) acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[n], fa[m], acc[n][m], 0, 0, 0, 0, 0, 0);
+              else acc[n][m] = multiply<M>(fb[n], fa[m], acc[n][m]);
+            }
+          }
+          fa[m] = fragment_of<M, A>(next, ra + m * 32u, ends ? 0u : j + 1u);
+          if (k + kStages - 1u < steps)
+#pragma unroll
+            for (uint32_t i = m * LOADS_A_PART / NA; i < (m + 1u) * LOADS_A_PART / NA; ++i) load(k + kStages - 1u, j * LOADS_A_PART + i);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (uint32_t n = 0; n < NB; ++n) fb[n] = fn[n];
+      }
+    }
+  }
+
+#pragma unroll
+  for (uint32_t m = 0; m < NA; ++m) {
+    const uint32_t r = r0 + ra + m * 32u + lane % 32u;   // this lane's row of the output
+    const bool there = r < out_rows;
+    float sx = 1.0f;
+    if (E == 1u && there) {
+      const uint32_t from = a.index == nullptr ? r : static_cast<uint32_t>(a.index[r]);
+      if (from < a.indexed_rows) sx = *reinterpret_cast<const float*>(a.a.scales + from * a.a.scale_stride);
+    }
+#pragma unroll
+    for (uint32_t n = 0; n < NB; ++n) {
+      f32x16 v = acc[n][m];
+      const uint32_t c = c0 + cb + n * 32u + lane / 32u * 4u;
+      if constexpr (E == 1u) {
+#pragma unroll
+        for (uint32_t i = 0; i < 16u; ++i) {
+          const uint32_t col = min(c + i / 4u * 8u + i % 4u, out_cols - 1u);
+          v[i] = v[i] * sx * *reinterpret_cast<const float*>(a.b.scales + (w0 + col) * a.b.scale_stride);
+        }
+      }
+      store_block(a, P == kGradW ? w0 + r : r, there, c0 + cb + n * 32u, out_cols, v);
+    }
+  }
 }
 
 }  // namespace
