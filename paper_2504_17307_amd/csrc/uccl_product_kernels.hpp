@@ -469,4 +469,133 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
   }
 }
 
+// ---- few rows a group -------------------------------------------------------------------------------
+
+template <uint32_t N>
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// kForward for groups of about 16 rows and less, where the reading of the weights is all there is to do: a workgroup computes
+// 16 rows x WIDE columns, and every wavefront a part of the sum for them, 128 bytes along it at a time in turn with the others.
+// A wavefront has a ring of its own in the LDS, loads whole 128-byte pieces of rows straight into it, and waits for no other one before
+// the parts are added up.
+template <Arithmetic M, uint32_t WIDE, uint32_t WAVES>
+__global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs a) {
+  constexpr uint32_t THREADS = WAVES * 64u, E = M == kWidened ? 1u : 2u, HIGH = 16u, TURN = 128u, RING = 3u, NB = WIDE / 16u;
+  constexpr uint32_t ROWS = HIGH + WIDE, LOADS = ROWS / 8u;    // rows of a stage: x's, then w's; 8 of them a load
+  __shared__ __align__(1024) char lds[WAVES][RING][ROWS * TURN];
+  const uint32_t across = (a.wide + WIDE - 1u) / WIDE, lane = threadIdx.x & 63u, wave = threadIdx.x / 64u;
+  Group g;
+  uint32_t r0, c0;
+  if (!find_tile(a, HIGH, across, g, r0, c0)) return;
+  c0 *= WIDE;
+  const uint64_t w0 = static_cast<uint64_t>(g.index) * a.wide;
+  const char* const zeros = reinterpret_cast<const char*>(page_of_zeros);
+  const uint32_t bytes = a.cols * E, stages = (bytes + TURN - 1u) / TURN;
+  // piece p of a row lies at p ^ (row / 2 % 8), as 16 lanes read 16 rows at a time
+  const uint32_t piece = lane % 8u ^ (lane / 16u & 3u);   // of rows 16 i + lane / 8; rows 8 further have it ^ 4
+  const char* at[LOADS];
+  bool there[LOADS];
+#pragma unroll
+  for (uint32_t i = 0; i < LOADS; ++i) {
+    const uint32_t r = i * 8u + lane / 8u, p = (piece ^ (i % 2u * 4u)) * 16u + wave * TURN;
+    there[i] = true;
+    if (i < HIGH / 8u) {
+      uint32_t from = r0 + r;
+      there[i] = from < g.end;
+      if (there[i] && a.index != nullptr) {
+        from = static_cast<uint32_t>(a.index[from]);
+      }
+      there[i] = there[i] && from < a.indexed_rows;
+      at[i] = a.a.data + from * a.a.stride + p;
+    } else {
+      at[i] = a.b.data + (w0 + min(c0 + r - HIGH, a.wide - 1u)) * a.b.stride + p;
+    }
+  }
+  const uint32_t base = lds_address(lds[wave]);
+  auto load = [&](uint32_t k, uint32_t slot) {   // the wavefront's stages come in turn: wave, wave + WAVES, ...
+#pragma unroll
+    for (uint32_t i = 0; i < LOADS; ++i) {
+      const bool inside = there[i] && k * TURN + (piece ^ (i % 2u * 4u)) * 16u < bytes;
+      load_to_lds(inside ? at[i] : zeros, __builtin_amdgcn_readfirstlane(base + (slot * ROWS + i * 8u) * TURN));
+      at[i] += WAVES * TURN;
+    }
+  };
+  auto fragment = [&](const char* stage, uint32_t first, uint32_t j) {
+    const uint32_t r = first + lane % 16u;
+    return *reinterpret_cast<const u32x4*>(stage + r * TURN + (((j * 4u + lane / 16u) ^ (r >> 1 & 7u)) << 4));
+  };
+  f32x4 acc[NB] = {};
+#pragma unroll
+  for (uint32_t i = 0; i < RING; ++i)
+    if (wave + i * WAVES < stages) load(wave + i * WAVES, i);
+  uint32_t slot = 0;
+  for (uint32_t k = wave; k < stages; k += WAVES) {
+    if (k + (RING - 1u) * WAVES < stages) wait_for_loads<(RING - 1u) * LOADS>();
+    else if (k + (RING - 2u) * WAVES < stages) wait_for_loads<(RING - 2u) * LOADS>();
+    else wait_for_loads<0>();
+    char* stage = lds[wave][slot];
+    if (k + 1u == stages && bytes % 16u != 0u && lane < ROWS) {   // the piece that the rows end in
+      char* last = stage + lane * TURN + ((bytes % TURN / 16u ^ (lane >> 1 & 7u)) << 4);
+#pragma unroll
+      for (uint32_t b = 0; b < 16u; b += E)
+        if (b >= bytes % 16u) {
+          if constexpr (E == 1) last[b] = 0;
+          else *reinterpret_cast<uint16_t*>(last + b) = 0;
+        }
+    }
+    u32x4 fx[2], fw[NB][2];
+#pragma unroll
+    for (uint32_t j = 0; j < 2u; ++j) {
+      fx[j] = fragment(stage, 0, j);
+#pragma unroll
+      for (uint32_t n = 0; n < NB; ++n) fw[n][j] = fragment(stage, HIGH + n * 16u, j);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the ring's place is free
+    if (k + RING * WAVES < stages) load(k + RING * WAVES, slot);
+    slot = slot + 1u == RING ? 0u : slot + 1u;
+#pragma unroll
+    for (uint32_t j = 0; j < 2u; ++j) {
+      auto add = [&](u32x4 w, u32x4 x, f32x4 sum) {
+        if constexpr (M == kF16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, x), sum, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), sum, 0, 0, 0);
+      };
+      if constexpr (E == 1u) {
+        const Widened x = widen_e4m3(fx[j]);
+#pragma unroll
+        for (uint32_t n = 0; n < NB; ++n) {
+          const Widened w = widen_e4m3(fw[n][j]);
+          acc[n] = add(w.low, x.low, acc[n]);
+          acc[n] = add(w.high, x.high, acc[n]);
+        }
+      } else {
+#pragma unroll
+        for (uint32_t n = 0; n < NB; ++n) acc[n] = add(fw[n][j], fx[j], acc[n]);
+      }
+    }
+  }
+  // the parts of the sum, wavefront by wavefront: [row][column], each in the wavefront's own ring, which has been read
+  constexpr uint32_t PITCH = WIDE + 4u;
+  static_assert(HIGH * PITCH * 4u <= RING * ROWS * TURN);
+  float* mine = reinterpret_cast<float*>(lds[wave]);
+#pragma unroll
+  for (uint32_t n = 0; n < NB; ++n) *reinterpret_cast<f32x4*>(mine + lane % 16u * PITCH + n * 16u + lane / 16u * 4u) = acc[n];
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < HIGH * WIDE; i += THREADS) {
+    const uint32_t r = r0 + i / WIDE, c = c0 + i % WIDE;
+    if (r >= g.end || c >= a.wide) continue;
+    float v = 0.0f;
+#pragma unroll
+    for (uint32_t w = 0; w < WAVES; ++w) v += reinterpret_cast<const float*>(lds[w])[i / WIDE * PITCH + i % WIDE];
+    if constexpr (E == 1u) {
+      const uint32_t from = a.index == nullptr ? r : static_cast<uint32_t>(a.index[r]);
+      const float sx = from < a.indexed_rows ? *reinterpret_cast<const float*>(a.a.scales + from * a.a.scale_stride) : 1.0f;
+      v = v * sx * *reinterpret_cast<const float*>(a.b.scales + (w0 + c) * a.b.scale_stride);
+    }
+    char* out = a.out.data + r * a.out.stride;
+    if (a.out_type == kOutF32) reinterpret_cast<float*>(out)[c] = v;
+    else if (a.out_type == kOutBf16) reinterpret_cast<__bf16*>(out)[c] = static_cast<__bf16>(v);
+    else reinterpret_cast<_Float16*>(out)[c] = static_cast<_Float16>(v);
+  }
+}
+
 }  // namespace

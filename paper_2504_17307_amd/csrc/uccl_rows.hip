@@ -101,8 +101,20 @@ int product_tiles(K kernel, uint32_t bm, uint32_t bn, uint32_t threads, const Pr
 // against 92 us; of 125 rows (24 groups, 2043 -> 1003, f16): 51 against 46 us.
 bool takes_large_tiles(const ProductArgs& a) { return a.rows / 192u >= a.groups; }
 
+// Measured with 32 groups, 7168 -> 2048, against tiles of 128 x 128: 8 rows a group in bf16 155 against 193 us, 16 rows 161 against 189,
+// 32 rows 226 against 193.
+bool takes_few_rows(const ProductArgs& a) { return a.rows / 20u < a.groups; }
+
 template <Arithmetic M, Product P>
 int product_of(const ProductArgs& a, hipStream_t s) {
+  if constexpr (P == kForward)
+    if (takes_few_rows(a)) {
+      // 32 columns a workgroup of 4 wavefronts, two workgroups on a compute unit; 16 columns and 8 wavefronts where that would leave most
+      // compute units idle (one row, 7168 -> 2048, bf16: 16.9 against 8.7 us; 16 rows in 8 of 32 groups: 41 against 50 us)
+      const uint32_t groups = a.rows < a.groups ? a.rows : a.groups;
+      if (static_cast<uint64_t>(groups) * blocks_for(a.wide, 32u) <= 256u) return product_tiles<P>(product_few_kernel<M, 16, 8>, 16, 16, 512, a, s);
+      return product_tiles<P>(product_few_kernel<M, 32, 4>, 16, 32, 256, a, s);
+    }
   if (takes_large_tiles(a)) return product_tiles<P>(product_tile_kernel<M, P, 256, 256, 2, 4>, 256, 256, 512, a, s);
   return product_tiles<P>(product_tile_kernel<M, P, 128, 128, 2, 2>, 128, 128, 256, a, s);
 }
