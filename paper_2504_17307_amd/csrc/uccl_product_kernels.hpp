@@ -146,28 +146,55 @@ __device__ __forceinline__ bool find_output(const ProductArgs& a, uint32_t heigh
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// 32 rows x 32 columns from `first` on: a lane has of its row (lane % 32; `there`: it is stored) the columns first + i / 4 * 8 +
-// lane / 32 * 4 + i % 4.  16-bit rows: the lane's other half hands it the 4 columns that make 8, so that 16 bytes are stored.
-__device__ __forceinline__ void store_block(const ProductArgs& a, uint64_t row, bool there, uint32_t first, uint32_t cols, f32x16 v) {
+template <class T>
+__device__ __forceinline__ uint32_t narrow_pair(float a, float b) {
+  typedef T pair __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, pair{static_cast<T>(a), static_cast<T>(b)});
+}
+
+// A block of the output as a matrix instruction leaves it: SIDE (16 or 32) rows, a lane has the row lane % SIDE (`there`: it is
+// stored) and of it, 4 at a time, neighbouring columns from `first` on.  16-bit rows: lanes hand each other what makes 8 columns
+// of one, so that 16 bytes are stored.
+__device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row, bool there, uint32_t first, uint32_t cols, f32x4 x, f32x4 y) {
+  // two blocks of 16 x 16 side by side: columns lane / 16 * 4 .. + 3 of each
+  char* at = a.out.data + row * a.out.stride;
+  const uint32_t quarter = threadIdx.x % 64u / 16u;
+  if (a.out_type == kOutF32) {
+    const uint32_t c = first + quarter * 4u;
+    if (there && c < cols) store_piece(at, c / 4u, Piece<float>{x[0], x[1], x[2], x[3]}, cols - c);
+    if (there && c + 16u < cols) store_piece(at, c / 4u + 4u, Piece<float>{y[0], y[1], y[2], y[3]}, cols - c - 16u);
+    return;
+  }
+  uint32_t wx[2], wy[2];
+#pragma unroll
+  for (uint32_t i = 0; i < 2u; ++i) {
+    wx[i] = a.out_type == kOutBf16 ? narrow_pair<__bf16>(x[2 * i], x[2 * i + 1]) : narrow_pair<_Float16>(x[2 * i], x[2 * i + 1]);
+    wy[i] = a.out_type == kOutBf16 ? narrow_pair<__bf16>(y[2 * i], y[2 * i + 1]) : narrow_pair<_Float16>(y[2 * i], y[2 * i + 1]);
+  }
+  // odd quarters of x against even quarters of y
+  const u32x2 s0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(wx[0], wy[0], false, false));
+  const u32x2 s1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(wx[1], wy[1], false, false));
+  const uint32_t c = first + quarter % 2u * 16u + quarter / 2u * 8u;
+  const Piece<uint16_t> p = __builtin_bit_cast(Piece<uint16_t>, u32x4{s0.x, s1.x, s0.y, s1.y});
+  if (there && c < cols) store_piece(at, c / 8u, p, cols - c);
+}
+__device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row, bool there, uint32_t first, uint32_t cols, f32x16 v) {
+  // one block of 32 x 32: columns i / 4 * 8 + lane / 32 * 4 + i % 4
   char* at = a.out.data + row * a.out.stride;
   const uint32_t half = threadIdx.x % 64u / 32u;
   if (a.out_type == kOutF32) {
 #pragma unroll
     for (uint32_t i = 0; i < 4u; ++i) {
       const uint32_t c = first + i * 8u + half * 4u;
-      const Piece<float> p{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
-      if (there && c < cols) store_piece(at, c / 4u, p, cols - c);
+      if (there && c < cols) store_piece(at, c / 4u, Piece<float>{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]}, cols - c);
     }
     return;
   }
   uint32_t w[8];
 #pragma unroll
-  for (uint32_t i = 0; i < 8u; ++i) {
-    if (a.out_type == kOutBf16) w[i] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(v[2 * i]), static_cast<__bf16>(v[2 * i + 1])});
-    else w[i] = __builtin_bit_cast(uint32_t, f16x2{static_cast<_Float16>(v[2 * i]), static_cast<_Float16>(v[2 * i + 1])});
-  }
+  for (uint32_t i = 0; i < 8u; ++i)
+    w[i] = a.out_type == kOutBf16 ? narrow_pair<__bf16>(v[2 * i], v[2 * i + 1]) : narrow_pair<_Float16>(v[2 * i], v[2 * i + 1]);
 #pragma unroll
   for (uint32_t i = 0; i < 8u; i += 4u) {
     const u32x2 s0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(w[i], w[i + 2], false, false));
@@ -185,9 +212,10 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 enum Arithmetic : uint32_t { kBf16, kF16, kWidened, kNative8 };   // kWidened: 8-bit operands as bf16
 
-// A stage is 64 bytes along the sum: 32 steps of 16 bits or 64 of 8.  Four of them are in the LDS: one is worked on, and up
-// to three are on their way.
-constexpr uint32_t kStageBytes = 64, kStages = 4;
+// A stage is 64 bytes along the sum: 32 steps of 16 bits or 64 of 8.  While the fragments of one are multiplied, those of the next
+// are read from the LDS and up to three more are on their way there: five places, of which the one that was read last is loaded
+// into again.
+constexpr uint32_t kStageBytes = 64, kAhead = 4, kStages = kAhead + 1;
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) char*)(p)));
@@ -198,24 +226,21 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from));
 }
-// Every wavefront has at most its newest `N` loads under way and has read what it asked of the LDS.  (Other loads of the
-// wavefront that are counted too only make this stricter: they return in order.)
+// Every wavefront has at most its newest `N` loads under way.  (Other loads of the wavefront that are counted too only make this
+// stricter: they return in order.)  Fragments that a wavefront has asked of the LDS may be under way too: it has them before it gets to
+// the next such barrier, for it multiplies them first, and their place is loaded into again after that one.
 template <uint32_t N>
-__device__ __forceinline__ void wait_for_stage() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_for_stage() { asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory"); }
 
 // Operands lie in the LDS in 16-byte pieces as they come from memory, in another order within a row so that the lanes of a
-// read meet different banks (64 of 4 bytes, 16 lanes at a time): along the sum, piece p of row r is at p ^ (r / 4 % 4); across
-// it (rows of a tile's width), pairs of pieces are at pair ^ turn(r).
-__device__ __forceinline__ uint32_t turn(uint32_t r) { return (r & 1u) * 2u ^ (r >> 1 & 1u) * 5u; }
+// read meet different banks (64 of 4 bytes; 16 lanes at a time with 16 bytes, 32 with 8): along the sum, piece p of row r is at
+// p ^ (r / 4 % 4); across it (rows of a tile's width), pairs of pieces are at pair ^ turn(r).
+__device__ __forceinline__ uint32_t turn(uint32_t r) { return ((r & 1u) * 2u) ^ ((r >> 1 & 1u) * 5u) ^ (r >> 3 & 1u); }
 
 template <Arithmetic M>
-__device__ __forceinline__ f32x16 multiply(u32x4 x, u32x4 y, f32x16 acc) {
-  if constexpr (M == kBf16) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
-  } else {
-    static_assert(M == kF16);
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), acc, 0, 0, 0);
-  }
+__device__ __forceinline__ f32x4 multiply(u32x4 x, u32x4 y, f32x4 acc) {
+  if constexpr (M == kF16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), acc, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
 }
 struct Widened { u32x4 low, high; };
 __device__ __forceinline__ Widened widen_e4m3(u32x4 v) {
@@ -237,51 +262,53 @@ struct Operand {
     const uint32_t slot = threadIdx.x % PITCH, r = row(i);
     return ALONG ? slot ^ (r >> 2 & 3u) : slot ^ (turn(r) << 1);
   }
-  static __device__ __forceinline__ uint32_t place(uint32_t stage, uint32_t i) {   // the wavefront's part of load i
-    return __builtin_amdgcn_readfirstlane(stage + (i * THREADS + (threadIdx.x & ~63u)) * 16u);
-  }
-  // 16 bytes of part j (of 2) of the stage for the lane's row / column of the 32 from `first` on; half the wavefront has the
-  // first 16 bytes of the part, the other half the other ones
+  // The lane's part of the stage for the SIDE rows / columns from `first` on: 16 bytes of one row of 16, a quarter of the
+  // wavefront the first 16 bytes, and so on; or of one row of 32, the j-th 32 bytes in halves
+  template <uint32_t SIDE16>
   static __device__ __forceinline__ u32x4 fragment(const char* stage, uint32_t first, uint32_t j) {
-    const uint32_t lane = threadIdx.x & 63u, half = lane / 32u;
+    const uint32_t lane = threadIdx.x & 63u;
     if constexpr (ALONG) {
-      const uint32_t r = first + lane % 32u;
-      return *reinterpret_cast<const u32x4*>(stage + r * kStageBytes + (((j * 2u + half) ^ (r >> 2 & 3u)) << 4));
+      const uint32_t r = lane % SIDE16, p = SIDE16 == 16u ? lane / 16u : j * 2u + lane / 32u;   // `first` is a multiple of 16
+      return *reinterpret_cast<const u32x4*>(stage + first * kStageBytes + (r * kStageBytes + ((p ^ (r >> 2 & 3u)) << 4)));
     } else {
+      static_assert(SIDE16 == 16u);
       // 16 lanes bring a block of 4 steps x 16 columns and get it transposed: a lane its column's 4 steps
-      const uint32_t step = j * 16u + half * 8u + lane % 16u / 4u, pair = (first + lane / 16u % 2u * 16u) / 16u;
-      const char* p = stage + step * PITCH * 16u + ((pair ^ turn(step)) << 5) + lane % 4u * 8u;
+      const uint32_t step = lane / 16u * 8u + lane % 16u / 4u;
+      const char* p = stage + step * PITCH * 16u + ((first / 16u ^ turn(step)) << 5) + lane % 4u * 8u;
       typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
       const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)));
-      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4u * PITCH * 16u)));
+      const char* q = stage + (step + 4u) * PITCH * 16u + ((first / 16u ^ turn(step + 4u)) << 5) + lane % 4u * 8u;
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q)));
       return u32x4{lo.x, lo.y, hi.x, hi.y};
     }
   }
 };
 
-// What a wavefront multiplies at a time: 16 bytes a lane, or both parts of a stage for the matrix instruction for 8 bits.
+// What a wavefront multiplies at a time: 16 rows x 64 bytes, or 32 x 64 for the matrix instruction for 8 bits.
 template <Arithmetic M, class O>
-__device__ __forceinline__ auto fragment_of(const char* stage, uint32_t first, uint32_t j) {
-  const u32x4 x = O::fragment(stage, first, j);
-  if constexpr (M == kNative8) return __builtin_bit_cast(i32x8, __builtin_shufflevector(x, O::fragment(stage, first, 1), 0, 1, 2, 3, 4, 5, 6, 7));
-  else return x;
+__device__ __forceinline__ auto fragment_of(const char* stage, uint32_t first) {
+  if constexpr (M == kNative8)
+    return __builtin_bit_cast(i32x8, __builtin_shufflevector(O::template fragment<32>(stage, first, 0), O::template fragment<32>(stage, first, 1), 0, 1, 2, 3, 4, 5, 6, 7));
+  else return O::template fragment<16>(stage, first, 0);
 }
 
 // A workgroup computes BM x BN of the output, WR x WC wavefronts a part each.  While the matrix cores work on one stage, the
-// next fragments are read from the LDS and loads straight into the LDS bring later stages, a few between every two of a
+// next fragments are read from the LDS and loads straight into the LDS bring later stages, one between every few of a
 // wavefront's multiplications: loads that are issued together hold up what comes after them.  The matrix instruction has the
-// output's columns as its rows, so that a lane holds 4 neighbouring columns of one row.
+// output's columns as its rows, so that a lane holds 4 neighbouring columns of one row.  It is the one for blocks of 16 x 16: what
+// bounds long products is power, and from registers alone it reaches 1.98 PFLOP/s in bf16 where the one for 32 x 32 reaches 1.70.
 template <Arithmetic M, Product P, uint32_t BM, uint32_t BN, uint32_t WR, uint32_t WC>
 __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs a) {
   constexpr uint32_t THREADS = WR * WC * 64u, E = M == kWidened || M == kNative8 ? 1u : 2u, DEEP = kStageBytes / E;
-  constexpr uint32_t NA = BM / WR / 32u, NB = BN / WC / 32u, STAGE = (BM + BN) * kStageBytes, PARTS = M == kNative8 ? 1u : 2u;
+  constexpr uint32_t SIDE = M == kNative8 ? 32u : 16u, NA = BM / WR / SIDE, NB = BN / WC / SIDE, STAGE = (BM + BN) * kStageBytes;
   constexpr bool A_ALONG = P != kGradW, B_ALONG = P == kForward;
   using A = Operand<A_ALONG, BM, THREADS>;
   using B = Operand<B_ALONG, BN, THREADS>;
-  constexpr uint32_t LOADS = A::LOADS + B::LOADS, LOADS_A_PART = LOADS / PARTS;   // a thread's
-  static_assert(LOADS % PARTS == 0);
+  constexpr uint32_t LOADS = A::LOADS + B::LOADS;   // a thread's, of a stage
+  using Block = std::conditional_t<M == kNative8, f32x16, f32x4>;
   __shared__ __align__(1024) char lds[kStages * STAGE];
-  const char* const zeros = reinterpret_cast<const char*>(page_of_zeros);
+  const char* zeros = reinterpret_cast<const char*>(page_of_zeros);
+  asm volatile("" : "+s"(zeros));   // an address in registers: not looked up again at every load
   const uint32_t out_cols = P == kForward ? a.wide : a.cols, across = (out_cols + BN - 1u) / BN;
   Group g;
   uint32_t r0, c0;
@@ -337,11 +364,10 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
     }
   }
 
-  // Ask for a thread's load i of stage k.  What lies behind the sum's end comes from a page of zeros.
-  const uint32_t base = lds_address(lds);
-  auto load = [&](uint32_t k, uint32_t i) {
-    const uint32_t stage = base + k % kStages * STAGE;
-    const bool last = k + 1u == steps;
+  // Ask for a thread's load i of a stage, into the LDS at `slot`.  What lies behind the end of the sum, in its last stage, comes from
+  // a page of zeros.
+  const uint32_t here = lds_address(lds) + __builtin_amdgcn_readfirstlane(threadIdx.x & ~63u) * 16u;
+  auto load = [&](uint32_t k, uint32_t slot, uint32_t i, bool last) {
     if (i < A::LOADS) {
       const char* from = la.at[i];
       if constexpr (A_ALONG) {
@@ -351,7 +377,7 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
         if (last && k * DEEP + A::row(i) >= depth) from = zeros;
         la.at[i] += DEEP * a.a.stride;
       }
-      load_to_lds(from, A::place(stage, i));
+      load_to_lds(from, here + slot + i * THREADS * 16u);
     } else {
       i -= A::LOADS;
       const char* from = lb.at[i];
@@ -365,106 +391,132 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
         from = lb.step[i] < a.indexed_rows ? from + lb.step[i] * a.b.stride : zeros;
         lb.step[i] = indexed((k + 1u) * DEEP + B::row(i));
       }
-      load_to_lds(from, B::place(stage + BM * kStageBytes, i));
+      load_to_lds(from, here + slot + BM * kStageBytes + i * THREADS * 16u);
     }
   };
-  // Wait for stage k, of which a wavefront has asked for `N` loads less than it has under way.  The piece that the sum ends in
-  // has what is behind the row's end: that is blanked.
-  auto ready = [&](uint32_t k, auto under_way) {
-    if (k + 2u < steps) wait_for_stage<decltype(under_way)::value>();
-    else wait_for_stage<0>();
-    if ((A_ALONG || B_ALONG) && k + 1u == steps && depth * E % 16u != 0u) {
-      const uint32_t tail = depth * E % kStageBytes, p = tail / 16u;
-      char* stage = lds + k % kStages * STAGE;
-      const uint32_t from = A_ALONG ? 0u : BM, to = B_ALONG ? BM + BN : BM;
-      for (uint32_t r = from + threadIdx.x; r < to; r += THREADS) {   // B's rows follow A's
-        char* piece = stage + r * kStageBytes + ((p ^ (r >> 2 & 3u)) << 4);
+  // The piece that the sum ends in has what is behind the row's end: that is blanked.
+  const bool ragged = (A_ALONG || B_ALONG) && depth * E % 16u != 0u;
+  auto trim = [&](char* stage) {
+    const uint32_t tail = depth * E % kStageBytes, p = tail / 16u;
+    const uint32_t from = A_ALONG ? 0u : BM, to = B_ALONG ? BM + BN : BM;
+    for (uint32_t r = from + threadIdx.x; r < to; r += THREADS) {   // B's rows follow A's
+      char* piece = stage + r * kStageBytes + ((p ^ (r >> 2 & 3u)) << 4);
 #pragma unroll
-        for (uint32_t b = 0; b < 16u; b += E)
-          if (b >= tail % 16u) {
-            if constexpr (E == 1) piece[b] = 0;
-            else *reinterpret_cast<uint16_t*>(piece + b) = 0;
-          }
-      }
-      wait_for_stage<0>();
+      for (uint32_t b = 0; b < 16u; b += E)
+        if (b >= tail % 16u) {
+          if constexpr (E == 1) piece[b] = 0;
+          else *reinterpret_cast<uint16_t*>(piece + b) = 0;
+        }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
 
   const uint32_t wave = threadIdx.x / 64u, lane = threadIdx.x & 63u;
   const uint32_t ra = wave / WC * (BM / WR), cb = wave % WC * (BN / WC);
-  f32x16 acc[NB][NA] = {};
+  Block acc[NB][NA] = {};
+  using Fragment = decltype(fragment_of<M, A>(lds, 0));
+  Fragment fa[NA], fb[2][NB];
+  uint32_t next_slot = STAGE, load_slot = kAhead * STAGE;   // bytes
+  // Stage k, whose fragments are fa and fb[TURN]: multiply, and bring the next ones.  STEADY: stage k + kAhead is there to be asked for, and
+  // is not the last.
+  auto work = [&](uint32_t k, auto steady, auto turn_) {
+    constexpr bool STEADY = decltype(steady)::value;
+    constexpr uint32_t TURN = decltype(turn_)::value;
+    const char* next = lds + next_slot;   // behind the last stage: read, and not used
+    if constexpr (STEADY) {
+      wait_for_stage<(kAhead - 2u) * LOADS>();
+    } else if (k + 1u < steps) {
+      wait_for_stage<0>();
+      if (ragged && k + 2u == steps) trim(lds + next_slot);
+    }
+#pragma unroll
+    for (uint32_t n = 0; n < NB; ++n) fb[TURN ^ 1u][n] = fragment_of<M, B>(next + BM * kStageBytes, cb + n * SIDE);
+#pragma unroll
+    for (uint32_t m = 0; m < NA; ++m) {
+      if constexpr (M == kWidened) {
+        const Widened x = widen_e4m3(fa[m]);
+#pragma unroll
+        for (uint32_t n = 0; n < NB; ++n) {
+          const Widened w = widen_e4m3(fb[TURN][n]);
+          acc[n][m] = multiply<M>(w.low, x.low, acc[n][m]);
+          acc[n][m] = multiply<M>(w.high, x.high, acc[n][m]);
+        }
+      } else {
+#pragma unroll
+        for (uint32_t n = 0; n < NB; ++n) {
+          if constexpr (M == kNative8) acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[TURN][n], fa[m], acc[n][m], 0, 0, 0, 0, 0, 0);
+          else acc[n][m] = multiply<M>(fb[TURN][n], fa[m], acc[n][m]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);   // the next fragment takes the registers of this one
+      fa[m] = fragment_of<M, A>(next, ra + m * SIDE);
+      if (STEADY || k + kAhead < steps)
+#pragma unroll
+        for (uint32_t i = m * LOADS / NA; i < (m + 1u) * LOADS / NA; ++i) load(k + kAhead, load_slot, i, !STEADY);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    next_slot = next_slot + STAGE == kStages * STAGE ? 0u : next_slot + STAGE;
+    load_slot = load_slot + STAGE == kStages * STAGE ? 0u : load_slot + STAGE;
+  };
   if (steps != 0u) {
 #pragma unroll
-    for (uint32_t k = 0; k + 1u < kStages; ++k)
+    for (uint32_t k = 0; k < kAhead; ++k)
       if (k < steps)
 #pragma unroll
-        for (uint32_t i = 0; i < LOADS; ++i) load(k, i);
-    ready(0, std::integral_constant<uint32_t, (kStages - 2u) * LOADS>{});
-    using Fragment = decltype(fragment_of<M, A>(lds, 0, 0));
-    Fragment fa[NA], fb[NB];
+        for (uint32_t i = 0; i < LOADS; ++i) load(k, k * STAGE, i, k + 1u == steps);
+    if (steps >= kAhead) wait_for_stage<(kAhead - 1u) * LOADS>();
+    else wait_for_stage<0>();
+    if (ragged && steps == 1u) trim(lds);
 #pragma unroll
-    for (uint32_t n = 0; n < NB; ++n) fb[n] = fragment_of<M, B>(lds + BM * kStageBytes, cb + n * 32u, 0);
+    for (uint32_t n = 0; n < NB; ++n) fb[0][n] = fragment_of<M, B>(lds + BM * kStageBytes, cb + n * SIDE);
 #pragma unroll
-    for (uint32_t m = 0; m < NA; ++m) fa[m] = fragment_of<M, A>(lds, ra + m * 32u, 0);
-    for (uint32_t k = 0; k < steps; ++k) {
-#pragma unroll
-      for (uint32_t j = 0; j < PARTS; ++j) {
-        const bool ends = j + 1u == PARTS;
-        if (ends && k + 1u < steps) ready(k + 1u, std::integral_constant<uint32_t, (kStages - 3u) * LOADS + (PARTS - 1u) * LOADS_A_PART>{});
-        const char* next = lds + (ends ? k + 1u : k) % kStages * STAGE;   // behind the last stage: read, and not used
-        Fragment fn[NB];
-#pragma unroll
-        for (uint32_t n = 0; n < NB; ++n) fn[n] = fragment_of<M, B>(next + BM * kStageBytes, cb + n * 32u, ends ? 0u : j + 1u);
-#pragma unroll
-        for (uint32_t m = 0; m < NA; ++m) {
-          if constexpr (M == kWidened) {
-            const Widened x = widen_e4m3(fa[m]);
-#pragma unroll
-            for (uint32_t n = 0; n < NB; ++n) {
-              const Widened w = widen_e4m3(fb[n]);
-              acc[n][m] = multiply<kBf16>(w.low, x.low, acc[n][m]);
-              acc[n][m] = multiply<kBf16>(w.high, x.high, acc[n][m]);
-            }
-          } else {
-#pragma unroll
-            for (uint32_t n = 0; n < NB; ++n) {
-              if constexpr (M == kNative8) acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[n], fa[m], acc[n][m], 0, 0, 0, 0, 0, 0);
-              else acc[n][m] = multiply<M>(fb[n], fa[m], acc[n][m]);
-            }
-          }
-          fa[m] = fragment_of<M, A>(next, ra + m * 32u, ends ? 0u : j + 1u);
-          if (k + kStages - 1u < steps)
-#pragma unroll
-            for (uint32_t i = m * LOADS_A_PART / NA; i < (m + 1u) * LOADS_A_PART / NA; ++i) load(k + kStages - 1u, j * LOADS_A_PART + i);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (uint32_t n = 0; n < NB; ++n) fb[n] = fn[n];
-      }
+    for (uint32_t m = 0; m < NA; ++m) fa[m] = fragment_of<M, A>(lds, ra + m * SIDE);
+    uint32_t k = 0;
+    for (; k + kAhead + 2u < steps; k += 2u) {
+      work(k, std::true_type{}, std::integral_constant<uint32_t, 0>{});
+      work(k + 1u, std::true_type{}, std::integral_constant<uint32_t, 1>{});
+    }
+    for (; k < steps; k += 2u) {
+      work(k, std::false_type{}, std::integral_constant<uint32_t, 0>{});
+      if (k + 1u < steps) work(k + 1u, std::false_type{}, std::integral_constant<uint32_t, 1>{});
     }
   }
 
 #pragma unroll
   for (uint32_t m = 0; m < NA; ++m) {
-    const uint32_t r = r0 + ra + m * 32u + lane % 32u;   // this lane's row of the output
+    const uint32_t r = r0 + ra + m * SIDE + lane % SIDE;   // this lane's row of the output
     const bool there = r < out_rows;
+    const uint64_t row = P == kGradW ? w0 + r : r;
     float sx = 1.0f;
     if (E == 1u && there) {
       const uint32_t from = a.index == nullptr ? r : static_cast<uint32_t>(a.index[r]);
       if (from < a.indexed_rows) sx = *reinterpret_cast<const float*>(a.a.scales + from * a.a.scale_stride);
     }
+    auto scaled = [&](float v, uint32_t c) {
+      if constexpr (E == 1u) return v * sx * *reinterpret_cast<const float*>(a.b.scales + (w0 + min(c, out_cols - 1u)) * a.b.scale_stride);
+      else return v;
+    };
+    if constexpr (SIDE == 32u) {
 #pragma unroll
-    for (uint32_t n = 0; n < NB; ++n) {
-      f32x16 v = acc[n][m];
-      const uint32_t c = c0 + cb + n * 32u + lane / 32u * 4u;
-      if constexpr (E == 1u) {
+      for (uint32_t n = 0; n < NB; ++n) {
+        const uint32_t first = c0 + cb + n * 32u;
+        f32x16 v = acc[n][m];
 #pragma unroll
-        for (uint32_t i = 0; i < 16u; ++i) {
-          const uint32_t col = min(c + i / 4u * 8u + i % 4u, out_cols - 1u);
-          v[i] = v[i] * sx * *reinterpret_cast<const float*>(a.b.scales + (w0 + col) * a.b.scale_stride);
-        }
+        for (uint32_t i = 0; i < 16u; ++i) v[i] = scaled(v[i], first + i / 4u * 8u + lane / 32u * 4u + i % 4u);
+        store_blocks(a, row, there, first, out_cols, v);
       }
-      store_block(a, P == kGradW ? w0 + r : r, there, c0 + cb + n * 32u, out_cols, v);
+    } else {
+#pragma unroll
+      for (uint32_t n = 0; n < NB; n += 2u) {
+        const uint32_t first = c0 + cb + n * 16u;
+        f32x4 x = acc[n][m], y = acc[n + 1u][m];
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; ++i) {
+          x[i] = scaled(x[i], first + lane / 16u * 4u + i);
+          y[i] = scaled(y[i], first + 16u + lane / 16u * 4u + i);
+        }
+        store_blocks(a, row, there, first, out_cols, x, y);
+      }
     }
   }
 }
@@ -489,7 +541,8 @@ __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs a) 
   if (!find_tile(a, HIGH, across, g, r0, c0)) return;
   c0 *= WIDE;
   const uint64_t w0 = static_cast<uint64_t>(g.index) * a.wide;
-  const char* const zeros = reinterpret_cast<const char*>(page_of_zeros);
+  const char* zeros = reinterpret_cast<const char*>(page_of_zeros);
+  asm volatile("" : "+s"(zeros));
   const uint32_t bytes = a.cols * E, stages = (bytes + TURN - 1u) / TURN;
   // piece p of a row lies at p ^ (row / 2 % 8), as 16 lanes read 16 rows at a time
   const uint32_t piece = lane % 8u ^ (lane / 16u & 3u);   // of rows 16 i + lane / 8; rows 8 further have it ^ 4
@@ -555,21 +608,17 @@ __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs a) 
     slot = slot + 1u == RING ? 0u : slot + 1u;
 #pragma unroll
     for (uint32_t j = 0; j < 2u; ++j) {
-      auto add = [&](u32x4 w, u32x4 x, f32x4 sum) {
-        if constexpr (M == kF16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, x), sum, 0, 0, 0);
-        else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), sum, 0, 0, 0);
-      };
       if constexpr (E == 1u) {
         const Widened x = widen_e4m3(fx[j]);
 #pragma unroll
         for (uint32_t n = 0; n < NB; ++n) {
           const Widened w = widen_e4m3(fw[n][j]);
-          acc[n] = add(w.low, x.low, acc[n]);
-          acc[n] = add(w.high, x.high, acc[n]);
+          acc[n] = multiply<M>(w.low, x.low, acc[n]);
+          acc[n] = multiply<M>(w.high, x.high, acc[n]);
         }
       } else {
 #pragma unroll
-        for (uint32_t n = 0; n < NB; ++n) acc[n] = add(fw[n][j], fx[j], acc[n]);
+        for (uint32_t n = 0; n < NB; ++n) acc[n] = multiply<M>(fw[n][j], fx[j], acc[n]);
       }
     }
   }
