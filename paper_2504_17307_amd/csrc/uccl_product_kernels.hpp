@@ -212,29 +212,30 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 enum Arithmetic : uint32_t { kBf16, kF16, kWidened, kNative8 };   // kWidened: 8-bit operands as bf16
 
-// A stage is 64 bytes along the sum: 32 steps of 16 bits or 64 of 8.  While the fragments of one are multiplied, those of the next
-// are read from the LDS and up to three more are on their way there: five places, of which the one that was read last is loaded
-// into again.
-constexpr uint32_t kStageBytes = 64, kAhead = 4, kStages = kAhead + 1;
+// A stage is 128 bytes along the sum: 64 steps of 16 bits or 128 of 8.  It is multiplied in two halves.  Rows are loaded 128 bytes at
+// a time: the L2 takes a request for 64 bytes as long as one for 128.
+constexpr uint32_t kStageBytes = 128;
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) char*)(p)));
 }
 
 // 64 lanes' 16 bytes from memory into the LDS at `to` (the same in every lane), lane by lane.  The compiler does not see the
-// write: wait_for_stage() orders it before the reads.
+// write: wait_for_loads() orders it before the reads.
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from));
 }
 // Every wavefront has at most its newest `N` loads under way.  (Other loads of the wavefront that are counted too only make this
-// stricter: they return in order.)  Fragments that a wavefront has asked of the LDS may be under way too: it has them before it gets to
-// the next such barrier, for it multiplies them first, and their place is loaded into again after that one.
+// stricter: they return in order.)
 template <uint32_t N>
-__device__ __forceinline__ void wait_for_stage() { asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory"); }
+// Every wavefront has what it asked of the LDS but for its newest `N` reads.
+template <uint32_t N>
+__device__ __forceinline__ void wait_for_reads() { asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory"); }
 
 // Operands lie in the LDS in 16-byte pieces as they come from memory, in another order within a row so that the lanes of a
 // read meet different banks (64 of 4 bytes; 16 lanes at a time with 16 bytes, 32 with 8): along the sum, piece p of row r is at
-// p ^ (r / 4 % 4); across it (rows of a tile's width), pairs of pieces are at pair ^ turn(r).
+// p ^ (r / 2 % 8); across it (rows of a tile's width), pairs of pieces are at pair ^ turn(r).
 __device__ __forceinline__ uint32_t turn(uint32_t r) { return ((r & 1u) * 2u) ^ ((r >> 1 & 1u) * 5u) ^ (r >> 3 & 1u); }
 
 template <Arithmetic M>
@@ -255,29 +256,31 @@ struct Operand {
   static constexpr uint32_t LOADS = SIDE * kStageBytes / 16u / THREADS, PITCH = ALONG ? kStageBytes / 16u : SIDE / 8u;   // pieces
   static_assert(SIDE * kStageBytes / 16u % THREADS == 0);
   const char* at[LOADS];     // the thread's next pieces; of an operand across the sum through an index: the piece in row 0
-  uint32_t step[LOADS];      // along the sum: how far it is to the next piece; through an index: the next row
+  uint32_t next[LOADS];      // through an index across the sum: the next row
+  uint32_t still;            // along the sum: bit i, the piece of load i is of a row of zeros and stays where it is
 
   static __device__ __forceinline__ uint32_t row(uint32_t i) { return (i * THREADS + threadIdx.x) / PITCH; }
   static __device__ __forceinline__ uint32_t piece(uint32_t i) {
     const uint32_t slot = threadIdx.x % PITCH, r = row(i);
-    return ALONG ? slot ^ (r >> 2 & 3u) : slot ^ (turn(r) << 1);
+    return ALONG ? slot ^ (r >> 1 & 7u) : slot ^ (turn(r) << 1);
   }
-  // The lane's part of the stage for the SIDE rows / columns from `first` on: 16 bytes of one row of 16, a quarter of the
-  // wavefront the first 16 bytes, and so on; or of one row of 32, the j-th 32 bytes in halves
+  // The lane's part of half a stage for the SIDE16 (16 or 32) rows / columns from `first`, a multiple of 16, on: 16 bytes of one row of
+  // 16, a quarter of the wavefront the first 16 bytes, and so on; or of one row of 32, the j-th 32 bytes in halves
   template <uint32_t SIDE16>
-  static __device__ __forceinline__ u32x4 fragment(const char* stage, uint32_t first, uint32_t j) {
+  static __device__ __forceinline__ u32x4 fragment(const char* stage, uint32_t first, uint32_t half, uint32_t j) {
     const uint32_t lane = threadIdx.x & 63u;
     if constexpr (ALONG) {
-      const uint32_t r = lane % SIDE16, p = SIDE16 == 16u ? lane / 16u : j * 2u + lane / 32u;   // `first` is a multiple of 16
-      return *reinterpret_cast<const u32x4*>(stage + first * kStageBytes + (r * kStageBytes + ((p ^ (r >> 2 & 3u)) << 4)));
+      const uint32_t r = lane % SIDE16, p = half * 4u + (SIDE16 == 16u ? lane / 16u : j * 2u + lane / 32u);
+      return *reinterpret_cast<const u32x4*>(stage + first * kStageBytes + (r * kStageBytes + ((p ^ (r >> 1 & 7u)) << 4)));
     } else {
       static_assert(SIDE16 == 16u);
       // 16 lanes bring a block of 4 steps x 16 columns and get it transposed: a lane its column's 4 steps
       const uint32_t step = lane / 16u * 8u + lane % 16u / 4u;
-      const char* p = stage + step * PITCH * 16u + ((first / 16u ^ turn(step)) << 5) + lane % 4u * 8u;
+      stage += half * 32u * PITCH * 16u + lane % 4u * 8u;
       typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const char* p = stage + step * PITCH * 16u + ((first / 16u ^ turn(step)) << 5);
       const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)));
-      const char* q = stage + (step + 4u) * PITCH * 16u + ((first / 16u ^ turn(step + 4u)) << 5) + lane % 4u * 8u;
+      const char* q = stage + (step + 4u) * PITCH * 16u + ((first / 16u ^ turn(step + 4u)) << 5);
       const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q)));
       return u32x4{lo.x, lo.y, hi.x, hi.y};
     }
@@ -286,27 +289,29 @@ struct Operand {
 
 // What a wavefront multiplies at a time: 16 rows x 64 bytes, or 32 x 64 for the matrix instruction for 8 bits.
 template <Arithmetic M, class O>
-__device__ __forceinline__ auto fragment_of(const char* stage, uint32_t first) {
+__device__ __forceinline__ auto fragment_of(const char* stage, uint32_t first, uint32_t half) {
   if constexpr (M == kNative8)
-    return __builtin_bit_cast(i32x8, __builtin_shufflevector(O::template fragment<32>(stage, first, 0), O::template fragment<32>(stage, first, 1), 0, 1, 2, 3, 4, 5, 6, 7));
-  else return O::template fragment<16>(stage, first, 0);
+    return __builtin_bit_cast(i32x8, __builtin_shufflevector(O::template fragment<32>(stage, first, half, 0), O::template fragment<32>(stage, first, half, 1), 0, 1, 2, 3, 4, 5, 6, 7));
+  else return O::template fragment<16>(stage, first, half, 0);
 }
 
-// A workgroup computes BM x BN of the output, WR x WC wavefronts a part each.  While the matrix cores work on one stage, the
-// next fragments are read from the LDS and loads straight into the LDS bring later stages, one between every few of a
-// wavefront's multiplications: loads that are issued together hold up what comes after them.  The matrix instruction has the
+// A workgroup computes BM x BN of the output, WR x WC wavefronts a part each.  While the matrix cores work on half a stage, the
+// next half's fragments are read from the LDS and loads straight into the LDS bring later stages, one between every few of a
+// wavefront's multiplications: loads that are issued together hold up what comes after them.  The LDS holds AHEAD + 1 stages of one
+// operand and AHEAD of the other: in the first half of stage k the former's stage k + AHEAD is asked for, and in its second half, when
+// every wavefront has read its last fragments of stage k, the latter's takes the place of stage k.  The matrix instruction has the
 // output's columns as its rows, so that a lane holds 4 neighbouring columns of one row.  It is the one for blocks of 16 x 16: what
 // bounds long products is power, and from registers alone it reaches 1.98 PFLOP/s in bf16 where the one for 32 x 32 reaches 1.70.
-template <Arithmetic M, Product P, uint32_t BM, uint32_t BN, uint32_t WR, uint32_t WC>
+template <Arithmetic M, Product P, uint32_t BM, uint32_t BN, uint32_t WR, uint32_t WC, uint32_t AHEAD>
 __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs a) {
   constexpr uint32_t THREADS = WR * WC * 64u, E = M == kWidened || M == kNative8 ? 1u : 2u, DEEP = kStageBytes / E;
-  constexpr uint32_t SIDE = M == kNative8 ? 32u : 16u, NA = BM / WR / SIDE, NB = BN / WC / SIDE, STAGE = (BM + BN) * kStageBytes;
+  constexpr uint32_t SIDE = M == kNative8 ? 32u : 16u, NA = BM / WR / SIDE, NB = BN / WC / SIDE;
   constexpr bool A_ALONG = P != kGradW, B_ALONG = P == kForward;
   using A = Operand<A_ALONG, BM, THREADS>;
   using B = Operand<B_ALONG, BN, THREADS>;
-  constexpr uint32_t LOADS = A::LOADS + B::LOADS;   // a thread's, of a stage
+  constexpr uint32_t A_STAGE = BM * kStageBytes, B_STAGE = BN * kStageBytes;
   using Block = std::conditional_t<M == kNative8, f32x16, f32x4>;
-  __shared__ __align__(1024) char lds[kStages * STAGE];
+  __shared__ __align__(1024) char lds_a[(AHEAD + 1u) * A_STAGE], lds_b[AHEAD * B_STAGE];
   const char* zeros = reinterpret_cast<const char*>(page_of_zeros);
   asm volatile("" : "+s"(zeros));   // an address in registers: not looked up again at every load
   const uint32_t out_cols = P == kForward ? a.wide : a.cols, across = (out_cols + BN - 1u) / BN;
@@ -322,16 +327,16 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
   // Where the thread's pieces are.  Rows and columns past the tile's end stand for its last ones: what they make is not stored.
   A la;
   B lb;
+  la.still = 0u;
 #pragma unroll
   for (uint32_t i = 0; i < A::LOADS; ++i) {
     if constexpr (A_ALONG) {
       uint32_t r = min(r0 + A::row(i), out_rows - 1u);
       if (P == kForward && a.index != nullptr) r = static_cast<uint32_t>(a.index[r]);
       la.at[i] = a.a.data + r * a.a.stride + A::piece(i) * 16u;
-      la.step[i] = kStageBytes;
       if (P == kForward && r >= a.indexed_rows) {           // zeros from the first stage to the last
         la.at[i] = zeros;
-        la.step[i] = 0u;
+        la.still |= 1u << i;
       }
     } else {
       la.at[i] = a.a.data + min(r0 / 8u + A::piece(i), (a.wide - 1u) / 8u) * 16ull + (static_cast<uint64_t>(g.begin) + A::row(i)) * a.a.stride;
@@ -360,126 +365,143 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
     } else {
       lb.at[i] = a.b.data + min(c0 / 8u + B::piece(i), (a.cols - 1u) / 8u) * 16ull;
       if constexpr (P == kGradX) lb.at[i] += (w0 + B::row(i)) * a.b.stride;
-      else lb.step[i] = indexed(B::row(i));
+      else lb.next[i] = indexed(B::row(i));
     }
   }
 
-  // Ask for a thread's load i of a stage, into the LDS at `slot`.  What lies behind the end of the sum, in its last stage, comes from
+  // Ask for a thread's load i of stage k, into the LDS at `slot`.  What lies behind the end of the sum, in its last stage, comes from
   // a page of zeros.
-  const uint32_t here = lds_address(lds) + __builtin_amdgcn_readfirstlane(threadIdx.x & ~63u) * 16u;
-  auto load = [&](uint32_t k, uint32_t slot, uint32_t i, bool last) {
-    if (i < A::LOADS) {
-      const char* from = la.at[i];
-      if constexpr (A_ALONG) {
-        if (last && k * kStageBytes + A::piece(i) * 16u >= depth * E) from = zeros;
-        la.at[i] += P == kForward ? la.step[i] : kStageBytes;
-      } else {
-        if (last && k * DEEP + A::row(i) >= depth) from = zeros;
-        la.at[i] += DEEP * a.a.stride;
-      }
-      load_to_lds(from, here + slot + i * THREADS * 16u);
+  const uint32_t mine = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63u) * 16u;
+  const uint32_t here_a = lds_address(lds_a) + mine, here_b = lds_address(lds_b) + mine;
+  auto load_a = [&](uint32_t k, uint32_t slot, uint32_t i, bool last) {
+    const char* from = la.at[i];
+    if constexpr (A_ALONG) {
+      if (last && k * kStageBytes + A::piece(i) * 16u >= depth * E) from = zeros;
+      la.at[i] += P == kForward && (la.still >> i & 1u) ? 0u : kStageBytes;
     } else {
-      i -= A::LOADS;
-      const char* from = lb.at[i];
-      if constexpr (B_ALONG) {
-        if (last && k * kStageBytes + B::piece(i) * 16u >= depth * E) from = zeros;
-        lb.at[i] += kStageBytes;
-      } else if constexpr (P == kGradX) {
-        if (last && k * DEEP + B::row(i) >= depth) from = zeros;
-        lb.at[i] += DEEP * a.b.stride;
-      } else {
-        from = lb.step[i] < a.indexed_rows ? from + lb.step[i] * a.b.stride : zeros;
-        lb.step[i] = indexed((k + 1u) * DEEP + B::row(i));
-      }
-      load_to_lds(from, here + slot + BM * kStageBytes + i * THREADS * 16u);
+      if (last && k * DEEP + A::row(i) >= depth) from = zeros;
+      la.at[i] += DEEP * a.a.stride;
     }
+    load_to_lds(from, here_a + slot + i * THREADS * 16u);
+  };
+  auto load_b = [&](uint32_t k, uint32_t slot, uint32_t i, bool last) {
+    const char* from = lb.at[i];
+    if constexpr (B_ALONG) {
+      if (last && k * kStageBytes + B::piece(i) * 16u >= depth * E) from = zeros;
+      lb.at[i] += kStageBytes;
+    } else if constexpr (P == kGradX) {
+      if (last && k * DEEP + B::row(i) >= depth) from = zeros;
+      lb.at[i] += DEEP * a.b.stride;
+    } else {
+      from = lb.next[i] < a.indexed_rows ? from + lb.next[i] * a.b.stride : zeros;
+      lb.next[i] = indexed((k + 1u) * DEEP + B::row(i));
+    }
+    load_to_lds(from, here_b + slot + i * THREADS * 16u);
   };
   // The piece that the sum ends in has what is behind the row's end: that is blanked.
   const bool ragged = (A_ALONG || B_ALONG) && depth * E % 16u != 0u;
-  auto trim = [&](char* stage) {
+  auto trim = [&](char* stage_a, char* stage_b) {
     const uint32_t tail = depth * E % kStageBytes, p = tail / 16u;
-    const uint32_t from = A_ALONG ? 0u : BM, to = B_ALONG ? BM + BN : BM;
-    for (uint32_t r = from + threadIdx.x; r < to; r += THREADS) {   // B's rows follow A's
-      char* piece = stage + r * kStageBytes + ((p ^ (r >> 2 & 3u)) << 4);
+    auto blank_rows = [&](char* stage, uint32_t rows) {
+      for (uint32_t r = threadIdx.x; r < rows; r += THREADS) {
+        char* piece = stage + r * kStageBytes + ((p ^ (r >> 1 & 7u)) << 4);
 #pragma unroll
-      for (uint32_t b = 0; b < 16u; b += E)
-        if (b >= tail % 16u) {
-          if constexpr (E == 1) piece[b] = 0;
-          else *reinterpret_cast<uint16_t*>(piece + b) = 0;
-        }
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        for (uint32_t b = 0; b < 16u; b += E)
+          if (b >= tail % 16u) {
+            if constexpr (E == 1) piece[b] = 0;
+            else *reinterpret_cast<uint16_t*>(piece + b) = 0;
+          }
+      }
+    };
+    if (A_ALONG) blank_rows(stage_a, BM);
+    if (B_ALONG) blank_rows(stage_b, BN);
+    wait_for_reads<0>();   // and the writes
   };
 
   const uint32_t wave = threadIdx.x / 64u, lane = threadIdx.x & 63u;
   const uint32_t ra = wave / WC * (BM / WR), cb = wave % WC * (BN / WC);
   Block acc[NB][NA] = {};
-  using Fragment = decltype(fragment_of<M, A>(lds, 0));
+  using Fragment = decltype(fragment_of<M, A>(lds_a, 0, 0));
   Fragment fa[NA], fb[2][NB];
-  uint32_t next_slot = STAGE, load_slot = kAhead * STAGE;   // bytes
-  // Stage k, whose fragments are fa and fb[TURN]: multiply, and bring the next ones.  STEADY: stage k + kAhead is there to be asked for, and
-  // is not the last.
-  auto work = [&](uint32_t k, auto steady, auto turn_) {
-    constexpr bool STEADY = decltype(steady)::value;
-    constexpr uint32_t TURN = decltype(turn_)::value;
-    const char* next = lds + next_slot;   // behind the last stage: read, and not used
-    if constexpr (STEADY) {
-      wait_for_stage<(kAhead - 2u) * LOADS>();
-    } else if (k + 1u < steps) {
-      wait_for_stage<0>();
-      if (ragged && k + 2u == steps) trim(lds + next_slot);
-    }
+  uint32_t a_slot = 0, b_slot = 0;   // stage k's, bytes
+  auto after = [](uint32_t slot, uint32_t by, uint32_t end) { return slot + by >= end ? slot + by - end : slot + by; };
+  // Half a stage, whose fragments are fa and fb[HALF]: multiply, and read the next half's.  `load(i)` asks for a load of a later stage,
+  // FROM: not before that many rows of blocks are done.
+  auto multiply_half = [&](auto half, const char* next_a, const char* next_b, auto count, auto from, auto&& load) {
+    constexpr uint32_t HALF = decltype(half)::value, COUNT = decltype(count)::value, FROM = decltype(from)::value;
 #pragma unroll
-    for (uint32_t n = 0; n < NB; ++n) fb[TURN ^ 1u][n] = fragment_of<M, B>(next + BM * kStageBytes, cb + n * SIDE);
+    for (uint32_t n = 0; n < NB; ++n) fb[HALF ^ 1u][n] = fragment_of<M, B>(next_b, cb + n * SIDE, HALF ^ 1u);
 #pragma unroll
     for (uint32_t m = 0; m < NA; ++m) {
       if constexpr (M == kWidened) {
         const Widened x = widen_e4m3(fa[m]);
 #pragma unroll
         for (uint32_t n = 0; n < NB; ++n) {
-          const Widened w = widen_e4m3(fb[TURN][n]);
+          const Widened w = widen_e4m3(fb[HALF][n]);
           acc[n][m] = multiply<M>(w.low, x.low, acc[n][m]);
           acc[n][m] = multiply<M>(w.high, x.high, acc[n][m]);
         }
       } else {
 #pragma unroll
         for (uint32_t n = 0; n < NB; ++n) {
-          if constexpr (M == kNative8) acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[TURN][n], fa[m], acc[n][m], 0, 0, 0, 0, 0, 0);
-          else acc[n][m] = multiply<M>(fb[TURN][n], fa[m], acc[n][m]);
+          if constexpr (M == kNative8) acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[HALF][n], fa[m], acc[n][m], 0, 0, 0, 0, 0, 0);
+          else acc[n][m] = multiply<M>(fb[HALF][n], fa[m], acc[n][m]);
         }
       }
       __builtin_amdgcn_sched_barrier(0);   // the next fragment takes the registers of this one
-      fa[m] = fragment_of<M, A>(next, ra + m * SIDE);
-      if (STEADY || k + kAhead < steps)
+      fa[m] = fragment_of<M, A>(next_a, ra + m * SIDE, HALF ^ 1u);
+      if constexpr (FROM != 0u)
+        if (m + 1u == FROM) load(COUNT);   // the wait that lets the loads begin
+      if (m >= FROM)
 #pragma unroll
-        for (uint32_t i = m * LOADS / NA; i < (m + 1u) * LOADS / NA; ++i) load(k + kAhead, load_slot, i, !STEADY);
+        for (uint32_t i = (m - FROM) * COUNT / (NA - FROM); i < (m + 1u - FROM) * COUNT / (NA - FROM); ++i) load(i);
       __builtin_amdgcn_sched_barrier(0);
     }
-    next_slot = next_slot + STAGE == kStages * STAGE ? 0u : next_slot + STAGE;
-    load_slot = load_slot + STAGE == kStages * STAGE ? 0u : load_slot + STAGE;
+  };
+  using First = std::integral_constant<uint32_t, 0>;
+  using Second = std::integral_constant<uint32_t, 1>;
+  // A quarter into the second half a wavefront has had all it asked of the stage before: what is newer are the other half's reads
+  using Quarter = std::integral_constant<uint32_t, NA / 4u == 0u ? 1u : NA / 4u>;
+  // STEADY: stage k + AHEAD is there to be asked for, and is not the last
+  auto work = [&](uint32_t k, auto steady) {
+    constexpr bool STEADY = decltype(steady)::value;
+    const bool more = STEADY || k + AHEAD < steps, last = !STEADY && k + AHEAD + 1u == steps;
+    const uint32_t a_next = after(a_slot, A_STAGE, (AHEAD + 1u) * A_STAGE), b_next = after(b_slot, B_STAGE, AHEAD * B_STAGE);
+    const uint32_t a_load = after(a_slot, AHEAD * A_STAGE, (AHEAD + 1u) * A_STAGE);
+    multiply_half(First{}, lds_a + a_slot, lds_b + b_slot, std::integral_constant<uint32_t, A::LOADS>{}, First{}, [&](uint32_t i) {
+      if (more) load_a(k + AHEAD, a_load, i, last);
+    });
+    if (more) wait_for_loads<(AHEAD - 2u) * (A::LOADS + B::LOADS) + A::LOADS>();
+    else if (k + 1u < steps) wait_for_loads<0>();
+    if (!STEADY && ragged && k + 2u == steps) trim(lds_a + a_next, lds_b + b_next);
+    // behind the last stage: read, and not used
+    multiply_half(Second{}, lds_a + a_next, lds_b + b_next, std::integral_constant<uint32_t, B::LOADS>{}, Quarter{}, [&](uint32_t i) {
+      if (!more) return;
+      if (i == B::LOADS) wait_for_reads<NB + Quarter::value - 1u>();
+      else load_b(k + AHEAD, b_slot, i, last);
+    });
+    a_slot = a_next;
+    b_slot = b_next;
   };
   if (steps != 0u) {
 #pragma unroll
-    for (uint32_t k = 0; k < kAhead; ++k)
-      if (k < steps)
+    for (uint32_t k = 0; k < AHEAD; ++k)
+      if (k < steps) {
 #pragma unroll
-        for (uint32_t i = 0; i < LOADS; ++i) load(k, k * STAGE, i, k + 1u == steps);
-    if (steps >= kAhead) wait_for_stage<(kAhead - 1u) * LOADS>();
-    else wait_for_stage<0>();
-    if (ragged && steps == 1u) trim(lds);
+        for (uint32_t i = 0; i < A::LOADS; ++i) load_a(k, k * A_STAGE, i, k + 1u == steps);
 #pragma unroll
-    for (uint32_t n = 0; n < NB; ++n) fb[0][n] = fragment_of<M, B>(lds + BM * kStageBytes, cb + n * SIDE);
+        for (uint32_t i = 0; i < B::LOADS; ++i) load_b(k, k * B_STAGE, i, k + 1u == steps);
+      }
+    if (steps >= AHEAD) wait_for_loads<(AHEAD - 1u) * (A::LOADS + B::LOADS)>();
+    else wait_for_loads<0>();
+    if (ragged && steps == 1u) trim(lds_a, lds_b);
 #pragma unroll
-    for (uint32_t m = 0; m < NA; ++m) fa[m] = fragment_of<M, A>(lds, ra + m * SIDE);
+    for (uint32_t n = 0; n < NB; ++n) fb[0][n] = fragment_of<M, B>(lds_b, cb + n * SIDE, 0);
+#pragma unroll
+    for (uint32_t m = 0; m < NA; ++m) fa[m] = fragment_of<M, A>(lds_a, ra + m * SIDE, 0);
     uint32_t k = 0;
-    for (; k + kAhead + 2u < steps; k += 2u) {
-      work(k, std::true_type{}, std::integral_constant<uint32_t, 0>{});
-      work(k + 1u, std::true_type{}, std::integral_constant<uint32_t, 1>{});
-    }
-    for (; k < steps; k += 2u) {
-      work(k, std::false_type{}, std::integral_constant<uint32_t, 0>{});
-      if (k + 1u < steps) work(k + 1u, std::false_type{}, std::integral_constant<uint32_t, 1>{});
-    }
+    for (; k + AHEAD + 1u < steps; ++k) work(k, std::true_type{});
+    for (; k < steps; ++k) work(k, std::false_type{});
   }
 
 #pragma unroll
@@ -524,7 +546,7 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
 // ---- few rows a group -------------------------------------------------------------------------------
 
 template <uint32_t N>
-__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_for_own_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // kForward for groups of about 16 rows and less, where the reading of the weights is all there is to do: a workgroup computes
 // 16 rows x WIDE columns, and every wavefront a part of the sum for them, 128 bytes along it at a time in turn with the others.
@@ -583,9 +605,9 @@ __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs a) 
     if (wave + i * WAVES < stages) load(wave + i * WAVES, i);
   uint32_t slot = 0;
   for (uint32_t k = wave; k < stages; k += WAVES) {
-    if (k + (RING - 1u) * WAVES < stages) wait_for_loads<(RING - 1u) * LOADS>();
-    else if (k + (RING - 2u) * WAVES < stages) wait_for_loads<(RING - 2u) * LOADS>();
-    else wait_for_loads<0>();
+    if (k + (RING - 1u) * WAVES < stages) wait_for_own_loads<(RING - 1u) * LOADS>();
+    else if (k + (RING - 2u) * WAVES < stages) wait_for_own_loads<(RING - 2u) * LOADS>();
+    else wait_for_own_loads<0>();
     char* stage = lds[wave][slot];
     if (k + 1u == stages && bytes % 16u != 0u && lane < ROWS) {   // the piece that the rows end in
       char* last = stage + lane * TURN + ((bytes % TURN / 16u ^ (lane >> 1 & 7u)) << 4);

@@ -96,14 +96,35 @@ int product_tiles(K kernel, uint32_t bm, uint32_t bn, uint32_t threads, const Pr
   return enqueue(kernel, dim3(static_cast<uint32_t>(tiles)), threads, s, a);
 }
 
-// Tiles of 256 x 256 do twice the work for what they read of tiles of 128 x 128, and leave more of themselves empty where groups are
-// small.  Measured on groups of 256 rows (ragged, 16 groups, 7168 -> 2048, e4m3): 133 against 165 us; of 8 rows (32 groups, bf16): 151
-// against 92 us; of 125 rows (24 groups, 2043 -> 1003, f16): 51 against 46 us.
-bool takes_large_tiles(const ProductArgs& a) { return a.rows / 192u >= a.groups; }
+// What a tile costs is about the same whether one compute unit works or all do, and a launch takes as long as the compute units
+// that get one tile more than others.  256 x 256 does the most work for what it reads; smaller tiles leave less of themselves empty
+// in small groups and fill the machine when there are few.  In units of a tile of 256 x 256 (which takes 196 us with a depth of 7168
+// in bf16, one a compute unit), 128 x 256 costs 0.69 and 128 x 128 0.45.  Measured in bf16, 256 x 256 / 128 x 256 / 128 x 128, us: 4096 rows in 16 ragged
+// groups, 7168 -> 2048, 201 / 223 / 234; 2048 rows 192 / 139 / 161; 1024 rows 181 / 120 / 115; 2999 rows in 24 groups, 2043 -> 1003, 57 / 35 / 45;
+// 8190 rows in 16 groups, 2048 -> 7168, 303 / 305 / 372; 512 rows in one group, 2048 -> 2048, 43 / 26 / 18.
+enum Tile : uint32_t { kTile256, kTile128x256, kTile128 };
 
-// Measured with 32 groups, 7168 -> 2048, against tiles of 128 x 128: 8 rows a group in bf16 155 against 193 us, 16 rows 161 against 189,
+template <Product P>
+Tile choose_tile(const ProductArgs& a) {
+  auto cost = [&](uint32_t high, uint32_t wide, double unit) {
+    // a group's last tile is half empty on average
+    const double down = P == kGradW ? static_cast<double>(a.groups) * blocks_for(a.wide, high)
+                                    : static_cast<double>(a.rows) / high + 0.5 * (a.groups < a.rows ? a.groups : a.rows);
+    return ceil(down * blocks_for(P == kForward ? a.wide : a.cols, wide) / 256.0) * unit;
+  };
+  const double large = cost(256u, 256u, 1.0), middle = cost(128u, 256u, 0.69), small = cost(128u, 128u, 0.45);
+  return large <= middle && large <= small ? kTile256 : middle <= small ? kTile128x256 : kTile128;
+}
+
+// Measured with 32 groups, 7168 -> 2048, bf16, against tiles of 128 x 128: 8 rows a group in bf16 155 against 193 us, 16 rows 161 against 189,
 // 32 rows 226 against 193.
 bool takes_few_rows(const ProductArgs& a) { return a.rows / 20u < a.groups; }
+
+// 8-bit operands are widened to bf16 and multiplied exactly, at the rate of 16 bits, but where the product is bound by
+// arithmetic and what the matrix instruction for 8 bits drops cannot be seen: it adds 64 products at a time and keeps of each what
+// is above about 2^-13 of the greatest (measured: at most 2^-12 of it lost in all), which over 512 and more terms is 2^-18 of
+// their magnitudes on random values, under the 2^-8 that rounding to 16 bits costs the result.
+bool takes_8_bit_instruction(const ProductArgs& a) { return a.out_type != kOutF32 && a.cols >= 512u; }
 
 template <Arithmetic M, Product P>
 int product_of(const ProductArgs& a, hipStream_t s) {
@@ -115,23 +136,23 @@ int product_of(const ProductArgs& a, hipStream_t s) {
       if (static_cast<uint64_t>(groups) * blocks_for(a.wide, 32u) <= 256u) return product_tiles<P>(product_few_kernel<M, 16, 8>, 16, 16, 512, a, s);
       return product_tiles<P>(product_few_kernel<M, 32, 4>, 16, 32, 256, a, s);
     }
-  if (takes_large_tiles(a)) return product_tiles<P>(product_tile_kernel<M, P, 256, 256, 2, 4>, 256, 256, 512, a, s);
-  return product_tiles<P>(product_tile_kernel<M, P, 128, 128, 2, 2>, 128, 128, 256, a, s);
+  const Tile tile = choose_tile<P>(a);
+  if constexpr (M == kWidened) {
+    if (tile != kTile128 && takes_8_bit_instruction(a)) {
+      if (tile == kTile256) return product_tiles<P>(product_tile_kernel<kNative8, P, 256, 256, 2, 4, 2>, 256, 256, 512, a, s);
+      return product_tiles<P>(product_tile_kernel<kNative8, P, 128, 256, 2, 4, 3>, 128, 256, 512, a, s);
+    }
+  } else {
+    if (tile == kTile256) return product_tiles<P>(product_tile_kernel<M, P, 256, 256, 2, 4, 2>, 256, 256, 512, a, s);
+    if (tile == kTile128x256) return product_tiles<P>(product_tile_kernel<M, P, 128, 256, 2, 4, 3>, 128, 256, 512, a, s);
+  }
+  return product_tiles<P>(product_tile_kernel<M, P, 128, 128, 2, 4, 4>, 128, 128, 512, a, s);
 }
-
-// 8-bit operands are widened to bf16 and multiplied exactly, at the rate of 16 bits, but where the product is bound by
-// arithmetic and what the matrix instruction for 8 bits drops cannot be seen: it adds 64 products at a time and keeps of each what
-// is above about 2^-13 of the greatest (measured: at most 2^-12 of it lost in all), which over 512 and more terms is 2^-18 of
-// their magnitudes on random values, under the 2^-8 that rounding to 16 bits costs the result.
-bool takes_8_bit_instruction(const ProductArgs& a) { return a.out_type != kOutF32 && a.cols >= 512u && takes_large_tiles(a); }
 
 template <Product P>
 int product(const ProductArgs& a, uint32_t dtype, hipStream_t s) {
   if constexpr (P == kForward)
-    if (dtype == UCCL_E4M3) {
-      if (takes_8_bit_instruction(a)) return product_tiles<P>(product_tile_kernel<kNative8, P, 256, 256, 2, 4>, 256, 256, 512, a, s);
-      return product_of<kWidened, P>(a, s);
-    }
+    if (dtype == UCCL_E4M3) return product_of<kWidened, P>(a, s);
   return dtype == UCCL_BF16 ? product_of<kBf16, P>(a, s) : product_of<kF16, P>(a, s);
 }
 

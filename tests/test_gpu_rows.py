@@ -316,6 +316,78 @@ def test_group_product_gradients(uccl, dtype, sizes, k, n):
             at += c
 
 
+# rows by group and columns that take tiles of 256 x 256, of 128 x 256 and (over several rounds of the machine) of 128 x 128
+LARGE = {"256x256": ([1100, 0, 1901], 4100), "128x256": ([1299], 4103), "128x128": ([257, 300, 0, 90], 2050), "64 groups": ([41 + g % 7 for g in range(67)], 777)}
+
+
+def in_pieces(f, n, step=1024):
+    """Of long columns, a piece at a time: 64-bit references of large outputs."""
+    for at in range(0, n, step):
+        f(slice(at, min(n, at + step)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "e4m3"])
+@pytest.mark.parametrize("shape", list(LARGE))
+@pytest.mark.parametrize("k", [40, 64, 200, 521, 1003])
+def test_group_product_of_many_tiles(uccl, dtype, shape, k):
+    counts, n = LARGE[shape]
+    g, rows, groups = gen(k + n), sum(counts), len(counts)
+    t = T["bf16" if dtype == "e4m3" else dtype]
+    x, xs, w, ws, ex, ew = product_inputs(g, dtype, rows, k, n, groups, 2)
+    index = torch.randint(0, rows + 2, (rows,), device="cuda", generator=g).to(torch.int32)
+    index[7] = -1
+    there = index >= 0
+    for idx, out in ((None, torch.float32), (index, t)):
+        y = aligned(rows, n, out, 1, fill=7.0)
+        around = margin(y)
+        uccl.uccl_group_product(y, x, w, offsets_of(counts), index=idx, x_scales=xs, w_scales=ws)
+        a_all = ex[:rows] if idx is None else torch.where(there[:, None], ex[index.long().clamp(min=0)], 0.0)
+        at = 0
+        for e, c in enumerate(counts):
+            a = a_all[at:at + c]
+            in_pieces(lambda s: close(y[at:at + c, s], a @ ew[e, s].T, a.abs() @ ew[e, s].abs().T, k + 4, f"group {e}"), n)
+            at += c
+        assert torch.equal(margin(y), around)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", list(LARGE))
+@pytest.mark.parametrize("n", [40, 333])
+def test_group_product_gradients_of_many_tiles(uccl, dtype, shape, n):
+    counts, k = LARGE[shape]
+    g, rows, groups, t = gen(k + n), sum(counts), len(counts), T[dtype]
+    x, _, w, _, ex, ew = product_inputs(g, dtype, rows, k, n, groups, 2)
+    dy = normal(g, rows, n, t)
+    index = torch.randperm(rows, device="cuda", generator=g).to(torch.int32)
+    index[5] = rows + 2
+    dx, dw = aligned(rows, k, t, 1, fill=7.0), aligned(groups * n, k, torch.float32, 1, fill=7.0)
+    around = margin(dx), margin(dw)
+    uccl.uccl_group_product_grad_x(dx, dy, w, offsets_of(counts))
+    uccl.uccl_group_product_grad_w(dw.unflatten(0, (groups, n)), dy, x, offsets_of(counts), index=index)
+    assert torch.equal(margin(dx), around[0]) and torch.equal(margin(dw), around[1])
+    rows_x = torch.where((index < rows + 2)[:, None], ex[index.long().clamp(max=rows + 1)], 0.0)
+    at = 0
+    for e, c in enumerate(counts):
+        d, a = dy[at:at + c].double(), rows_x[at:at + c]
+        in_pieces(lambda s: close(dx[at:at + c, s], d @ ew[e][:, s], d.abs() @ ew[e][:, s].abs(), n + 4, f"dx, group {e}"), k)
+        in_pieces(lambda s: close(dw.unflatten(0, (groups, n))[e][:, s], d.T @ a[:, s], d.abs().T @ a[:, s].abs(), c + 4, f"dw, group {e}"), k)
+        at += c
+
+
+@pytest.mark.parametrize("n,k", [(2900, 2300), (630, 4100)])
+def test_gradient_of_the_weights_in_large_tiles(uccl, n, k):
+    counts = [70, 0, 129]
+    g, rows, t = gen(n), sum(counts), torch.bfloat16
+    x, dy = normal(g, rows, k, t), normal(g, rows, n, t)
+    dw = aligned(3 * n, k, torch.bfloat16, fill=7.0)
+    uccl.uccl_group_product_grad_w(dw.unflatten(0, (3, n)), dy, x, offsets_of(counts))
+    at = 0
+    for e, c in enumerate(counts):
+        d, a = dy[at:at + c].double(), x[at:at + c].double()
+        in_pieces(lambda s: close(dw[e * n:(e + 1) * n, s], d.T @ a[:, s], d.abs().T @ a[:, s].abs(), c + 4, f"dw, group {e}"), k)
+        at += c
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 def test_what_is_beside_the_rows_changes_nothing(uccl, dtype):
     """NaN in rows of other groups, in rows that no index names, in the pieces behind a row's end and in w of other groups."""

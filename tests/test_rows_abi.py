@@ -228,3 +228,73 @@ def test_kernels_use_no_scratch_memory(tmp_path):
     assert len(re.findall(r"\.name: +_Z\S*kernel", notes)) > 10
     assert set(re.findall(r"\.private_segment_fixed_size: +(\d+)", notes)) == {"0"}
     assert set(re.findall(r"\.vgpr_spill_count: +(\d+)", notes)) == {"0"}
+
+
+# ---- which kernel a product is launched as: the HIP runtime of tests/hip_stub.c reports it, nothing runs ----------------
+
+def product_kernels(rt):
+    """(what is multiplied, kernel as it is named in the library) of products by rows, groups, columns and depth."""
+    for dtype, rows_, groups, wide, cols, out, kernel in (
+        (BF16, 1, 1, 2048, 7168, BF16, "few_kernelILNS_10ArithmeticE0ELj16ELj8E"),
+        (BF16, 16, 32, 2048, 7168, BF16, "few_kernelILNS_10ArithmeticE0ELj32ELj4E"),
+        (F16, 128, 32, 2048, 7168, F16, "few_kernelILNS_10ArithmeticE1ELj32ELj4E"),
+        (E4M3, 128, 32, 2048, 7168, BF16, "few_kernelILNS_10ArithmeticE2ELj32ELj4E"),
+        (E4M3, 4096, 16, 2048, 7168, BF16, "tile_kernelILNS_10ArithmeticE3ELNS_7ProductE0ELj256ELj256E"),
+        (E4M3, 2048, 16, 2048, 7168, BF16, "tile_kernelILNS_10ArithmeticE3ELNS_7ProductE0ELj128ELj256E"),
+        (E4M3, 4096, 16, 2048, 7168, F32, "tile_kernelILNS_10ArithmeticE2ELNS_7ProductE0ELj128ELj128E"),   # exact where it can be seen
+        (E4M3, 4096, 16, 2048, 500, BF16, "tile_kernelILNS_10ArithmeticE2ELNS_7ProductE0ELj128ELj128E"),
+        (E4M3, 512, 1, 2048, 7168, BF16, "tile_kernelILNS_10ArithmeticE2ELNS_7ProductE0ELj128ELj128E"),
+        (BF16, 4096, 16, 2048, 7168, BF16, "tile_kernelILNS_10ArithmeticE0ELNS_7ProductE0ELj256ELj256E"),
+        (F16, 2999, 24, 1003, 2043, F16, "tile_kernelILNS_10ArithmeticE1ELNS_7ProductE0ELj128ELj256E"),
+        (BF16, 512, 1, 2048, 2048, BF16, "tile_kernelILNS_10ArithmeticE0ELNS_7ProductE0ELj128ELj128E"),
+        # those of tests/test_gpu_rows.py that are there for the large tiles
+        (BF16, 3001, 3, 4100, 40, BF16, "tile_kernelILNS_10ArithmeticE0ELNS_7ProductE0ELj256ELj256E"),
+        (BF16, 1299, 1, 4103, 40, BF16, "tile_kernelILNS_10ArithmeticE0ELNS_7ProductE0ELj128ELj256E"),
+        (E4M3, 3001, 3, 4100, 521, BF16, "tile_kernelILNS_10ArithmeticE3ELNS_7ProductE0ELj256ELj256E"),
+        (E4M3, 1299, 1, 4103, 521, BF16, "tile_kernelILNS_10ArithmeticE3ELNS_7ProductE0ELj128ELj256E"),
+        (BF16, 647, 4, 2050, 40, BF16, "tile_kernelILNS_10ArithmeticE0ELNS_7ProductE0ELj128ELj128E"),
+    ):
+        rt.launches.clear(), rt.symbols.clear()
+        make = (lambda n, c: q8(n, c)) if dtype == E4M3 else (lambda n, c: rows(n, c, dtype))
+        y, x, w = rows(rows_, wide, out), make(rows_, cols), make(groups * wide, cols)
+        assert rt.lib.uccl_group_product(y, x, None, w, M, groups, None) == OK
+        assert len(rt.symbols) == 1 and kernel in rt.symbols[0], (rt.symbols, kernel)
+    for rows_, groups, wide, cols, x_kernel, w_kernel in (
+        (4096, 16, 2048, 7168, "ProductE1ELj256ELj256E", "ProductE2ELj256ELj256E"),
+        (1299, 1, 40, 4103, "ProductE1ELj128ELj256E", "ProductE2ELj128ELj128E"),
+        (199, 3, 2900, 2300, "ProductE1ELj128ELj128E", "ProductE2ELj256ELj256E"),
+        (199, 3, 630, 4100, "ProductE1ELj128ELj128E", "ProductE2ELj128ELj256E"),
+    ):
+        rt.symbols.clear()
+        dy, x, w = rows(rows_, wide), rows(rows_, cols), rows(groups * wide, cols)
+        assert rt.lib.uccl_group_product_grad_x(x, dy, w, M, groups, None) == OK
+        assert rt.lib.uccl_group_product_grad_w(w, dy, x, None, M, groups, None) == OK
+        assert x_kernel in rt.symbols[0] and w_kernel in rt.symbols[1], rt.symbols
+    # the grid: a workgroup for every tile that there could be, by eights, and a launch that HIP could not take is refused
+    rt.launches.clear()
+    assert rt.lib.uccl_group_product(rows(512, 2048), rows(512, 2048), None, rows(2048, 2048), M, 1, None) == OK
+    assert rt.launches[-1][1:3] == ((512 // 128 + 1) * 16, 512)
+    rt.launches.clear()
+    big = (1 << 31) - 1
+    assert rt.lib.uccl_group_product(rows(big, 8 << 20), rows(big, 64), None, rows(8 << 20, 64), M, 1, None) == pkg.UCCL_ETOOBIG
+    assert rt.launches == []
+    assert rt.lib.uccl_combine_rows(rows(big, 1 << 20), rows(9, 1 << 20), M, None, 2, None, None) == pkg.UCCL_ETOOBIG
+    # launches that the runtime refuses come back as such
+    rt.refuse = lambda *a: True
+    assert rt.lib.uccl_group_product(rows(512, 2048), rows(512, 2048), None, rows(2048, 2048), M, 1, None) == pkg.UCCL_ELAUNCH
+    assert rt.lib.uccl_norm_rows(rows(2, 8), None, None, rows(2, 8), None, B, C.byref(pkg.uccl_norm_opts(1e-6)), None) == pkg.UCCL_ELAUNCH
+    assert b"as the test asked" in rt.lib.uccl_last_error_detail()
+
+
+def test_which_kernel_a_product_is_launched_as(tmp_path):
+    import os
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    stub = str(tmp_path / "libamdhip64.so.7")
+    subprocess.check_call(["gcc", "-shared", "-fPIC", "-O1", "-Wl,-soname,libamdhip64.so.7", "-I/opt/rocm/include", os.path.join(here, "hip_stub.c"), "-o", stub])
+    code = (f"import sys; sys.path[:0] = [{here!r}, {os.path.dirname(here)!r}]\n"
+            f"import test_host_launches as h, test_rows_abi as t\n"
+            f"rt = h.Runtime({stub!r})\n"
+            f"for n, (r, a) in t.pkg.ROWS_SIGNATURES.items():\n    f = getattr(rt.lib, n); f.restype, f.argtypes = r, a\n"
+            f"t.product_kernels(rt)\n")
+    subprocess.run([sys.executable, "-c", code], check=True)
