@@ -154,10 +154,28 @@ def _nbytes(x):
     return 0 if x is None else x.numel() * x.element_size()
 
 
+def _find_current_stream():
+    """A function that returns the handle of torch's current stream on the current device (None where there is no GPU): by torch's
+    inner functions, 0.3 us, or, where a version does not have them, by a Stream object, 3.4 us."""
+    import torch
+    if not torch.cuda.is_available():
+        return lambda: None
+    device, raw = getattr(torch._C, "_cuda_getDevice", None), getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if device is None or raw is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    torch.cuda.init()
+    return lambda: raw(device())
+
+
+_current_stream = None
+
+
 def _stream(s):
+    global _current_stream
     if s is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
+        if _current_stream is None:
+            _current_stream = _find_current_stream()
+        return _current_stream()
     if isinstance(s, int):
         return s
     return s.cuda_stream

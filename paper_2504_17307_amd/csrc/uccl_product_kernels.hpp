@@ -162,8 +162,8 @@ __device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row,
   const uint32_t quarter = threadIdx.x % 64u / 16u;
   if (a.out_type == kOutF32) {
     const uint32_t c = first + quarter * 4u;
-    if (there && c < cols) store_piece(at, c / 4u, Piece<float>{x[0], x[1], x[2], x[3]}, cols - c);
-    if (there && c + 16u < cols) store_piece(at, c / 4u + 4u, Piece<float>{y[0], y[1], y[2], y[3]}, cols - c - 16u);
+    if (there && c < cols) store_piece<false>(at, c / 4u, Piece<float>{x[0], x[1], x[2], x[3]}, cols - c);
+    if (there && c + 16u < cols) store_piece<false>(at, c / 4u + 4u, Piece<float>{y[0], y[1], y[2], y[3]}, cols - c - 16u);
     return;
   }
   uint32_t wx[2], wy[2];
@@ -177,7 +177,7 @@ __device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row,
   const u32x2 s1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(wx[1], wy[1], false, false));
   const uint32_t c = first + quarter % 2u * 16u + quarter / 2u * 8u;
   const Piece<uint16_t> p = __builtin_bit_cast(Piece<uint16_t>, u32x4{s0.x, s1.x, s0.y, s1.y});
-  if (there && c < cols) store_piece(at, c / 8u, p, cols - c);
+  if (there && c < cols) store_piece<false>(at, c / 8u, p, cols - c);
 }
 __device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row, bool there, uint32_t first, uint32_t cols, f32x16 v) {
   // one block of 32 x 32: columns i / 4 * 8 + lane / 32 * 4 + i % 4
@@ -187,7 +187,7 @@ __device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row,
 #pragma unroll
     for (uint32_t i = 0; i < 4u; ++i) {
       const uint32_t c = first + i * 8u + half * 4u;
-      if (there && c < cols) store_piece(at, c / 4u, Piece<float>{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]}, cols - c);
+      if (there && c < cols) store_piece<false>(at, c / 4u, Piece<float>{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]}, cols - c);
     }
     return;
   }
@@ -201,7 +201,7 @@ __device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row,
     const u32x2 s1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(w[i + 1], w[i + 3], false, false));
     const uint32_t c = first + i * 4u + half * 8u;
     const Piece<uint16_t> p = __builtin_bit_cast(Piece<uint16_t>, u32x4{s0.x, s1.x, s0.y, s1.y});
-    if (there && c < cols) store_piece(at, c / 8u, p, cols - c);
+    if (there && c < cols) store_piece<false>(at, c / 8u, p, cols - c);
   }
 }
 

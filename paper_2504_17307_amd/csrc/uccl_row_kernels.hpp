@@ -36,31 +36,40 @@ struct NormArgs {
 __device__ __forceinline__ float add_square(float h, float shrink, float sum) { return __builtin_fmaf(h * shrink, h * shrink, sum); }
 
 // One workgroup a row.  h = x + r; s = rsqrt(mean h^2 + eps); y = h s w, from h as it was summed in 32 bits, not as it
-// is rounded for storage.  E8: y in e4m3 with a scale a row.
-template <class T, bool E8, uint32_t THREADS, uint32_t NV>
+// is rounded for storage.  E8: y in e4m3 with a scale a row.  All loads are issued before the first is waited for: threads past
+// the row's end load its last piece.
+template <class T, bool E8, uint32_t THREADS, uint32_t NV, bool ONCE>
 __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
   constexpr uint32_t N = Piece<T>::N;
   __shared__ float buffer[2][THREADS / 64u];
   const uint64_t row = blockIdx.x;
   const uint32_t pieces = (a.cols + N - 1) / N;
   const char* x = a.x.data + row * a.x.stride;
-  const char* r = a.r.data == nullptr ? nullptr : a.r.data + row * a.r.stride;
+  Piece<T> px[NV], pr[NV], w[NV];
+  uint32_t valid[NV];
+#pragma unroll
+  for (uint32_t k = 0; k < NV; ++k) px[k] = load_piece_once<T>(x, min(threadIdx.x + k * THREADS, pieces - 1u));
+  if (a.r.data != nullptr) {
+    const char* r = a.r.data + row * a.r.stride;
+#pragma unroll
+    for (uint32_t k = 0; k < NV; ++k) pr[k] = load_piece_once<T>(r, min(threadIdx.x + k * THREADS, pieces - 1u));
+  } else {
+#pragma unroll
+    for (uint32_t k = 0; k < NV; ++k) pr[k] = Piece<T>{};
+  }
+#pragma unroll
+  for (uint32_t k = 0; k < NV; ++k) w[k] = load_piece<T>(a.weight, min(threadIdx.x + k * THREADS, pieces - 1u));
   float h[NV][N];
   float ss = 0.0f;
 #pragma unroll
   for (uint32_t k = 0; k < NV; ++k) {
-    const uint32_t p = threadIdx.x + k * THREADS;
-    Piece<T> px{}, pr{};
-    if (p < pieces) {
-      px = load_piece<T>(x, p);
-      if (r != nullptr) pr = load_piece<T>(r, p);
-      const uint32_t valid = a.cols - p * N;
-      blank(px, valid);
-      blank(pr, valid);
-    }
+    valid[k] = valid_of<T>(threadIdx.x + k * THREADS, pieces, a.cols);
+    blank(px[k], valid[k]);
+    blank(pr[k], valid[k]);
+    blank(w[k], valid[k]);
 #pragma unroll
     for (uint32_t i = 0; i < N; ++i) {
-      h[k][i] = widen(px.v[i]) + widen(pr.v[i]);
+      h[k][i] = widen(px[k].v[i]) + widen(pr[k].v[i]);
       ss = add_square(h[k][i], a.shrink, ss);
     }
   }
@@ -71,24 +80,19 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
 #pragma unroll
   for (uint32_t k = 0; k < NV; ++k) {
     const uint32_t p = threadIdx.x + k * THREADS;
-    if (p < pieces) {
-      const uint32_t valid = a.cols - p * N;
-      Piece<T> w = load_piece<T>(a.weight, p);
-      blank(w, valid);
-      Piece<T> out;
-      if (a.h.data != nullptr) {
+    Piece<T> out;
+    if (a.h.data != nullptr) {
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) out.v[i] = static_cast<T>(h[k][i]);
-        store_piece(a.h.data + row * a.h.stride, p, out, valid);
-      }
-#pragma unroll
-      for (uint32_t i = 0; i < N; ++i) {
-        h[k][i] = h[k][i] * s * widen(w.v[i]);
-        if constexpr (E8) most = fmaxf(most, fabsf(h[k][i]));
-        else out.v[i] = static_cast<T>(h[k][i]);
-      }
-      if constexpr (!E8) store_piece(a.y.data + row * a.y.stride, p, out, valid);
+      for (uint32_t i = 0; i < N; ++i) out.v[i] = static_cast<T>(h[k][i]);
+      store_piece<ONCE>(a.h.data + row * a.h.stride, p, out, valid[k]);
     }
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) {
+      h[k][i] = h[k][i] * s * widen(w[k].v[i]);
+      if constexpr (E8) most = fmaxf(most, fabsf(h[k][i]));
+      else out.v[i] = static_cast<T>(h[k][i]);
+    }
+    if constexpr (!E8) store_piece<ONCE>(a.y.data + row * a.y.stride, p, out, valid[k]);
   }
   if constexpr (E8) {
     most = group_reduce<THREADS, true>(most, buffer[1]);
@@ -99,23 +103,22 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
 #pragma unroll
     for (uint32_t k = 0; k < NV; ++k) {
       const uint32_t p = threadIdx.x + k * THREADS;
-      if (p < pieces) {
-        const uint32_t valid = a.cols - p * N;
-        uint32_t q[N / 4];
+      uint32_t q[N / 4];
 #pragma unroll
-        for (uint32_t i = 0; i < N / 4; ++i) {
-          int v = __builtin_amdgcn_cvt_pk_fp8_f32(h[k][4 * i] * per, h[k][4 * i + 1] * per, 0, false);
-          q[i] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(h[k][4 * i + 2] * per, h[k][4 * i + 3] * per, v, true));
-        }
-        char* at = y + p * N;
-        if (valid >= N) {
-          if constexpr (N == 8) *reinterpret_cast<u32x2*>(at) = u32x2{q[0], q[1]};
-          else *reinterpret_cast<uint32_t*>(at) = q[0];
-        } else {
+      for (uint32_t i = 0; i < N / 4; ++i) {
+        int v = __builtin_amdgcn_cvt_pk_fp8_f32(h[k][4 * i] * per, h[k][4 * i + 1] * per, 0, false);
+        q[i] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(h[k][4 * i + 2] * per, h[k][4 * i + 3] * per, v, true));
+      }
+      char* at = y + p * N;
+      if (valid[k] >= N) {
+        if constexpr (N == 8 && ONCE) __builtin_nontemporal_store(u32x2{q[0], q[1]}, reinterpret_cast<u32x2*>(at));
+        else if constexpr (N == 8) *reinterpret_cast<u32x2*>(at) = u32x2{q[0], q[1]};
+        else if constexpr (ONCE) __builtin_nontemporal_store(q[0], reinterpret_cast<uint32_t*>(at));
+        else *reinterpret_cast<uint32_t*>(at) = q[0];
+      } else {
 #pragma unroll
-          for (uint32_t i = 0; i < N; ++i)
-            if (i < valid) at[i] = static_cast<char>(q[i / 4] >> (8 * (i % 4)));
-        }
+        for (uint32_t i = 0; i < N; ++i)
+          if (i < valid[k]) at[i] = static_cast<char>(q[i / 4] >> (8 * (i % 4)));
       }
     }
   }
@@ -174,7 +177,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     if (a.h.data != nullptr) {
 #pragma unroll
       for (uint32_t i = 0; i < N; ++i) out.v[i] = static_cast<T>(h[i]);
-      store_piece(a.h.data + row * a.h.stride, p, out, valid);
+      store_piece<false>(a.h.data + row * a.h.stride, p, out, valid);
     }
 #pragma unroll
     for (uint32_t i = 0; i < N; ++i) {
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
         out.v[i] = static_cast<T>(v);
       }
     }
-    if constexpr (!E8) store_piece(y, p, out, valid);
+    if constexpr (!E8) store_piece<false>(y, p, out, valid);
   }
 }
 
@@ -198,78 +201,89 @@ struct NormGradArgs {
 };
 
 // n = h s, g = dy w: dx = dh + s (g - n mean(g n)); the weight's gradient is the sum of dy n over the rows, of which a
-// workgroup takes every gridDim.x-th and leaves its sum for column_sum_kernel: no atomics, the order is always the same.
-template <class T, uint32_t THREADS, uint32_t NV>
+// workgroup takes every gridDim.x-th and leaves its sum for column_sum_kernel: no atomics, the order is always the same.  A row's
+// loads are issued before the row before it is reduced and written.
+template <class T, uint32_t THREADS, uint32_t NV, bool ONCE>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a) {
   constexpr uint32_t N = Piece<T>::N;
   __shared__ float buffer[2][THREADS / 64u];
   const uint32_t pieces = (a.cols + N - 1) / N;
-  float dw[NV][N];
-  Piece<T> w[NV];
+  uint32_t at[NV], valid[NV];
 #pragma unroll
   for (uint32_t k = 0; k < NV; ++k) {
-    const uint32_t p = threadIdx.x + k * THREADS;
-    w[k] = Piece<T>{};
-    if (p < pieces) w[k] = load_piece<T>(a.weight, p);
+    at[k] = min(threadIdx.x + k * THREADS, pieces - 1u);
+    valid[k] = valid_of<T>(threadIdx.x + k * THREADS, pieces, a.cols);
+  }
+  struct Row {
+    Piece<T> d[NV], h[NV], c[NV];
+    float s;
+  };
+  auto load = [&](uint64_t row) {
+    Row r;
+#pragma unroll
+    for (uint32_t k = 0; k < NV; ++k) {
+      r.d[k] = load_piece_once<T>(a.dy.data + row * a.dy.stride, at[k]);
+      r.h[k] = load_piece_once<T>(a.h.data + row * a.h.stride, at[k]);
+    }
+    if (a.dh.data != nullptr) {
+#pragma unroll
+      for (uint32_t k = 0; k < NV; ++k) r.c[k] = load_piece_once<T>(a.dh.data + row * a.dh.stride, at[k]);
+    } else {
+#pragma unroll
+      for (uint32_t k = 0; k < NV; ++k) r.c[k] = Piece<T>{};
+    }
+    r.s = a.rstd[row];
+    return r;
+  };
+  float dw[NV][N];
+  Piece<T> w[NV];
+  Row next = load(blockIdx.x);
+#pragma unroll
+  for (uint32_t k = 0; k < NV; ++k) {
+    w[k] = load_piece<T>(a.weight, at[k]);
+    blank(w[k], valid[k]);
 #pragma unroll
     for (uint32_t i = 0; i < N; ++i) dw[k][i] = 0.0f;
   }
   uint32_t turn = 0;
   for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1u) {
-    const char* dy = a.dy.data + row * a.dy.stride;
-    const char* h = a.h.data + row * a.h.stride;
-    const char* dh = a.dh.data == nullptr ? nullptr : a.dh.data + row * a.dh.stride;
-    Piece<T> pd[NV], ph[NV], pc[NV];
-#pragma unroll
-    for (uint32_t k = 0; k < NV; ++k) {
-      const uint32_t p = threadIdx.x + k * THREADS;
-      pd[k] = ph[k] = pc[k] = Piece<T>{};
-      if (p < pieces) {
-        pd[k] = load_piece<T>(dy, p);
-        ph[k] = load_piece<T>(h, p);
-        if (dh != nullptr) pc[k] = load_piece<T>(dh, p);
-        const uint32_t valid = a.cols - p * N;
-        blank(pd[k], valid);
-        blank(ph[k], valid);
-        blank(w[k], valid);
-      }
-    }
-    const float s = a.rstd[row];
+    Row r = next;
+    // dx may lie where dy or dh does, but a row is only written when it has been read, and by no other workgroup; the last row
+    // is loaded once more for nothing, before it is written
+    next = load(row + gridDim.x < a.rows ? row + gridDim.x : row);
     float along = 0.0f;
 #pragma unroll
-    for (uint32_t k = 0; k < NV; ++k)
+    for (uint32_t k = 0; k < NV; ++k) {
+      blank(r.d[k], valid[k]);
+      blank(r.h[k], valid[k]);
 #pragma unroll
       for (uint32_t i = 0; i < N; ++i) {
-        const float n = widen(ph[k].v[i]) * s, d = widen(pd[k].v[i]);
+        const float n = widen(r.h[k].v[i]) * r.s, d = widen(r.d[k].v[i]);
         dw[k][i] = __builtin_fmaf(d, n, dw[k][i]);
         along = __builtin_fmaf(d * widen(w[k].v[i]), n, along);
       }
+    }
     // two buffers in turn: a wavefront that is ahead writes the other one, and the barrier of that row keeps it from the next
     along = group_reduce<THREADS, false>(along, buffer[turn]) / static_cast<float>(a.cols);
 #pragma unroll
     for (uint32_t k = 0; k < NV; ++k) {
-      const uint32_t p = threadIdx.x + k * THREADS;
-      if (p < pieces) {
-        Piece<T> out;
+      Piece<T> out;
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) {
-          const float n = widen(ph[k].v[i]) * s, g = widen(pd[k].v[i]) * widen(w[k].v[i]);
-          out.v[i] = static_cast<T>(__builtin_fmaf(s, g - n * along, widen(pc[k].v[i])));
-        }
-        store_piece(a.dx.data + row * a.dx.stride, p, out, a.cols - p * N);
+      for (uint32_t i = 0; i < N; ++i) {
+        const float n = widen(r.h[k].v[i]) * r.s, g = widen(r.d[k].v[i]) * widen(w[k].v[i]);
+        out.v[i] = static_cast<T>(__builtin_fmaf(r.s, g - n * along, widen(r.c[k].v[i])));
       }
+      store_piece<ONCE>(a.dx.data + row * a.dx.stride, threadIdx.x + k * THREADS, out, valid[k]);
     }
   }
 #pragma unroll
-  for (uint32_t k = 0; k < NV; ++k) {
-    const uint32_t p = threadIdx.x + k * THREADS;
+  for (uint32_t k = 0; k < NV; ++k)
 #pragma unroll
     for (uint32_t i = 0; i < N; ++i)
-      if (p < pieces && p * N + i < a.cols) a.parts[static_cast<uint64_t>(blockIdx.x) * a.cols + p * N + i] = dw[k][i];
-  }
+      if (i < valid[k]) a.parts[static_cast<uint64_t>(blockIdx.x) * a.cols + (threadIdx.x + k * THREADS) * N + i] = dw[k][i];
 }
 
-// The same for rows of any length, a column block of 4096 / N pieces at a time: the row's sum first, then what needs it.
+// The same for rows of any length: the row's sum first, then what needs it.
 template <class T>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGradArgs a) {
   constexpr uint32_t N = Piece<T>::N, THREADS = 1024;
@@ -306,21 +320,31 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGradArgs a) {
         const float n = widen(ph.v[i]) * s, g = widen(pd.v[i]) * widen(w.v[i]);
         out.v[i] = static_cast<T>(__builtin_fmaf(s, g - n * along, widen(pc.v[i])));
       }
-      store_piece(a.dx.data + row * a.dx.stride, p, out, a.cols - p * N);
+      store_piece<false>(a.dx.data + row * a.dx.stride, p, out, a.cols - p * N);
     }
   }
 }
 
-// sums[c] = parts[0][c] + parts[1][c] + ...: 64 columns a workgroup, every wavefront a share of the parts.
-__global__ __launch_bounds__(256) void column_sum_kernel(float* sums, const float* parts, uint32_t n, uint32_t cols) {
-  __shared__ float buffer[4][64];
-  const uint32_t c = blockIdx.x * 64u + (threadIdx.x & 63u), wave = threadIdx.x / 64u;
+// sums[c] = parts[0][c] + parts[1][c] + ...: 64 columns a workgroup, every one of 16 wavefronts a share of the parts, 8 loads at a time.
+__global__ __launch_bounds__(1024) void column_sum_kernel(float* sums, const float* parts, uint32_t n, uint32_t cols) {
+  __shared__ float buffer[16][64];
+  const uint32_t lane = threadIdx.x & 63u, c = blockIdx.x * 64u + lane, wave = threadIdx.x / 64u;
   float v = 0.0f;
   if (c < cols)
-    for (uint32_t i = wave; i < n; i += 4u) v += parts[static_cast<uint64_t>(i) * cols + c];
-  buffer[wave][threadIdx.x & 63u] = v;
+    for (uint32_t i = wave; i < n; i += 16u * 8u) {
+      float p[8];
+#pragma unroll
+      for (uint32_t j = 0; j < 8u; ++j) p[j] = i + j * 16u < n ? parts[static_cast<uint64_t>(i + j * 16u) * cols + c] : 0.0f;
+#pragma unroll
+      for (uint32_t j = 0; j < 8u; ++j) v += p[j];
+    }
+  buffer[wave][lane] = v;
   __syncthreads();
-  if (wave == 0u && c < cols) sums[c] = (buffer[0][threadIdx.x] + buffer[1][threadIdx.x]) + (buffer[2][threadIdx.x] + buffer[3][threadIdx.x]);
+  if (wave == 0u && c < cols) {
+#pragma unroll
+    for (uint32_t i = 1; i < 16u; ++i) v += buffer[i][lane];
+    sums[c] = v;
+  }
 }
 
 struct CombineArgs {
@@ -332,48 +356,66 @@ struct CombineArgs {
 };
 
 // out = r + sum_j w_j y[pos_j].  A thread has one 16-byte piece of the token's row and loads it from up to 8 of the rows
-// before it adds the first: the work is the reading of those rows.
-template <class T>
-__global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
-  constexpr uint32_t N = Piece<T>::N, AT_ONCE = 8;
-  const uint64_t token = blockIdx.x / a.blocks;
-  const uint32_t p = (blockIdx.x % a.blocks) * 256u + threadIdx.x, pieces = (a.cols + N - 1) / N;
-  if (p >= pieces) return;
-  float sum[N];
-  if (a.r.data != nullptr) {
-    const Piece<T> pr = load_piece<T>(a.r.data + token * a.r.stride, p);
+// before it adds the first: the work is the reading of those rows.  A slot without a row reads row 0 and does not count, so that no load
+// waits for another; the host sees to it that there is a row 0, or no slot.
+constexpr uint32_t kSlotsAtOnce = 8;
+
+struct Slots {
+  uint32_t row[kSlotsAtOnce];
+  bool there[kSlotsAtOnce];
+  float weight[kSlotsAtOnce];   // 0 where there is no row
+};
+__device__ __forceinline__ Slots load_slots(const int32_t* pos, const float* weights, uint32_t first, uint32_t slots, uint32_t y_rows) {
+  Slots s;
 #pragma unroll
-    for (uint32_t i = 0; i < N; ++i) sum[i] = widen(pr.v[i]);
+  for (uint32_t j = 0; j < kSlotsAtOnce; ++j) s.row[j] = static_cast<uint32_t>(pos[min(first + j, slots - 1u)]);
+  if (weights != nullptr) {
+#pragma unroll
+    for (uint32_t j = 0; j < kSlotsAtOnce; ++j) s.weight[j] = weights[min(first + j, slots - 1u)];
   } else {
 #pragma unroll
-    for (uint32_t i = 0; i < N; ++i) sum[i] = 0.0f;
+    for (uint32_t j = 0; j < kSlotsAtOnce; ++j) s.weight[j] = 1.0f;
   }
-  const int32_t* pos = a.pos + token * a.slots;
-  for (uint32_t j0 = 0; j0 < a.slots; j0 += AT_ONCE) {
-    Piece<T> py[AT_ONCE];
-    float w[AT_ONCE];
-    bool there[AT_ONCE];
 #pragma unroll
-    for (uint32_t j = 0; j < AT_ONCE; ++j) {
-      const uint32_t at = j0 + j < a.slots ? static_cast<uint32_t>(pos[j0 + j]) : 0xFFFFFFFFu;
-      there[j] = at < a.y_rows;
-      w[j] = 1.0f;
-      if (there[j]) {
-        py[j] = load_piece<T>(a.y.data + at * a.y.stride, p);
-        if (a.weights != nullptr) w[j] = a.weights[token * a.slots + j0 + j];
-      }
+  for (uint32_t j = 0; j < kSlotsAtOnce; ++j) {
+    s.there[j] = first + j < slots && s.row[j] < y_rows;
+    s.row[j] = s.there[j] ? s.row[j] : 0u;
+    s.weight[j] = s.there[j] ? s.weight[j] : 0.0f;
+  }
+  return s;
+}
+
+template <class T, uint32_t THREADS, bool ONCE>
+__global__ __launch_bounds__(THREADS) void combine_kernel(CombineArgs a) {
+  constexpr uint32_t N = Piece<T>::N;
+  const uint64_t token = blockIdx.x / a.blocks;
+  const uint32_t p = (blockIdx.x % a.blocks) * THREADS + threadIdx.x, pieces = (a.cols + N - 1) / N;
+  if (p >= pieces) return;
+  Piece<T> pr{};
+  if (a.r.data != nullptr) pr = load_piece_once<T>(a.r.data + token * a.r.stride, p);
+  float sum[N];
+  for (uint32_t j0 = 0; j0 < a.slots; j0 += kSlotsAtOnce) {
+    const Slots s = load_slots(a.pos + token * a.slots, a.weights == nullptr ? nullptr : a.weights + token * a.slots, j0, a.slots, a.y_rows);
+    Piece<T> py[kSlotsAtOnce];
+#pragma unroll
+    for (uint32_t j = 0; j < kSlotsAtOnce; ++j) py[j] = load_piece_once<T>(a.y.data + s.row[j] * a.y.stride, p);
+    if (j0 == 0u) {
+#pragma unroll
+      for (uint32_t i = 0; i < N; ++i) sum[i] = widen(pr.v[i]);
     }
 #pragma unroll
-    for (uint32_t j = 0; j < AT_ONCE; ++j)
-      if (there[j]) {
+    for (uint32_t j = 0; j < kSlotsAtOnce; ++j)
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) sum[i] = __builtin_fmaf(w[j], widen(py[j].v[i]), sum[i]);
-      }
+      for (uint32_t i = 0; i < N; ++i) sum[i] = __builtin_fmaf(s.weight[j], s.there[j] ? widen(py[j].v[i]) : 0.0f, sum[i]);
+  }
+  if (a.slots == 0u) {
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) sum[i] = widen(pr.v[i]);
   }
   Piece<T> out;
 #pragma unroll
   for (uint32_t i = 0; i < N; ++i) out.v[i] = static_cast<T>(sum[i]);
-  store_piece(a.out.data + token * a.out.stride, p, out, a.cols - p * N);
+  store_piece<ONCE>(a.out.data + token * a.out.stride, p, out, a.cols - p * N);
 }
 
 struct CombineGradArgs {
@@ -385,52 +427,49 @@ struct CombineGradArgs {
 };
 
 // dy[pos_j] = w_j dout; dw_j = dout . y[pos_j].  One workgroup a token, 8 slots at a time, so that dout is read once for them.
-template <class T>
+template <class T, bool ONCE>
 __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
-  constexpr uint32_t N = Piece<T>::N, AT_ONCE = 8;
-  __shared__ float buffer[4][AT_ONCE];
+  constexpr uint32_t N = Piece<T>::N;
+  __shared__ float buffer[4][kSlotsAtOnce];
   const uint64_t token = blockIdx.x;
   const uint32_t pieces = (a.cols + N - 1) / N;
   const char* dout = a.dout.data + token * a.dout.stride;
-  for (uint32_t j0 = 0; j0 < a.slots; j0 += AT_ONCE) {
-    float dot[AT_ONCE], w[AT_ONCE];
-    uint32_t at[AT_ONCE];
+  for (uint32_t j0 = 0; j0 < a.slots; j0 += kSlotsAtOnce) {
+    const Slots s = load_slots(a.pos + token * a.slots, a.weights == nullptr ? nullptr : a.weights + token * a.slots, j0, a.slots, a.y_rows);
+    float dot[kSlotsAtOnce];
 #pragma unroll
-    for (uint32_t j = 0; j < AT_ONCE; ++j) {
-      at[j] = j0 + j < a.slots ? static_cast<uint32_t>(a.pos[token * a.slots + j0 + j]) : 0xFFFFFFFFu;
-      w[j] = at[j] < a.y_rows && a.weights != nullptr ? a.weights[token * a.slots + j0 + j] : 1.0f;
-      dot[j] = 0.0f;
-    }
+    for (uint32_t j = 0; j < kSlotsAtOnce; ++j) dot[j] = 0.0f;
     for (uint32_t p = threadIdx.x; p < pieces; p += 256u) {
       const uint32_t valid = a.cols - p * N;
-      Piece<T> pd = load_piece<T>(dout, p), py[AT_ONCE];
+      Piece<T> pd = load_piece<T>(dout, p), py[kSlotsAtOnce];
       if (a.dw != nullptr) {
 #pragma unroll
-        for (uint32_t j = 0; j < AT_ONCE; ++j)
-          if (at[j] < a.y_rows) py[j] = load_piece<T>(a.y.data + at[j] * a.y.stride, p);
+        for (uint32_t j = 0; j < kSlotsAtOnce; ++j) py[j] = load_piece_once<T>(a.y.data + s.row[j] * a.y.stride, p);
+#pragma unroll
+        for (uint32_t j = 0; j < kSlotsAtOnce; ++j) blank(py[j], s.there[j] ? valid : 0u);
+        blank(pd, valid);
+#pragma unroll
+        for (uint32_t j = 0; j < kSlotsAtOnce; ++j)
+#pragma unroll
+          for (uint32_t i = 0; i < N; ++i) dot[j] = __builtin_fmaf(widen(pd.v[i]), widen(py[j].v[i]), dot[j]);
       }
-      blank(pd, valid);
 #pragma unroll
-      for (uint32_t j = 0; j < AT_ONCE; ++j)
-        if (at[j] < a.y_rows) {
+      for (uint32_t j = 0; j < kSlotsAtOnce; ++j)
+        if (s.there[j]) {
           Piece<T> out;
-          if (a.dw != nullptr) blank(py[j], valid);
 #pragma unroll
-          for (uint32_t i = 0; i < N; ++i) {
-            if (a.dw != nullptr) dot[j] = __builtin_fmaf(widen(pd.v[i]), widen(py[j].v[i]), dot[j]);
-            out.v[i] = static_cast<T>(w[j] * widen(pd.v[i]));
-          }
-          store_piece(a.dy.data + at[j] * a.dy.stride, p, out, valid);
+          for (uint32_t i = 0; i < N; ++i) out.v[i] = static_cast<T>(s.weight[j] * widen(pd.v[i]));
+          store_piece<ONCE>(a.dy.data + s.row[j] * a.dy.stride, p, out, valid);
         }
     }
     if (a.dw != nullptr) {
 #pragma unroll
-      for (uint32_t j = 0; j < AT_ONCE; ++j) {
+      for (uint32_t j = 0; j < kSlotsAtOnce; ++j) {
         const float v = wave_sum(dot[j]);
         if ((threadIdx.x & 63u) == 0u) buffer[threadIdx.x / 64u][j] = v;
       }
       __syncthreads();
-      if (threadIdx.x < AT_ONCE && j0 + threadIdx.x < a.slots)
+      if (threadIdx.x < kSlotsAtOnce && j0 + threadIdx.x < a.slots)
         a.dw[token * a.slots + j0 + threadIdx.x] =
             (buffer[0][threadIdx.x] + buffer[1][threadIdx.x]) + (buffer[2][threadIdx.x] + buffer[3][threadIdx.x]);
       __syncthreads();

@@ -59,25 +59,37 @@ int with_type(uint32_t dtype, F f) {
   return dtype == UCCL_F32 ? f(float{}) : dtype == UCCL_BF16 ? f(__bf16{}) : f(_Float16{});
 }
 
-template <class T, bool E8>
+// Outputs of more than this do not stay in the L2s (8 of 4 MiB) until they are read, and are stored past them: norm of 4096 x 7168 in
+// bf16 to e4m3 48 -> 39 us (loads past them too), combination of 8 x 4096 rows 104 -> 86.
+bool too_large_to_keep(const uccl_rows* m) { return static_cast<uint64_t>(m->rows) * m->cols * element_bytes(m->dtype) > (32ull << 20); }
+
+// A workgroup a row, with its row in registers.  Many rows: two pieces a thread (4096 x 7168, bf16 to e4m3: 36.5 us with 512 threads,
+// 39 with 256 and four pieces, 43 with 1024 and one); few rows, where latency counts: one piece (one row of 7168: 3.4 us, 4.9 with 256 threads).
+template <class T, bool E8, bool ONCE>
 int norm(const NormArgs& a, hipStream_t s) {
   const uint32_t pieces = blocks_for(a.cols, Piece<T>::N);
   const dim3 grid(a.rows);
-  if (pieces <= 64u) return enqueue(norm_kernel<T, E8, 64, 1>, grid, 64, s, a);
-  if (pieces <= 256u) return enqueue(norm_kernel<T, E8, 256, 1>, grid, 256, s, a);
-  if (pieces <= 512u) return enqueue(norm_kernel<T, E8, 256, 2>, grid, 256, s, a);
-  if (pieces <= 1024u) return enqueue(norm_kernel<T, E8, 256, 4>, grid, 256, s, a);
+  if (pieces <= 64u) return enqueue(norm_kernel<T, E8, 64, 1, ONCE>, grid, 64, s, a);
+  if (pieces <= 256u) return enqueue(norm_kernel<T, E8, 256, 1, ONCE>, grid, 256, s, a);
+  if (pieces <= 512u) return enqueue(norm_kernel<T, E8, 512, 1, ONCE>, grid, 512, s, a);
+  if (pieces <= 1024u && a.rows > 512u) return enqueue(norm_kernel<T, E8, 512, 2, ONCE>, grid, 512, s, a);
+  if (pieces <= 1024u) return enqueue(norm_kernel<T, E8, 1024, 1, ONCE>, grid, 1024, s, a);
+  if (pieces <= 2048u) return enqueue(norm_kernel<T, E8, 512, 4, ONCE>, grid, 512, s, a);
   return enqueue(norm_long_kernel<T, E8>, grid, 1024, s, a);
 }
 
-constexpr uint32_t kGradGroups = 512;   // workgroups that share the rows of a norm's gradient
+// Workgroups that share the rows of a norm's gradient, at most: one a compute unit.  (512 of them come in two rounds: 4096 x 7168 in bf16
+// 44 against 52 us, and half the sums to add up.)
+constexpr uint32_t kGradGroups = 256;
 
-template <class T>
+template <class T, bool ONCE>
 int norm_grad(const NormGradArgs& a, uint32_t groups, hipStream_t s) {
   const uint32_t pieces = blocks_for(a.cols, Piece<T>::N);
-  if (pieces <= 256u) return enqueue(norm_grad_kernel<T, 256, 1>, dim3(groups), 256, s, a);
-  if (pieces <= 512u) return enqueue(norm_grad_kernel<T, 256, 2>, dim3(groups), 256, s, a);
-  if (pieces <= 1024u) return enqueue(norm_grad_kernel<T, 1024, 1>, dim3(groups), 1024, s, a);
+  if (pieces <= 256u) return enqueue(norm_grad_kernel<T, 256, 1, ONCE>, dim3(groups), 256, s, a);
+  if (pieces <= 512u) return enqueue(norm_grad_kernel<T, 512, 1, ONCE>, dim3(groups), 512, s, a);
+  if (pieces <= 1024u) return enqueue(norm_grad_kernel<T, 1024, 1, ONCE>, dim3(groups), 1024, s, a);
+  if constexpr (sizeof(T) == 4)
+    if (pieces <= 2048u) return enqueue(norm_grad_kernel<T, 512, 4, ONCE>, dim3(groups), 512, s, a);
   return enqueue(norm_grad_long_kernel<T>, dim3(groups), 1024, s, a);
 }
 
@@ -184,10 +196,12 @@ int uccl_norm_rows(const uccl_rows* y, const uccl_rows* h, float* rstd, const uc
   const float shrink = ldexpf(1.0f, -ilogbf(static_cast<float>(x->cols)) / 2);
   const NormArgs a{rows_of(y), rows_of(h), rows_of(x), rows_of(r), static_cast<const char*>(weight), rstd, x->rows, x->cols, opts->eps, shrink,
                    1.0f / (static_cast<float>(x->cols) * shrink * shrink)};
+  const bool once = too_large_to_keep(y) || (h != nullptr && too_large_to_keep(h));
   const hipStream_t s = static_cast<hipStream_t>(stream);
   return with_type(x->dtype, [&](auto t) {
     using T = decltype(t);
-    return y->dtype == UCCL_E4M3 ? norm<T, true>(a, s) : norm<T, false>(a, s);
+    if (y->dtype == UCCL_E4M3) return once ? norm<T, true, true>(a, s) : norm<T, true, false>(a, s);
+    return once ? norm<T, false, true>(a, s) : norm<T, false, false>(a, s);
   });
 }
 
@@ -213,10 +227,13 @@ int uccl_norm_rows_grad(const uccl_rows* dx, float* dweight, const uccl_rows* dy
     if (rstd == nullptr || weight == nullptr || scratch == nullptr || scratch_bytes < uccl_norm_rows_scratch(h->rows, h->cols)) return UCCL_EINVAL;
     if (misaligned(weight, 16) || misaligned(rstd, 4) || misaligned(scratch, 16)) return UCCL_EALIGN;
     const NormGradArgs a{rows_of(dx), rows_of(dy), rows_of(h), rows_of(dh), static_cast<const char*>(weight), rstd, static_cast<float*>(scratch), h->rows, h->cols};
-    e = with_type(h->dtype, [&](auto t) { return norm_grad<decltype(t)>(a, groups, s); });
+    e = with_type(h->dtype, [&](auto t) {
+      using T = decltype(t);
+      return too_large_to_keep(dx) ? norm_grad<T, true>(a, groups, s) : norm_grad<T, false>(a, groups, s);
+    });
     if (e != UCCL_OK) return e;
   }
-  return enqueue(column_sum_kernel, dim3(blocks_for(h->cols, 64u)), 256, s, dweight, static_cast<const float*>(scratch), groups, h->cols);
+  return enqueue(column_sum_kernel, dim3(blocks_for(h->cols, 64u)), 1024, s, dweight, static_cast<const float*>(scratch), groups, h->cols);
 }
 
 // What the three products have in common.  `x` of kForward and kGradW is read through the index.
@@ -287,11 +304,13 @@ int uccl_combine_rows(const uccl_rows* out, const uccl_rows* y, const int32_t* p
   if (out->rows == 0u || out->cols == 0u) return UCCL_OK;
   return with_type(out->dtype, [&](auto t) {
     using T = decltype(t);
-    const uint32_t blocks = blocks_for(blocks_for(out->cols, Piece<T>::N), 256u);
+    const uint32_t blocks = blocks_for(blocks_for(out->cols, Piece<T>::N), 128u);
     const uint64_t grid = static_cast<uint64_t>(out->rows) * blocks;
-    if (grid > 0xFFFFFFFFull / 256u) return static_cast<int>(UCCL_ETOOBIG);
-    const CombineArgs a{rows_of(out), rows_of(y), rows_of(r), pos, weights, out->rows, slots, y->rows, out->cols, blocks};
-    return enqueue(combine_kernel<T>, dim3(static_cast<uint32_t>(grid)), 256, static_cast<hipStream_t>(stream), a);
+    if (grid > 0xFFFFFFFFull / 128u) return static_cast<int>(UCCL_ETOOBIG);
+    const CombineArgs a{rows_of(out), rows_of(y), rows_of(r), pos, weights, out->rows, y->rows == 0u ? 0u : slots, y->rows, out->cols, blocks};
+    const dim3 g(static_cast<uint32_t>(grid));
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    return too_large_to_keep(out) ? enqueue(combine_kernel<T, 128, true>, g, 128, s, a) : enqueue(combine_kernel<T, 128, false>, g, 128, s, a);
   });
 }
 
@@ -305,8 +324,11 @@ int uccl_combine_rows_grad(const uccl_rows* dy, float* dweights, const uccl_rows
   if (misaligned(dweights, 4)) return UCCL_EALIGN;
   if (dout->rows == 0u || slots == 0u) return UCCL_OK;
   return with_type(y->dtype, [&](auto t) {
-    const CombineGradArgs a{rows_of(dy), rows_of(dout), rows_of(y), pos, weights, dweights, dout->rows, slots, y->rows, dout->cols};
-    return enqueue(combine_grad_kernel<decltype(t)>, dim3(dout->rows), 256, static_cast<hipStream_t>(stream), a);
+    using T = decltype(t);
+    // (without a row there is nothing to write but the weights' gradient: an empty sum for every slot)
+    const CombineGradArgs a{rows_of(dy), rows_of(dout), rows_of(y), pos, weights, dweights, dout->rows, slots, y->rows, y->rows == 0u ? 0u : dout->cols};
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    return too_large_to_keep(dy) ? enqueue(combine_grad_kernel<T, true>, dim3(dout->rows), 256, s, a) : enqueue(combine_grad_kernel<T, false>, dim3(dout->rows), 256, s, a);
   });
 }
 

@@ -43,7 +43,7 @@ def _type(dtype):
         import torch
         from . import UCCL_BF16, UCCL_F16, UCCL_F32
         _types.update({torch.float32: (UCCL_F32, 4), torch.bfloat16: (UCCL_BF16, 2), torch.float16: (UCCL_F16, 2),
-                       torch.float8_e4m3fn: (UCCL_E4M3, 1)})
+                       torch.float8_e4m3fn: (UCCL_E4M3, 1), "scale": torch.float32})
     if dtype not in _types:
         raise ValueError(f"rows of {dtype} are not supported")
     return _types[dtype]
@@ -69,16 +69,15 @@ def _rows(t, scales=None):
         raise ValueError("the last dimension of a tensor of rows has to be contiguous")
     at, between = None, 0
     if scales is not None:
-        if scales.element_size() != 4 or not scales.is_floating_point() or scales.numel() != rows:
+        if scales.dtype is not _types["scale"] or scales.numel() != rows:
             raise ValueError("scales are float32, one for every row")
-        if scales.dim() > 1 and scales.shape[-1] == 1:
-            scales = scales[..., 0]
-        apart = 0
-        if scales.dim():
-            apart = scales.stride(0) if scales.dim() == 2 and scales.shape[1] == 1 else scales.stride(-1)
-            if scales.dim() == 2 and scales.shape[0] > 1 and scales.stride(0) != scales.shape[1] * apart:
-                raise ValueError("scales have to be the same distance apart throughout")
-        at, between = scales.data_ptr(), 4 * apart
+        lengths, apart = scales.shape, scales.stride()
+        if len(lengths) > 1 and lengths[-1] == 1:   # a last dimension of one scale
+            lengths, apart = lengths[:-1], apart[:-1]
+        if len(lengths) == 2 and lengths[0] > 1 and lengths[1] > 1 and apart[0] != lengths[1] * apart[1] or len(lengths) > 2:
+            raise ValueError("scales have to be the same distance apart throughout")
+        between = 0 if not lengths else 4 * (apart[0] if lengths[-1] == 1 else apart[-1])
+        at = scales.data_ptr()
     return C.byref(uccl_rows(t.data_ptr(), step * size, at, between, rows, cols, number, 0))
 
 
