@@ -153,34 +153,65 @@ __device__ __forceinline__ uint32_t narrow_pair(float a, float b) {
   return __builtin_bit_cast(uint32_t, pair{static_cast<T>(a), static_cast<T>(b)});
 }
 
-// A block of the output as a matrix instruction leaves it: SIDE (16 or 32) rows, a lane has the row lane % SIDE (`there`: it is
-// stored) and of it, 4 at a time, neighbouring columns from `first` on.  16-bit rows: lanes hand each other what makes 8 columns
-// of one, so that 16 bytes are stored.
-__device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row, bool there, uint32_t first, uint32_t cols, f32x4 x, f32x4 y) {
-  // two blocks of 16 x 16 side by side: columns lane / 16 * 4 .. + 3 of each
-  char* at = a.out.data + row * a.out.stride;
-  const uint32_t quarter = threadIdx.x % 64u / 16u;
-  if (a.out_type == kOutF32) {
-    const uint32_t c = first + quarter * 4u;
-    if (there && c < cols) store_piece<false>(at, c / 4u, Piece<float>{x[0], x[1], x[2], x[3]}, cols - c);
-    if (there && c + 16u < cols) store_piece<false>(at, c / 4u + 4u, Piece<float>{y[0], y[1], y[2], y[3]}, cols - c - 16u);
-    return;
-  }
+// Blocks of 16 x 16 of the output as the matrix instruction leaves them: a lane has of row lane % 16 four neighbouring columns,
+// lane / 16 * 4 on.  They are stored 16 bytes a lane, with as much of a 128-byte line at a time as there is.
+//
+// Eight neighbouring columns in 16 bits from two blocks side by side: odd quarters of x against even quarters of y.  The lane's are then
+// quarter % 2 * 16 + quarter / 2 * 8 on.
+__device__ __forceinline__ u32x4 narrow_blocks(uint32_t out_type, f32x4 x, f32x4 y) {
   uint32_t wx[2], wy[2];
 #pragma unroll
   for (uint32_t i = 0; i < 2u; ++i) {
-    wx[i] = a.out_type == kOutBf16 ? narrow_pair<__bf16>(x[2 * i], x[2 * i + 1]) : narrow_pair<_Float16>(x[2 * i], x[2 * i + 1]);
-    wy[i] = a.out_type == kOutBf16 ? narrow_pair<__bf16>(y[2 * i], y[2 * i + 1]) : narrow_pair<_Float16>(y[2 * i], y[2 * i + 1]);
+    wx[i] = out_type == kOutBf16 ? narrow_pair<__bf16>(x[2 * i], x[2 * i + 1]) : narrow_pair<_Float16>(x[2 * i], x[2 * i + 1]);
+    wy[i] = out_type == kOutBf16 ? narrow_pair<__bf16>(y[2 * i], y[2 * i + 1]) : narrow_pair<_Float16>(y[2 * i], y[2 * i + 1]);
   }
-  // odd quarters of x against even quarters of y
   const u32x2 s0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(wx[0], wy[0], false, false));
   const u32x2 s1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(wx[1], wy[1], false, false));
+  return u32x4{s0.x, s1.x, s0.y, s1.y};
+}
+
+// Two pieces a lane that are APART columns from each other make lines of 128 bytes of 8 rows at a time: lanes 8 apart exchange the first
+// row's second piece for the second row's first one.  The lane's pieces start at column `c` of rows `row` + lane % 16 of 16, of which
+// those below `rows` are stored.
+template <class T, uint32_t APART, bool ONCE>
+__device__ __forceinline__ void store_lines(const ProductArgs& a, uint64_t row, uint32_t rows, uint32_t c, uint32_t cols, u32x4 p, u32x4 q) {
+  const bool upper = (threadIdx.x & 8u) != 0u;
+  u32x4 x, y;
+#pragma unroll
+  for (uint32_t i = 0; i < 4u; ++i) {
+    const uint32_t other = static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(upper ? p[i] : q[i]), 0x128, 0xF, 0xF, true));   // a row of lanes by 8
+    x[i] = upper ? other : p[i];
+    y[i] = upper ? q[i] : other;
+  }
+  if (upper) c += APART;
+  const uint32_t r = threadIdx.x & 7u;
+  char* at = a.out.data + (row + r) * a.out.stride;
+  if (r < rows && c < cols) store_piece<ONCE>(at, c / Piece<T>::N, __builtin_bit_cast(Piece<T>, x), cols - c);
+  if (r + 8u < rows && c < cols) store_piece<ONCE>(at + 8u * a.out.stride, c / Piece<T>::N, __builtin_bit_cast(Piece<T>, y), cols - c);
+}
+
+// Four blocks side by side (two, if there are no more) from column `first` on.
+template <bool ONCE, uint32_t BLOCKS>
+__device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row, uint32_t rows, uint32_t first, uint32_t cols, const f32x4 (&v)[BLOCKS]) {
+  static_assert(BLOCKS == 2u || BLOCKS == 4u);
+  const uint32_t quarter = threadIdx.x % 64u / 16u;
+  if (a.out_type == kOutF32) {
+#pragma unroll
+    for (uint32_t n = 0; n < BLOCKS; n += 2u)
+      store_lines<float, 16, ONCE>(a, row, rows, first + n * 16u + quarter * 4u, cols, __builtin_bit_cast(u32x4, v[n]), __builtin_bit_cast(u32x4, v[n + 1u]));
+    return;
+  }
   const uint32_t c = first + quarter % 2u * 16u + quarter / 2u * 8u;
-  const Piece<uint16_t> p = __builtin_bit_cast(Piece<uint16_t>, u32x4{s0.x, s1.x, s0.y, s1.y});
-  if (there && c < cols) store_piece<false>(at, c / 8u, p, cols - c);
+  const u32x4 p = narrow_blocks(a.out_type, v[0], v[1]);
+  if constexpr (BLOCKS == 4u) {
+    store_lines<uint16_t, 32, ONCE>(a, row, rows, c, cols, p, narrow_blocks(a.out_type, v[2], v[3]));
+  } else {
+    const uint32_t r = threadIdx.x & 15u;
+    if (r < rows && c < cols) store_piece<false>(a.out.data + (row + r) * a.out.stride, c / 8u, __builtin_bit_cast(Piece<uint16_t>, p), cols - c);
+  }
 }
 __device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row, bool there, uint32_t first, uint32_t cols, f32x16 v) {
-  // one block of 32 x 32: columns i / 4 * 8 + lane / 32 * 4 + i % 4
+  // one block of 32 x 32: a lane has of row lane % 32 (`there`: it is stored) columns i / 4 * 8 + lane / 32 * 4 + i % 4
   char* at = a.out.data + row * a.out.stride;
   const uint32_t half = threadIdx.x % 64u / 32u;
   if (a.out_type == kOutF32) {
@@ -420,6 +451,8 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
 
   const uint32_t wave = threadIdx.x / 64u, lane = threadIdx.x & 63u;
   const uint32_t ra = wave / WC * (BM / WR), cb = wave % WC * (BN / WC);
+  // Blocks of rows that the wavefront has in this tile, at most NA: the others are not multiplied
+  const uint32_t high = __builtin_amdgcn_readfirstlane(r0 + ra < out_rows ? min((out_rows - r0 - ra + SIDE - 1u) / SIDE, NA) : 0u);
   Block acc[NB][NA] = {};
   using Fragment = decltype(fragment_of<M, A>(lds_a, 0, 0));
   Fragment fa[NA], fb[2][NB];
@@ -433,7 +466,8 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
     for (uint32_t n = 0; n < NB; ++n) fb[HALF ^ 1u][n] = fragment_of<M, B>(next_b, cb + n * SIDE, HALF ^ 1u);
 #pragma unroll
     for (uint32_t m = 0; m < NA; ++m) {
-      if constexpr (M == kWidened) {
+      if (m >= high) {
+      } else if constexpr (M == kWidened) {
         const Widened x = widen_e4m3(fa[m]);
 #pragma unroll
         for (uint32_t n = 0; n < NB; ++n) {
@@ -528,16 +562,21 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
         store_blocks(a, row, there, first, out_cols, v);
       }
     } else {
+      constexpr uint32_t BLOCKS = NB % 4u == 0u ? 4u : 2u;
+      const uint32_t top = r0 + ra + m * 16u;   // of the 16 rows that the wavefront has
+      const uint32_t rows = top < out_rows ? out_rows - top : 0u;
 #pragma unroll
-      for (uint32_t n = 0; n < NB; n += 2u) {
+      for (uint32_t n = 0; n < NB; n += BLOCKS) {
         const uint32_t first = c0 + cb + n * 16u;
-        f32x4 x = acc[n][m], y = acc[n + 1u][m];
+        f32x4 v[BLOCKS];
 #pragma unroll
-        for (uint32_t i = 0; i < 4u; ++i) {
-          x[i] = scaled(x[i], first + lane / 16u * 4u + i);
-          y[i] = scaled(y[i], first + 16u + lane / 16u * 4u + i);
+        for (uint32_t b = 0; b < BLOCKS; ++b) {
+          v[b] = acc[n + b][m];
+#pragma unroll
+          for (uint32_t i = 0; i < 4u; ++i) v[b][i] = scaled(v[b][i], first + b * 16u + lane / 16u * 4u + i);
         }
-        store_blocks(a, row, there, first, out_cols, x, y);
+        // a launch of tiles of 256 x 256 writes more than the L2s keep
+        store_blocks<BM == 256u>(a, P == kGradW ? w0 + top : top, rows, first, out_cols, v);
       }
     }
   }
