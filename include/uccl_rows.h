@@ -38,7 +38,7 @@ typedef struct uccl_rows {
   uint64_t stride;
   void* scales;          /* UCCL_E4M3 only, NULL otherwise */
   uint64_t scale_stride; /* bytes */
-  uint32_t rows, cols;   /* at most 2^31 - 1 each */
+  uint32_t rows, cols;   /* at most 2^31 - 1 rows of at most 2^30 columns */
   uint32_t dtype;        /* UCCL_F32, UCCL_BF16, UCCL_F16 or UCCL_E4M3 */
   uint32_t reserved;     /* 0 */
 } uccl_rows;
@@ -57,7 +57,8 @@ typedef struct uccl_rows {
  * its type and stride.  A NaN or an infinity in a row makes the row's y what the formula makes it; elements that are not finite do
  * not enter the scale unless they are infinities.
  * UCCL_OK, also for no rows or no columns (nothing is enqueued); UCCL_EINVAL: a null pointer, shapes or types that do not
- * match; UCCL_EALIGN; UCCL_ELAUNCH.
+ * match; UCCL_EALIGN; UCCL_ELAUNCH.  On an error nothing has been enqueued (but for uccl_norm_rows_grad, two launches, of which HIP
+ * may take the first and refuse the second).
  */
 typedef struct uccl_norm_opts { /* HOST struct, read during the call */
   float eps;
@@ -92,7 +93,13 @@ uint64_t uccl_norm_rows_scratch(uint32_t rows, uint32_t cols);
  *   w        read: n_groups * n rows of k columns, x's type; the n rows of a group follow each other
  *   offsets  read: n_groups + 1 int32, 4-byte aligned, in ascending order; one that is below its predecessor counts as
  *            that, below 0 as 0, above the rows of y as these
- * Sums are held in binary32 and rounded once; 8-bit operands are multiplied as they are and the sum by both scales.
+ * Sums are held in binary32 and rounded once; 8-bit operands are multiplied as they are and the sum by both scales.  Their
+ * products are exact but where y is 16 bits wide, k at least 512 and the call large enough for the matrix instruction for 8 bits:
+ * that adds 64 products at a time and drops of each what is below about 2^-13 of the greatest of them, which is far below what
+ * rounding y to 16 bits drops.
+ * What a call is cut into depends on its sizes alone, never on the offsets' values.  UCCL_OK, also where there is nothing to
+ * compute; UCCL_EINVAL: a null pointer, shapes or types that do not match; UCCL_EALIGN; UCCL_ETOOBIG: more than 2^24 tiles (of
+ * 128 x 128 elements of the output, or 16 rows x 32 columns for groups of few rows: split the call); UCCL_ELAUNCH.
  */
 int uccl_group_product(const uccl_rows* y, const uccl_rows* x, const int32_t* index, const uccl_rows* w,
                        const int32_t* offsets, uint32_t n_groups, void* stream);

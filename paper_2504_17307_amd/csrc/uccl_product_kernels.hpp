@@ -40,8 +40,10 @@ struct Group {
 // Offsets are taken as they can be used, whatever they hold: each is at least the one before it, at least 0 and at most
 // `rows`.  Groups never overlap then and no row outside the matrix is touched.
 //
-// 64 groups' ranges, a lane each, and how many tiles of `height` rows these are (every group is cut into tiles of its own)
-// up to and with the lane's.  `before`: the greatest offset of earlier groups.
+// 64 groups' ranges, a lane each, and how many tiles of `height` rows these are (every group is cut into tiles of its own), full ones
+// and those that a group ends in: the lane's, and up to and with the lane's, both numbers in one word.  `before`: the greatest offset
+// of earlier groups.
+constexpr uint32_t kFullBits = 25;   // a launch has at most 2^24 tiles, and 64 groups end in at most 64
 struct Ranges {
   uint32_t begin, end, tiles, sum;
   int32_t most;
@@ -60,7 +62,8 @@ __device__ __forceinline__ Ranges group_ranges(const ProductArgs& a, uint32_t at
   const int32_t previous = __shfl_up(r.most, 1);
   r.begin = static_cast<uint32_t>(min(max(lane == 0u ? max(begin, before) : previous, 0), limit));
   r.end = static_cast<uint32_t>(min(max(r.most, 0), limit));
-  r.tiles = mine < a.groups ? (r.end - r.begin + height - 1u) / height : 0u;
+  const uint32_t n = mine < a.groups ? r.end - r.begin : 0u;
+  r.tiles = n / height | (n % height != 0u ? 1u << kFullBits : 0u);
   r.sum = r.tiles;
 #pragma unroll
   for (uint32_t d = 1; d < 64u; d <<= 1) {
@@ -70,11 +73,12 @@ __device__ __forceinline__ Ranges group_ranges(const ProductArgs& a, uint32_t at
   return r;
 }
 
-// Workgroups of a launch go round the eight XCDs in turn.  Each XCD gets a contiguous eighth of the n tiles, so that tiles
-// with the same rows or the same weights, which are neighbours, share an L2.  False: there is no tile for this workgroup.
-__device__ __forceinline__ bool tile_of_xcd(uint32_t block, uint32_t n, uint32_t& tile) {
-  const uint32_t each = (n + 7u) / 8u, place = block / 8u;
-  tile = block % 8u * each + place;
+// Workgroups of a launch go round the eight XCDs in turn, and start in order.  Each XCD gets a contiguous eighth of the n tiles, so
+// that tiles with the same rows or the same weights, which are neighbours, share an L2.  `place`: the workgroup's turn on its XCD;
+// false: there is no tile for it.
+__device__ __forceinline__ bool tile_of_xcd(uint32_t place, uint32_t n, uint32_t& tile) {
+  const uint32_t each = (n + 7u) / 8u;
+  tile = blockIdx.x % 8u * each + place;
   return place < each && tile < n;
 }
 
@@ -88,33 +92,41 @@ __device__ __forceinline__ void place_in_band(uint32_t& tile, uint32_t down, uin
 }
 
 // The workgroup's tile of the products by rows: its group, its first row and its place across.  All lanes of a wavefront call
-// it.  The launch has a workgroup for every tile that there could be; which there are is known here only.
+// it.  The launch has a workgroup for every tile that there could be; which there are is known here only.  Full tiles come
+// first, and tiles that groups end in, which take less, fill up what they leave.
 __device__ __forceinline__ bool find_tile(const ProductArgs& a, uint32_t height, uint32_t across, Group& g, uint32_t& first_row, uint32_t& place) {
+  constexpr uint32_t kFull = (1u << kFullBits) - 1u;
   Ranges r = group_ranges(a, 0, 0, height);
-  uint32_t total = __builtin_amdgcn_readlane(r.sum, 63);
+  uint32_t sum = __builtin_amdgcn_readlane(r.sum, 63), full = sum & kFull, ends = sum >> kFullBits;
   if (a.groups > 64u) {
     int32_t before = __builtin_amdgcn_readlane(r.most, 63);
     for (uint32_t at = 64; at < a.groups; at += 64u) {
       const Ranges next = group_ranges(a, at, before, height);
       before = __builtin_amdgcn_readlane(next.most, 63);
-      total += __builtin_amdgcn_readlane(next.sum, 63);
+      sum = __builtin_amdgcn_readlane(next.sum, 63);
+      full += sum & kFull;
+      ends += sum >> kFullBits;
     }
   }
+  const uint32_t turn = blockIdx.x / 8u, each = (full * across + 7u) / 8u;
+  const bool whole = turn < each;
   uint32_t tile;
-  if (!tile_of_xcd(blockIdx.x, total * across, tile)) return false;
-  place_in_band(tile, total, across, place);
+  if (!tile_of_xcd(whole ? turn : turn - each, (whole ? full : ends) * across, tile)) return false;
+  place_in_band(tile, whole ? full : ends, across, place);
   uint32_t passed = 0;
   for (uint32_t at = 0;; at += 64u) {
-    const uint64_t holds = __ballot(passed + r.sum > tile);
+    const uint32_t count = whole ? r.sum & kFull : r.sum >> kFullBits, own = whole ? r.tiles & kFull : r.tiles >> kFullBits;
+    const uint64_t holds = __ballot(passed + count > tile);
     if (holds != 0u) {
       const int l = __ffsll(static_cast<unsigned long long>(holds)) - 1;
       g.index = at + static_cast<uint32_t>(l);
       g.begin = __builtin_amdgcn_readlane(r.begin, l);
       g.end = __builtin_amdgcn_readlane(r.end, l);
-      first_row = g.begin + (tile - passed - (__builtin_amdgcn_readlane(r.sum, l) - __builtin_amdgcn_readlane(r.tiles, l))) * height;
+      const uint32_t nth = whole ? tile - passed - (__builtin_amdgcn_readlane(count, l) - __builtin_amdgcn_readlane(own, l)) : (g.end - g.begin) / height;
+      first_row = g.begin + nth * height;
       return true;
     }
-    passed += __builtin_amdgcn_readlane(r.sum, 63);
+    passed += __builtin_amdgcn_readlane(count, 63);
     r = group_ranges(a, at + 64u, __builtin_amdgcn_readlane(r.most, 63), height);
   }
 }
@@ -137,7 +149,7 @@ __device__ __forceinline__ bool find_output(const ProductArgs& a, uint32_t heigh
   if constexpr (P != kGradW) return find_tile(a, height, across, g, first_row, place);
   const uint32_t down = (a.wide + height - 1u) / height;
   uint32_t tile;
-  if (!tile_of_xcd(blockIdx.x, a.groups * down * across, tile)) return false;
+  if (!tile_of_xcd(blockIdx.x / 8u, a.groups * down * across, tile)) return false;
   place_in_band(tile, a.groups * down, across, place);
   g = group_rows(a, tile / down);
   first_row = tile % down * height;

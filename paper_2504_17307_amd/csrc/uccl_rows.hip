@@ -13,7 +13,7 @@
 
 namespace {
 
-constexpr uint32_t kMost = 0x7FFFFFFFu;   // rows, columns, slots, groups
+constexpr uint32_t kMost = 0x7FFFFFFFu, kMostCols = 1u << 30;   // rows, slots, groups; columns
 
 bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
@@ -31,7 +31,7 @@ bool same_shape(const uccl_rows* a, const uccl_rows* b) { return a->rows == b->r
 
 // What holds for every matrix by itself.
 int check(const uccl_rows* m) {
-  if (m == nullptr || m->reserved != 0u || element_bytes(m->dtype) == 0u || m->rows > kMost || m->cols > kMost) return UCCL_EINVAL;
+  if (m == nullptr || m->reserved != 0u || element_bytes(m->dtype) == 0u || m->rows > kMost || m->cols > kMostCols) return UCCL_EINVAL;
   if ((m->dtype == UCCL_E4M3) != (m->scales != nullptr) && m->rows != 0u) return UCCL_EINVAL;
   if (m->rows == 0u || m->cols == 0u) return UCCL_OK;
   if (m->data == nullptr) return UCCL_EINVAL;
@@ -95,25 +95,24 @@ int norm_grad(const NormGradArgs& a, uint32_t groups, hipStream_t s) {
 
 OutType out_type(const uccl_rows* m) { return m->dtype == UCCL_F32 ? kOutF32 : m->dtype == UCCL_BF16 ? kOutBf16 : kOutF16; }
 
-// Tiles that the rows of `groups` groups can make at most: every group has one that is not full, whatever the offsets.
-uint64_t most_tiles(uint32_t rows, uint32_t groups, uint32_t height) { return rows / height + static_cast<uint64_t>(groups < rows ? groups : rows); }
-
-// A launch over tiles of BM x BN: a workgroup for each that there could be, by eights.
+// A launch over tiles of BM x BN: a workgroup for each that there could be whatever the offsets are, by eights.
 template <Product P, class K>
 int product_tiles(K kernel, uint32_t bm, uint32_t bn, uint32_t threads, const ProductArgs& a, hipStream_t s) {
-  const uint32_t out_cols = P == kForward ? a.wide : a.cols, across = blocks_for(out_cols, bn);
-  const uint64_t down = P == kGradW ? static_cast<uint64_t>(a.groups) * blocks_for(a.wide, bm) : most_tiles(a.rows, a.groups, bm);
-  const uint64_t tiles = (down * across + 7u) / 8u * 8u;
-  if (tiles > 0xFFFFFFFFull / threads) return UCCL_ETOOBIG;
+  const uint64_t across = blocks_for(P == kForward ? a.wide : a.cols, bn);
+  auto by_eights = [](uint64_t n) { return (n + 7u) / 8u * 8u; };
+  const uint64_t tiles = P == kGradW ? by_eights(static_cast<uint64_t>(a.groups) * blocks_for(a.wide, bm) * across)
+                                     : by_eights(a.rows / bm * across) + by_eights((a.groups < a.rows ? a.groups : a.rows) * across);
+  if (tiles > 0xFFFFFFFFull / threads || tiles > 1u << 24) return UCCL_ETOOBIG;
   return enqueue(kernel, dim3(static_cast<uint32_t>(tiles)), threads, s, a);
 }
 
-// What a tile costs is about the same whether one compute unit works or all do, and a launch takes as long as the compute units
-// that get one tile more than others.  256 x 256 does the most work for what it reads; smaller tiles leave less of themselves empty
-// in small groups and fill the machine when there are few.  In units of a tile of 256 x 256 (which takes 196 us with a depth of 7168
-// in bf16, one a compute unit), 128 x 256 costs 0.69 and 128 x 128 0.45.  Measured in bf16, 256 x 256 / 128 x 256 / 128 x 128, us: 4096 rows in 16 ragged
-// groups, 7168 -> 2048, 201 / 223 / 234; 2048 rows 192 / 139 / 161; 1024 rows 181 / 120 / 115; 2999 rows in 24 groups, 2043 -> 1003, 57 / 35 / 45;
-// 8190 rows in 16 groups, 2048 -> 7168, 303 / 305 / 372; 512 rows in one group, 2048 -> 2048, 43 / 26 / 18.
+// What a tile costs is about the same whether one compute unit works or all do, and whether all of its rows are there or a few, and
+// a launch of few tiles takes as long as the compute units that get one more than others.  256 x 256 does the most work for what
+// it reads; smaller tiles leave less of themselves empty in small groups and fill the machine when there are few.  In units of
+// a tile of 256 x 256 (180 us with a depth of 7168 in bf16, one a compute unit), 128 x 256 costs 0.69 and 128 x 128 0.45.  Measured in bf16,
+// 256 x 256 / 128 x 256 / 128 x 128, us: 4096 rows in 16 ragged groups, 7168 -> 2048, 182 / 223 / 240; 2048 rows 163 / 132 / 164; 1024 rows
+// 152 / 119 / 112; 2999 rows in 24 groups, 2043 -> 1003, 50 / 35 / 44; 8190 rows in 16 groups, 2048 -> 7168, 290 / 339 / 398; 512 rows in one group,
+// 2048 -> 2048, 45 / 28 / 18; both gradients of 3000 rows in 8 groups, 3360 -> 1120, 123 / 153 / 184.
 enum Tile : uint32_t { kTile256, kTile128x256, kTile128 };
 
 template <Product P>
@@ -122,7 +121,8 @@ Tile choose_tile(const ProductArgs& a) {
     // a group's last tile is half empty on average
     const double down = P == kGradW ? static_cast<double>(a.groups) * blocks_for(a.wide, high)
                                     : static_cast<double>(a.rows) / high + 0.5 * (a.groups < a.rows ? a.groups : a.rows);
-    return ceil(down * blocks_for(P == kForward ? a.wide : a.cols, wide) / 256.0) * unit;
+    const double rounds = down * blocks_for(P == kForward ? a.wide : a.cols, wide) / 256.0;   // over 256 compute units
+    return unit * (rounds <= 2.0 ? ceil(rounds) : rounds + 0.5);
   };
   const double large = cost(256u, 256u, 1.0), middle = cost(128u, 256u, 0.69), small = cost(128u, 128u, 0.45);
   return large <= middle && large <= small ? kTile256 : middle <= small ? kTile128x256 : kTile128;
