@@ -12,6 +12,12 @@
  * work on `stream` and returns: no allocation, no host synchronisation, no host read of device memory.  Calls may be
  * captured into a graph.  The results of a call on the same inputs are the same bit for bit: no atomics.
  *
+ * Every call returns UCCL_OK, also where there is nothing to compute; UCCL_EINVAL: a null pointer, shapes or types that do not
+ * match; UCCL_EALIGN; UCCL_ETOOBIG: more workgroups than one launch can have (2^32 threads: 2^22 - 1 rows of a norm, and fewer than 2^23 tiles
+ * of 128 x 128 elements of a product always fit; split the call); UCCL_ELAUNCH: HIP's, the text in uccl_last_error_detail().  Nothing has
+ * been enqueued then, but for uccl_norm_rows_grad: two launches, of which HIP may take the first and refuse the second.
+ * uccl_time_next_launch times these calls too.
+ *
  * The operators are no passage of the paper, which moves such rows and leaves the work on them to the application
  * (its evaluation has expert-parallel prefill and decode among the applications).
  */
@@ -56,9 +62,6 @@ typedef struct uccl_rows {
  * Sums are held in binary32, and y is computed from h before that is rounded for storage.  y may be x or r itself if it has
  * its type and stride.  A NaN or an infinity in a row makes the row's y what the formula makes it; elements that are not finite do
  * not enter the scale unless they are infinities.
- * UCCL_OK, also for no rows or no columns (nothing is enqueued); UCCL_EINVAL: a null pointer, shapes or types that do not
- * match; UCCL_EALIGN; UCCL_ELAUNCH.  On an error nothing has been enqueued (but for uccl_norm_rows_grad, two launches, of which HIP
- * may take the first and refuse the second).
  */
 typedef struct uccl_norm_opts { /* HOST struct, read during the call */
   float eps;
@@ -97,9 +100,7 @@ uint64_t uccl_norm_rows_scratch(uint32_t rows, uint32_t cols);
  * products are exact but where y is 16 bits wide, k at least 512 and the call large enough for the matrix instruction for 8 bits:
  * that adds 64 products at a time and drops of each what is below about 2^-13 of the greatest of them, which is far below what
  * rounding y to 16 bits drops.
- * What a call is cut into depends on its sizes alone, never on the offsets' values.  UCCL_OK, also where there is nothing to
- * compute; UCCL_EINVAL: a null pointer, shapes or types that do not match; UCCL_EALIGN; UCCL_ETOOBIG: more than 2^24 tiles (of
- * 128 x 128 elements of the output, or 16 rows x 32 columns for groups of few rows: split the call); UCCL_ELAUNCH.
+ * What a call is cut into depends on its sizes alone, never on the offsets' values.
  */
 int uccl_group_product(const uccl_rows* y, const uccl_rows* x, const int32_t* index, const uccl_rows* w,
                        const int32_t* offsets, uint32_t n_groups, void* stream);

@@ -53,6 +53,14 @@ Rows rows_of(const uccl_rows* m) {
 
 uint32_t blocks_for(uint64_t n, uint32_t each) { return static_cast<uint32_t>((n + each - 1) / each); }
 
+// A grid of `groups` workgroups; HIP takes fewer than 2^32 threads a launch.
+bool fits(uint64_t groups, uint32_t threads) { return groups <= 0xFFFFFFFFull / threads; }
+
+template <class K, class... A>
+int launch(K kernel, uint64_t groups, uint32_t threads, hipStream_t s, A... a) {
+  return fits(groups, threads) ? enqueue(kernel, dim3(static_cast<uint32_t>(groups)), threads, s, a...) : static_cast<int>(UCCL_ETOOBIG);
+}
+
 // Calls f with a value of the element type of 16- or 32-bit rows.
 template <class F>
 int with_type(uint32_t dtype, F f) {
@@ -68,14 +76,13 @@ bool too_large_to_keep(const uccl_rows* m) { return static_cast<uint64_t>(m->row
 template <class T, bool E8, bool ONCE>
 int norm(const NormArgs& a, hipStream_t s) {
   const uint32_t pieces = blocks_for(a.cols, Piece<T>::N);
-  const dim3 grid(a.rows);
-  if (pieces <= 64u) return enqueue(norm_kernel<T, E8, 64, 1, ONCE>, grid, 64, s, a);
-  if (pieces <= 256u) return enqueue(norm_kernel<T, E8, 256, 1, ONCE>, grid, 256, s, a);
-  if (pieces <= 512u) return enqueue(norm_kernel<T, E8, 512, 1, ONCE>, grid, 512, s, a);
-  if (pieces <= 1024u && a.rows > 512u) return enqueue(norm_kernel<T, E8, 512, 2, ONCE>, grid, 512, s, a);
-  if (pieces <= 1024u) return enqueue(norm_kernel<T, E8, 1024, 1, ONCE>, grid, 1024, s, a);
-  if (pieces <= 2048u) return enqueue(norm_kernel<T, E8, 512, 4, ONCE>, grid, 512, s, a);
-  return enqueue(norm_long_kernel<T, E8>, grid, 1024, s, a);
+  if (pieces <= 64u) return launch(norm_kernel<T, E8, 64, 1, ONCE>, a.rows, 64, s, a);
+  if (pieces <= 256u) return launch(norm_kernel<T, E8, 256, 1, ONCE>, a.rows, 256, s, a);
+  if (pieces <= 512u) return launch(norm_kernel<T, E8, 512, 1, ONCE>, a.rows, 512, s, a);
+  if (pieces <= 1024u && a.rows > 512u) return launch(norm_kernel<T, E8, 512, 2, ONCE>, a.rows, 512, s, a);
+  if (pieces <= 1024u) return launch(norm_kernel<T, E8, 1024, 1, ONCE>, a.rows, 1024, s, a);
+  if (pieces <= 2048u) return launch(norm_kernel<T, E8, 512, 4, ONCE>, a.rows, 512, s, a);
+  return launch(norm_long_kernel<T, E8>, a.rows, 1024, s, a);
 }
 
 // Workgroups that share the rows of a norm's gradient, at most: one a compute unit.  (512 of them come in two rounds: 4096 x 7168 in bf16
@@ -85,12 +92,12 @@ constexpr uint32_t kGradGroups = 256;
 template <class T, bool ONCE>
 int norm_grad(const NormGradArgs& a, uint32_t groups, hipStream_t s) {
   const uint32_t pieces = blocks_for(a.cols, Piece<T>::N);
-  if (pieces <= 256u) return enqueue(norm_grad_kernel<T, 256, 1, ONCE>, dim3(groups), 256, s, a);
-  if (pieces <= 512u) return enqueue(norm_grad_kernel<T, 512, 1, ONCE>, dim3(groups), 512, s, a);
-  if (pieces <= 1024u) return enqueue(norm_grad_kernel<T, 1024, 1, ONCE>, dim3(groups), 1024, s, a);
+  if (pieces <= 256u) return launch(norm_grad_kernel<T, 256, 1, ONCE>, groups, 256, s, a);
+  if (pieces <= 512u) return launch(norm_grad_kernel<T, 512, 1, ONCE>, groups, 512, s, a);
+  if (pieces <= 1024u) return launch(norm_grad_kernel<T, 1024, 1, ONCE>, groups, 1024, s, a);
   if constexpr (sizeof(T) == 4)
-    if (pieces <= 2048u) return enqueue(norm_grad_kernel<T, 512, 4, ONCE>, dim3(groups), 512, s, a);
-  return enqueue(norm_grad_long_kernel<T>, dim3(groups), 1024, s, a);
+    if (pieces <= 2048u) return launch(norm_grad_kernel<T, 512, 4, ONCE>, groups, 512, s, a);
+  return launch(norm_grad_long_kernel<T>, groups, 1024, s, a);
 }
 
 OutType out_type(const uccl_rows* m) { return m->dtype == UCCL_F32 ? kOutF32 : m->dtype == UCCL_BF16 ? kOutBf16 : kOutF16; }
@@ -102,8 +109,8 @@ int product_tiles(K kernel, uint32_t bm, uint32_t bn, uint32_t threads, const Pr
   auto by_eights = [](uint64_t n) { return (n + 7u) / 8u * 8u; };
   const uint64_t tiles = P == kGradW ? by_eights(static_cast<uint64_t>(a.groups) * blocks_for(a.wide, bm) * across)
                                      : by_eights(a.rows / bm * across) + by_eights((a.groups < a.rows ? a.groups : a.rows) * across);
-  if (tiles > 0xFFFFFFFFull / threads || tiles > 1u << 24) return UCCL_ETOOBIG;
-  return enqueue(kernel, dim3(static_cast<uint32_t>(tiles)), threads, s, a);
+  if (tiles > 1u << 24) return UCCL_ETOOBIG;   // find_tile() counts them in 25 bits
+  return launch(kernel, tiles, threads, s, a);
 }
 
 // What a tile costs is about the same whether one compute unit works or all do, and whether all of its rows are there or a few, and
@@ -143,7 +150,7 @@ int product_of(const ProductArgs& a, hipStream_t s) {
   if constexpr (P == kForward)
     if (takes_few_rows(a)) {
       // 32 columns a workgroup of 4 wavefronts, two workgroups on a compute unit; 16 columns and 8 wavefronts where that would leave most
-      // compute units idle (one row, 7168 -> 2048, bf16: 16.9 against 8.7 us; 16 rows in 8 of 32 groups: 41 against 50 us)
+      // compute units idle (one row, 7168 -> 2048, bf16: 8.7 us so, 16.9 with 32 columns; 16 rows in 8 of 32 groups: 50 so, 41 with 32)
       const uint32_t groups = a.rows < a.groups ? a.rows : a.groups;
       if (static_cast<uint64_t>(groups) * blocks_for(a.wide, 32u) <= 256u) return product_tiles<P>(product_few_kernel<M, 16, 8>, 16, 16, 512, a, s);
       return product_tiles<P>(product_few_kernel<M, 32, 4>, 16, 32, 256, a, s);
@@ -221,6 +228,8 @@ int uccl_norm_rows_grad(const uccl_rows* dx, float* dweight, const uccl_rows* dy
   if (h->cols == 0u) return UCCL_OK;
   if (dweight == nullptr) return UCCL_EINVAL;
   if (misaligned(dweight, 4)) return UCCL_EALIGN;
+  const uint32_t sums = blocks_for(h->cols, 64u);
+  if (!fits(sums, 1024)) return UCCL_ETOOBIG;   // before the first of the two launches
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const uint32_t groups = h->rows < kGradGroups ? h->rows : kGradGroups;
   if (h->rows != 0u) {
@@ -233,7 +242,7 @@ int uccl_norm_rows_grad(const uccl_rows* dx, float* dweight, const uccl_rows* dy
     });
     if (e != UCCL_OK) return e;
   }
-  return enqueue(column_sum_kernel, dim3(blocks_for(h->cols, 64u)), 1024, s, dweight, static_cast<const float*>(scratch), groups, h->cols);
+  return launch(column_sum_kernel, sums, 1024, s, dweight, static_cast<const float*>(scratch), groups, h->cols);
 }
 
 // What the three products have in common.  `x` of kForward and kGradW is read through the index.
@@ -306,11 +315,9 @@ int uccl_combine_rows(const uccl_rows* out, const uccl_rows* y, const int32_t* p
     using T = decltype(t);
     const uint32_t blocks = blocks_for(blocks_for(out->cols, Piece<T>::N), 128u);
     const uint64_t grid = static_cast<uint64_t>(out->rows) * blocks;
-    if (grid > 0xFFFFFFFFull / 128u) return static_cast<int>(UCCL_ETOOBIG);
     const CombineArgs a{rows_of(out), rows_of(y), rows_of(r), pos, weights, out->rows, y->rows == 0u ? 0u : slots, y->rows, out->cols, blocks};
-    const dim3 g(static_cast<uint32_t>(grid));
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    return too_large_to_keep(out) ? enqueue(combine_kernel<T, 128, true>, g, 128, s, a) : enqueue(combine_kernel<T, 128, false>, g, 128, s, a);
+    return too_large_to_keep(out) ? launch(combine_kernel<T, 128, true>, grid, 128, s, a) : launch(combine_kernel<T, 128, false>, grid, 128, s, a);
   });
 }
 
@@ -328,7 +335,7 @@ int uccl_combine_rows_grad(const uccl_rows* dy, float* dweights, const uccl_rows
     // (without a row there is nothing to write but the weights' gradient: an empty sum for every slot)
     const CombineGradArgs a{rows_of(dy), rows_of(dout), rows_of(y), pos, weights, dweights, dout->rows, slots, y->rows, y->rows == 0u ? 0u : dout->cols};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    return too_large_to_keep(dy) ? enqueue(combine_grad_kernel<T, true>, dim3(dout->rows), 256, s, a) : enqueue(combine_grad_kernel<T, false>, dim3(dout->rows), 256, s, a);
+    return too_large_to_keep(dy) ? launch(combine_grad_kernel<T, true>, dout->rows, 256, s, a) : launch(combine_grad_kernel<T, false>, dout->rows, 256, s, a);
   });
 }
 

@@ -69,6 +69,7 @@ OK, EINVAL, EALIGN = pkg.UCCL_OK, pkg.UCCL_EINVAL, pkg.UCCL_EALIGN
     (rows(0, 8), None, None, rows(0, 8, data=None), None, None, 1e-6, OK),
     (rows(2, 0), None, None, rows(2, 0, data=None), None, None, 1e-6, OK),
     (rows(1 << 31, 8), None, None, rows(1 << 31, 8), None, B, 1e-6, EINVAL),
+    (rows(1, (1 << 30) + 8), None, None, rows(1, (1 << 30) + 8), None, B, 1e-6, EINVAL),
 ])
 def test_norm_refusals(y, h, rstd, x, r, weight, eps, code):
     assert pkg.load().uccl_norm_rows(y, h, rstd, x, r, weight, C.byref(pkg.uccl_norm_opts(eps)), None) == code
@@ -279,6 +280,14 @@ def product_kernels(rt):
     assert rt.lib.uccl_group_product(rows(big, 8 << 20), rows(big, 64), None, rows(8 << 20, 64), M, 1, None) == pkg.UCCL_ETOOBIG
     assert rt.launches == []
     assert rt.lib.uccl_combine_rows(rows(big, 1 << 20), rows(9, 1 << 20), M, None, 2, None, None) == pkg.UCCL_ETOOBIG
+    norm = lambda n, c: rt.lib.uccl_norm_rows(rows(n, c), None, None, rows(n, c), None, B, C.byref(pkg.uccl_norm_opts(1e-6)), None)
+    assert [norm(n, c) for n, c in ((1 << 26, 128), ((1 << 22) - 1, 1 << 20), (1 << 22, 1 << 20))] == [pkg.UCCL_ETOOBIG, OK, pkg.UCCL_ETOOBIG]
+    assert len(rt.launches) == 1
+    rt.launches.clear()
+    wide = 1 << 28
+    assert rt.lib.uccl_norm_rows_grad(rows(1, wide), D, rows(1, wide), None, rows(1, wide), D, B, S, 4 * wide, None) == pkg.UCCL_ETOOBIG
+    assert rt.lib.uccl_combine_rows_grad(rows(9, 8), None, rows(1 << 24, 8), rows(9, 8), M, None, 1, None) == pkg.UCCL_ETOOBIG
+    assert rt.launches == []
     # launches that the runtime refuses come back as such
     rt.refuse = lambda *a: True
     assert rt.lib.uccl_group_product(rows(512, 2048), rows(512, 2048), None, rows(2048, 2048), M, 1, None) == pkg.UCCL_ELAUNCH
