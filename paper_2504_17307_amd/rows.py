@@ -8,6 +8,7 @@ for, say) is checked here and raises ValueError.  Outputs are the caller's tenso
 """
 import ctypes as C
 import os
+import struct
 
 UCCL_E4M3 = 16
 ROWS_HEADER_PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "uccl_rows.h")
@@ -22,10 +23,14 @@ class uccl_norm_opts(C.Structure):
     _fields_ = [("eps", C.c_float), ("reserved", C.c_uint32 * 3)]
 
 
-_R, _P, _U32 = C.POINTER(uccl_rows), C.c_void_p, C.c_uint32
+# Rows are passed as the struct's bytes, which take a third of the time of a ctypes structure's making.
+_pack_rows = struct.Struct("@QQQQIIII").pack
+assert len(_pack_rows(*[0] * 8)) == C.sizeof(uccl_rows)
+
+_R, _P, _U32 = C.c_void_p, C.c_void_p, C.c_uint32
 
 ROWS_SIGNATURES = {
-    "uccl_norm_rows": (C.c_int, [_R, _R, _P, _R, _R, _P, C.POINTER(uccl_norm_opts), _P]),
+    "uccl_norm_rows": (C.c_int, [_R, _R, _P, _R, _R, _P, _P, _P]),
     "uccl_norm_rows_grad": (C.c_int, [_R, _P, _R, _R, _R, _P, _P, _P, C.c_uint64, _P]),
     "uccl_norm_rows_scratch": (C.c_uint64, [_U32, _U32]),
     "uccl_group_product": (C.c_int, [_R, _R, _P, _R, _P, _U32, _P]),
@@ -50,35 +55,39 @@ def _type(dtype):
 
 
 def _rows(t, scales=None):
-    """A HOST uccl_rows for a tensor, as an argument; None for None."""
+    """The bytes of a HOST uccl_rows for a tensor, as an argument; None for None."""
     if t is None:
         return None
-    number, size = _type(t.dtype)
-    shape, strides = t.shape, t.stride()
+    number, size = _types.get(t.dtype) or _type(t.dtype)
+    shape = t.shape
     if len(shape) == 2:
         rows, cols = shape
-        step = strides[0]
+        step, last = t.stride()
     elif len(shape) == 3:
-        rows, cols = shape[0] * shape[1], shape[2]
-        step = strides[1] if shape[1] > 1 else strides[0]
-        if shape[0] > 1 and rows and cols and strides[0] != shape[1] * step:
+        groups, each, cols = shape
+        apart, step, last = t.stride()
+        rows = groups * each
+        if each == 1:
+            step = apart
+        elif groups > 1 and rows and cols and apart != each * step:
             raise ValueError("the rows of a three-dimensional tensor have to be the same distance apart throughout")
     else:
         raise ValueError("a tensor of rows has two or three dimensions")
-    if cols > 1 and strides[-1] != 1:
+    if last != 1 and cols > 1:
         raise ValueError("the last dimension of a tensor of rows has to be contiguous")
-    at, between = None, 0
-    if scales is not None:
-        if scales.dtype is not _types["scale"] or scales.numel() != rows:
-            raise ValueError("scales are float32, one for every row")
-        lengths, apart = scales.shape, scales.stride()
-        if len(lengths) > 1 and lengths[-1] == 1:   # a last dimension of one scale
-            lengths, apart = lengths[:-1], apart[:-1]
-        if len(lengths) == 2 and lengths[0] > 1 and lengths[1] > 1 and apart[0] != lengths[1] * apart[1] or len(lengths) > 2:
-            raise ValueError("scales have to be the same distance apart throughout")
-        between = 0 if not lengths else 4 * (apart[0] if lengths[-1] == 1 else apart[-1])
-        at = scales.data_ptr()
-    return C.byref(uccl_rows(t.data_ptr(), step * size, at, between, rows, cols, number, 0))
+    if rows > 0xFFFFFFFF or cols > 0xFFFFFFFF:
+        raise ValueError("a tensor of rows has fewer than 2^32 rows and columns")
+    if scales is None:
+        return _pack_rows(t.data_ptr(), step * size, 0, 0, rows, cols, number, 0)
+    if scales.dtype is not _types["scale"] or scales.numel() != rows:
+        raise ValueError("scales are float32, one for every row")
+    lengths, apart = scales.shape, scales.stride()
+    if len(lengths) > 1 and lengths[-1] == 1:   # a last dimension of one scale
+        lengths, apart = lengths[:-1], apart[:-1]
+    if len(lengths) == 2 and lengths[0] > 1 and lengths[1] > 1 and apart[0] != lengths[1] * apart[1] or len(lengths) > 2:
+        raise ValueError("scales have to be the same distance apart throughout")
+    between = 0 if not lengths else 4 * (apart[0] if lengths[-1] == 1 else apart[-1])
+    return _pack_rows(t.data_ptr(), step * size, scales.data_ptr(), between, rows, cols, number, 0)
 
 
 def _vector(t, kind, n, what):

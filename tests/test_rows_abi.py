@@ -203,6 +203,33 @@ def test_the_binding_refuses_what_only_the_tensors_know():
     assert e.value.code == EINVAL
 
 
+def test_the_binding_refuses_more_rows_than_the_struct_can_say():
+    """2^32 rows and more do not come down to what is left of them: no rows, or one."""
+    import torch
+    one = torch.zeros(1, 8, dtype=torch.bfloat16)
+    for n in (1 << 32, (1 << 32) + 1):
+        many = one.expand(n, 8)
+        with pytest.raises(ValueError):
+            pkg.uccl_norm_rows(many, many, one[0], 1e-6, stream=0)
+        with pytest.raises(ValueError):
+            pkg.uccl_combine_rows(one[:0], many, torch.zeros(0, 2, dtype=torch.int32), stream=0)
+
+
+def test_prepared_calls_hold_their_structs():
+    """The bytes of a uccl_rows live as long as the prepared call does."""
+    import gc
+    import torch
+    x, eps = torch.zeros(3, 8, dtype=torch.bfloat16), 1e-6
+    call = pkg.uccl_prepare(pkg.uccl_norm_rows, x, x, torch.zeros(8, dtype=torch.bfloat16), eps, stream=0, h=x[:2])   # refused: shapes
+    gc.collect()
+    junk = [bytes(48) for _ in range(1000)]
+    for _ in range(3):
+        with pytest.raises(pkg.UcclError) as e:
+            call()
+        assert e.value.code == EINVAL
+    assert junk
+
+
 def test_calls_can_be_prepared():
     import torch
     bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
