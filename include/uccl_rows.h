@@ -13,7 +13,7 @@
  * captured into a graph.  The results of a call on the same inputs are the same bit for bit: no atomics.
  *
  * Every call returns UCCL_OK, also where there is nothing to compute; UCCL_EINVAL: a null pointer, shapes or types that do not
- * match; UCCL_EALIGN; UCCL_ETOOBIG: more workgroups than one launch can have (2^32 threads: 2^22 - 1 rows of a norm, and fewer than 2^23 tiles
+ * match; UCCL_EALIGN; UCCL_ETOOBIG: more workgroups than one launch can have (2^32 threads: 2^22 - 1 rows of a norm, and fewer than 2^22 tiles
  * of 128 x 128 elements of a product always fit; split the call); UCCL_ELAUNCH: HIP's, the text in uccl_last_error_detail().  Nothing has
  * been enqueued then, but for uccl_norm_rows_grad: two launches, of which HIP may take the first and refuse the second.
  * uccl_time_next_launch times these calls too.

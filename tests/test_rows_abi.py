@@ -271,7 +271,15 @@ def product_kernels(rt):
         (E4M3, 2048, 16, 2048, 7168, BF16, "tile_kernelILNS_10ArithmeticE3ELNS_7ProductE0ELj128ELj256E"),
         (E4M3, 4096, 16, 2048, 7168, F32, "tile_kernelILNS_10ArithmeticE2ELNS_7ProductE0ELj128ELj128E"),   # exact where it can be seen
         (E4M3, 4096, 16, 2048, 500, BF16, "tile_kernelILNS_10ArithmeticE2ELNS_7ProductE0ELj128ELj128E"),
-        (E4M3, 512, 1, 2048, 7168, BF16, "tile_kernelILNS_10ArithmeticE2ELNS_7ProductE0ELj128ELj128E"),
+        (E4M3, 512, 1, 2048, 7168, BF16, "tile_kernelILNS_10ArithmeticE3ELNS_7ProductE0ELj128ELj256E"),
+        (E4M3, 4000, 4, 2048, 7168, BF16, "tile_kernelILNS_10ArithmeticE3ELNS_7ProductE0ELj256ELj256E"),
+        # few rows: by 16 while that is cheaper than the tiles that leave the machine idle
+        (BF16, 20, 1, 2048, 7168, BF16, "few_kernelILNS_10ArithmeticE0ELj16ELj8E"),
+        (BF16, 100, 1, 2048, 7168, BF16, "few_kernelILNS_10ArithmeticE0ELj32ELj4E"),
+        (E4M3, 20, 8, 1200, 3000, BF16, "few_kernelILNS_10ArithmeticE2ELj32ELj4E"),
+        (BF16, 400, 1, 2048, 7168, BF16, "tile_kernelILNS_10ArithmeticE0ELNS_7ProductE0ELj128ELj128E"),
+        (E4M3, 200, 1, 2048, 7168, BF16, "few_kernelILNS_10ArithmeticE2ELj32ELj4E"),
+        (BF16, 4096, 3, 5, 500, BF16, "few_kernelILNS_10ArithmeticE0ELj32ELj4E"),
         (BF16, 4096, 16, 2048, 7168, BF16, "tile_kernelILNS_10ArithmeticE0ELNS_7ProductE0ELj256ELj256E"),
         (F16, 2999, 24, 1003, 2043, F16, "tile_kernelILNS_10ArithmeticE1ELNS_7ProductE0ELj128ELj256E"),
         (BF16, 512, 1, 2048, 2048, BF16, "tile_kernelILNS_10ArithmeticE0ELNS_7ProductE0ELj128ELj128E"),
