@@ -279,7 +279,7 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 // 64 lanes' 16 bytes from memory into the LDS at `to` (the same in every lane), lane by lane.  The compiler does not see the
 // write: wait_for_loads() orders it before the reads.
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "m0");
 }
 // Every wavefront has at most its newest `N` loads under way.  (Other loads of the wavefront that are counted too only make this
 // stricter: they return in order.)
