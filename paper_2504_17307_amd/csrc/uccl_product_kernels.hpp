@@ -31,6 +31,7 @@ struct ProductArgs {
   const int32_t* index;     // or nullptr: row i itself
   const int32_t* offsets;   // groups + 1
   uint32_t groups, rows, indexed_rows, wide, cols, out_type;
+  uint32_t together;        // by rows: the order of the tiles, find_tile()
 };
 
 struct Group {
@@ -40,15 +41,12 @@ struct Group {
 // Offsets are taken as they can be used, whatever they hold: each is at least the one before it, at least 0 and at most
 // `rows`.  Groups never overlap then and no row outside the matrix is touched.
 //
-// 64 groups' ranges, a lane each, and how many tiles of `height` rows these are (every group is cut into tiles of its own), full ones
-// and those that a group ends in: the lane's, and up to and with the lane's, both numbers in one word.  `before`: the greatest offset
-// of earlier groups.
-constexpr uint32_t kFullBits = 25;   // a launch has at most 2^24 tiles, and 64 groups end in at most 64
+// 64 groups' ranges, a lane each.  `before`: the greatest offset of earlier groups.
 struct Ranges {
-  uint32_t begin, end, tiles, sum;
-  int32_t most;
+  uint32_t begin, end;
+  int32_t most;   // up to and with the lane's
 };
-__device__ __forceinline__ Ranges group_ranges(const ProductArgs& a, uint32_t at, int32_t before, uint32_t height) {
+__device__ __forceinline__ Ranges group_ranges(const ProductArgs& a, uint32_t at, int32_t before) {
   const uint32_t lane = threadIdx.x & 63u, mine = at + lane;
   const int32_t begin = mine <= a.groups ? a.offsets[mine] : 0, end = mine < a.groups ? a.offsets[mine + 1u] : 0;
   const int32_t limit = static_cast<int32_t>(a.rows);
@@ -61,16 +59,25 @@ __device__ __forceinline__ Ranges group_ranges(const ProductArgs& a, uint32_t at
   }
   const int32_t previous = __shfl_up(r.most, 1);
   r.begin = static_cast<uint32_t>(min(max(lane == 0u ? max(begin, before) : previous, 0), limit));
-  r.end = static_cast<uint32_t>(min(max(r.most, 0), limit));
-  const uint32_t n = mine < a.groups ? r.end - r.begin : 0u;
-  r.tiles = n / height | (n % height != 0u ? 1u << kFullBits : 0u);
-  r.sum = r.tiles;
+  r.end = mine < a.groups ? static_cast<uint32_t>(min(max(r.most, 0), limit)) : r.begin;
+  return r;
+}
+// A sum up to and with the lane's.
+__device__ __forceinline__ uint32_t sum_to_lane(uint32_t v) {
 #pragma unroll
   for (uint32_t d = 1; d < 64u; d <<= 1) {
-    const uint32_t other = __shfl_up(r.sum, d);
-    if (lane >= d) r.sum += other;
+    const uint32_t other = __shfl_up(v, d);
+    if ((threadIdx.x & 63u) >= d) v += other;
   }
-  return r;
+  return v;
+}
+
+// How many tiles of `height` rows the lanes' groups are cut into (every group into tiles of its own): full ones, and those that a group ends
+// in above them in the same word.
+constexpr uint32_t kFullBits = 25;   // a launch has at most 2^24 tiles, and 64 groups end in at most 64
+__device__ __forceinline__ uint32_t full_and_ends(const Ranges& r, uint32_t height) {
+  const uint32_t n = r.end - r.begin;
+  return n / height | (n % height != 0u ? 1u << kFullBits : 0u);
 }
 
 // Workgroups of a launch go round the eight XCDs in turn, and start in order.  Each XCD gets a contiguous eighth of the n tiles, so
@@ -91,19 +98,18 @@ __device__ __forceinline__ void place_in_band(uint32_t& tile, uint32_t down, uin
   tile = band * kBand + at % high;
 }
 
-// The workgroup's tile of the products by rows: its group, its first row and its place across.  All lanes of a wavefront call
-// it.  The launch has a workgroup for every tile that there could be; which there are is known here only.  Full tiles come
-// first, and tiles that groups end in, which take less, fill up what they leave.
-__device__ __forceinline__ bool find_tile(const ProductArgs& a, uint32_t height, uint32_t across, Group& g, uint32_t& first_row, uint32_t& place) {
+// Full tiles first, and tiles that groups end in, which take less, after them: they fill up what the last round leaves.
+__device__ __forceinline__ bool find_tile_by_size(const ProductArgs& a, uint32_t height, uint32_t across, Group& g, uint32_t& first_row, uint32_t& place) {
   constexpr uint32_t kFull = (1u << kFullBits) - 1u;
-  Ranges r = group_ranges(a, 0, 0, height);
-  uint32_t sum = __builtin_amdgcn_readlane(r.sum, 63), full = sum & kFull, ends = sum >> kFullBits;
+  Ranges r = group_ranges(a, 0, 0);
+  uint32_t own = full_and_ends(r, height), to = sum_to_lane(own);
+  uint32_t sum = __builtin_amdgcn_readlane(to, 63), full = sum & kFull, ends = sum >> kFullBits;
   if (a.groups > 64u) {
     int32_t before = __builtin_amdgcn_readlane(r.most, 63);
     for (uint32_t at = 64; at < a.groups; at += 64u) {
-      const Ranges next = group_ranges(a, at, before, height);
+      const Ranges next = group_ranges(a, at, before);
       before = __builtin_amdgcn_readlane(next.most, 63);
-      sum = __builtin_amdgcn_readlane(next.sum, 63);
+      sum = __builtin_amdgcn_readlane(sum_to_lane(full_and_ends(next, height)), 63);
       full += sum & kFull;
       ends += sum >> kFullBits;
     }
@@ -115,20 +121,50 @@ __device__ __forceinline__ bool find_tile(const ProductArgs& a, uint32_t height,
   place_in_band(tile, whole ? full : ends, across, place);
   uint32_t passed = 0;
   for (uint32_t at = 0;; at += 64u) {
-    const uint32_t count = whole ? r.sum & kFull : r.sum >> kFullBits, own = whole ? r.tiles & kFull : r.tiles >> kFullBits;
+    const uint32_t count = whole ? to & kFull : to >> kFullBits, mine = whole ? own & kFull : own >> kFullBits;
     const uint64_t holds = __ballot(passed + count > tile);
     if (holds != 0u) {
       const int l = __ffsll(static_cast<unsigned long long>(holds)) - 1;
-      g.index = at + static_cast<uint32_t>(l);
-      g.begin = __builtin_amdgcn_readlane(r.begin, l);
-      g.end = __builtin_amdgcn_readlane(r.end, l);
-      const uint32_t nth = whole ? tile - passed - (__builtin_amdgcn_readlane(count, l) - __builtin_amdgcn_readlane(own, l)) : (g.end - g.begin) / height;
+      g = Group{at + static_cast<uint32_t>(l), static_cast<uint32_t>(__builtin_amdgcn_readlane(r.begin, l)), static_cast<uint32_t>(__builtin_amdgcn_readlane(r.end, l))};
+      const uint32_t nth = whole ? tile - passed - (__builtin_amdgcn_readlane(count, l) - __builtin_amdgcn_readlane(mine, l)) : (g.end - g.begin) / height;
       first_row = g.begin + nth * height;
       return true;
     }
     passed += __builtin_amdgcn_readlane(count, 63);
-    r = group_ranges(a, at + 64u, __builtin_amdgcn_readlane(r.most, 63), height);
+    r = group_ranges(a, at + 64u, __builtin_amdgcn_readlane(r.most, 63));
+    own = full_and_ends(r, height);
+    to = sum_to_lane(own);
   }
+}
+
+// Each XCD takes an eighth of every group's tiles, column by column: those that read the same weights are on one XCD at the same time.
+__device__ __forceinline__ bool find_tile_by_group(const ProductArgs& a, uint32_t height, uint32_t across, Group& g, uint32_t& first_row, uint32_t& place) {
+  uint32_t turn = blockIdx.x / 8u;
+  int32_t before = 0;
+  for (uint32_t at = 0; at < a.groups; at += 64u) {
+    const Ranges r = group_ranges(a, at, before);
+    // the remainders of the eighths go round with the groups
+    const uint32_t eighth = (blockIdx.x + at + (threadIdx.x & 63u)) % 8u, down = (r.end - r.begin + height - 1u) / height, tiles = down * across;
+    const uint32_t first = tiles * eighth / 8u, own = tiles * (eighth + 1u) / 8u - first, to = sum_to_lane(own);
+    const uint64_t holds = __ballot(to > turn);
+    if (holds != 0u) {
+      const int l = __ffsll(static_cast<unsigned long long>(holds)) - 1;
+      g = Group{at + static_cast<uint32_t>(l), static_cast<uint32_t>(__builtin_amdgcn_readlane(r.begin, l)), static_cast<uint32_t>(__builtin_amdgcn_readlane(r.end, l))};
+      const uint32_t tile = __builtin_amdgcn_readlane(first, l) + turn - (__builtin_amdgcn_readlane(to, l) - __builtin_amdgcn_readlane(own, l)), high = __builtin_amdgcn_readlane(down, l);
+      first_row = g.begin + tile % high * height;
+      place = tile / high;
+      return true;
+    }
+    turn -= __builtin_amdgcn_readlane(to, 63);
+    before = __builtin_amdgcn_readlane(r.most, 63);
+  }
+  return false;
+}
+
+// The workgroup's tile of the products by rows: its group, its first row and its place across.  All lanes of a wavefront call
+// it.  The launch has a workgroup for every tile that there could be; which there are is known here only.
+__device__ __forceinline__ bool find_tile(const ProductArgs& a, uint32_t height, uint32_t across, Group& g, uint32_t& first_row, uint32_t& place) {
+  return a.together != 0u ? find_tile_by_group(a, height, across, g, first_row, place) : find_tile_by_size(a, height, across, g, first_row, place);
 }
 
 // The rows of group g, by the same rule.

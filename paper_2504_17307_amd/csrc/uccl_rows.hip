@@ -102,9 +102,24 @@ int norm_grad(const NormGradArgs& a, uint32_t groups, hipStream_t s) {
 
 OutType out_type(const uccl_rows* m) { return m->dtype == UCCL_F32 ? kOutF32 : m->dtype == UCCL_BF16 ? kOutBf16 : kOutF16; }
 
+uint32_t used_groups(const ProductArgs& a) { return a.groups < a.rows ? a.groups : a.rows; }   // that have rows, at most
+
+// How many tiles of so many rows the groups are cut into: the last one of a group is half empty on average.
+double tiles_down(const ProductArgs& a, uint32_t high) {
+  return a.groups == 1u ? blocks_for(a.rows, high) : static_cast<double>(a.rows) / high + 0.5 * used_groups(a);
+}
+
 // A launch over tiles of BM x BN: a workgroup for each that there could be whatever the offsets are, by eights.
+//
+// The tiles of products by rows come in one of two orders.  Full ones first keep the last round short; all of a group's together read its
+// weights once, which pays where a group has many.  Measured, by size / by group, us: 8190 rows in 16 groups, 2048 -> 7168, bf16 (70 tiles a group) 297 / 273
+// (1.1 GB read, XXX); gradients of 4096 rows in 16 groups, 7168 x 2048 (42) 183 / 167; by 16 rows, 3000 -> 1200, bf16, 100 rows in one group / 3 / 8 (266, 98,
+// 49) 10.6 / 8.9, 13.8 / 8.9, 17.2 / 15.2; 200 rows in one group, 7168 -> 2048 (32) 48 / 50; 400 rows in 8 groups (14) 47 / 50; gradients of 2000 rows in
+// 32 groups, 1003 x 600 (5) 13 / 17.
+constexpr double kTogether = 40.0;
+
 template <Product P, class K>
-int product_tiles(K kernel, uint32_t bm, uint32_t bn, uint32_t threads, const ProductArgs& a, hipStream_t stream) {
+int product_tiles(K kernel, uint32_t bm, uint32_t bn, uint32_t threads, ProductArgs a, hipStream_t stream) {
   const uint64_t across = blocks_for(P == kForward ? a.wide : a.cols, bn);
   auto by_eights = [](uint64_t n) { return (n + 7u) / 8u * 8u; };
   uint64_t tiles;
@@ -114,7 +129,10 @@ int product_tiles(K kernel, uint32_t bm, uint32_t bn, uint32_t threads, const Pr
     const Slices s = slices_of(static_cast<uint32_t>(group));
     tiles = by_eights(static_cast<uint64_t>(a.groups) * s.n) * s.each;
   } else {
-    tiles = by_eights(a.rows / bm * across) + by_eights((a.groups < a.rows ? a.groups : a.rows) * across);
+    a.together = tiles_down(a, bm) * across >= kTogether * used_groups(a);
+    // by group, an XCD has of every group one tile more than its eighth at most
+    tiles = a.together ? by_eights((a.rows / bm + used_groups(a)) * across) + 8ull * used_groups(a)
+                       : by_eights(a.rows / bm * across) + by_eights(used_groups(a) * across);
   }
   if (tiles > 1u << 24) return UCCL_ETOOBIG;   // find_tile() counts them in 25 bits
   return launch(kernel, tiles, threads, stream, a);
@@ -131,13 +149,6 @@ int product_tiles(K kernel, uint32_t bm, uint32_t bn, uint32_t threads, const Pr
 // 128 x 256 / 128 x 128 by widened operands: 4000 rows in 4 groups, 7168 -> 2048, 76 / 98 / 171; 2500 rows 75 / 47 / 117; 333 rows 53 / 43 / 60; 4000 rows
 // in 16 groups 105 / 120 / 181; 1000 rows 58 / 52 / 115; 3000 rows in 32 groups, 1500 -> 800, 24 / 21 / 37.
 enum Tile : uint32_t { kTile256, kTile128x256, kTile128 };
-
-uint32_t used_groups(const ProductArgs& a) { return a.groups < a.rows ? a.groups : a.rows; }   // that have rows, at most
-
-// How many tiles of so many rows the groups are cut into: the last one of a group is half empty on average.
-double tiles_down(const ProductArgs& a, uint32_t high) {
-  return a.groups == 1u ? blocks_for(a.rows, high) : static_cast<double>(a.rows) / high + 0.5 * used_groups(a);
-}
 
 template <Product P>
 Tile choose_tile(const ProductArgs& a, bool native8) {
@@ -291,7 +302,7 @@ int uccl_group_product(const uccl_rows* y, const uccl_rows* x, const int32_t* in
   if ((n_groups != 0u && y->cols != wide) || (index == nullptr && x->rows < y->rows)) return UCCL_EINVAL;
   if (n_groups == 0u || y->rows == 0u || y->cols == 0u) return UCCL_OK;
   const uint32_t depth = x->rows == 0u ? 0u : x->cols;   // no row of x: nothing to add
-  const ProductArgs a{rows_of(y), rows_of(x), rows_of(w), index, offsets, n_groups, y->rows, x->rows, wide, depth, out_type(y)};
+  const ProductArgs a{rows_of(y), rows_of(x), rows_of(w), index, offsets, n_groups, y->rows, x->rows, wide, depth, out_type(y), 0};
   return product<kForward>(a, x->dtype, static_cast<hipStream_t>(stream));
 }
 
@@ -304,7 +315,7 @@ int uccl_group_product_grad_x(const uccl_rows* dx, const uccl_rows* dy, const uc
   if (e != UCCL_OK) return e;
   if (n_groups != 0u && dy->cols != wide) return UCCL_EINVAL;
   if (n_groups == 0u || dx->rows == 0u || dx->cols == 0u) return UCCL_OK;
-  const ProductArgs a{rows_of(dx), rows_of(dy), rows_of(w), nullptr, offsets, n_groups, dx->rows, dx->rows, wide, dx->cols, out_type(dx)};
+  const ProductArgs a{rows_of(dx), rows_of(dy), rows_of(w), nullptr, offsets, n_groups, dx->rows, dx->rows, wide, dx->cols, out_type(dx), 0};
   return product<kGradX>(a, dy->dtype, static_cast<hipStream_t>(stream));
 }
 
@@ -318,7 +329,7 @@ int uccl_group_product_grad_w(const uccl_rows* dw, const uccl_rows* dy, const uc
   if (e != UCCL_OK) return e;
   if ((n_groups != 0u && dy->cols != wide) || (index == nullptr && x->rows < dy->rows) || (n_groups != 0u && offsets == nullptr)) return UCCL_EINVAL;
   if (n_groups == 0u || wide == 0u || dw->cols == 0u) return UCCL_OK;
-  const ProductArgs a{rows_of(dw), rows_of(dy), rows_of(x), index, offsets, n_groups, dy->rows, x->rows, wide, dw->cols, out_type(dw)};
+  const ProductArgs a{rows_of(dw), rows_of(dy), rows_of(x), index, offsets, n_groups, dy->rows, x->rows, wide, dw->cols, out_type(dw), 0};
   return product<kGradW>(a, dy->dtype, static_cast<hipStream_t>(stream));
 }
 

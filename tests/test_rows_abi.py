@@ -309,7 +309,9 @@ def product_kernels(rt):
     # the grid: a workgroup for every tile that there could be, by eights, and a launch that HIP could not take is refused
     rt.launches.clear()
     assert rt.lib.uccl_group_product(rows(512, 2048), rows(512, 2048), None, rows(2048, 2048), M, 1, None) == OK
-    assert rt.launches[-1][1:3] == ((512 // 128 + 1) * 16, 512)
+    assert rt.launches[-1][1:3] == ((512 // 128 + 1) * 16 + 8, 512)      # a group's tiles together: an XCD's eighth may be one more
+    assert rt.lib.uccl_group_product(rows(500, 700), rows(500, 2048), None, rows(5600, 2048), M, 8, None) == OK
+    assert rt.launches[-1][1:3] == (3 * 6 + 6 + 8 * 6, 512)              # full tiles and those that groups end in, by eights
     rt.launches.clear()
     big = (1 << 31) - 1
     assert rt.lib.uccl_group_product(rows(big, 8 << 20), rows(big, 64), None, rows(8 << 20, 64), M, 1, None) == pkg.UCCL_ETOOBIG
