@@ -113,7 +113,7 @@ double tiles_down(const ProductArgs& a, uint32_t high) {
 //
 // The tiles of products by rows come in one of two orders.  Full ones first keep the last round short; all of a group's together read its
 // weights once, which pays where a group has many.  Measured, by size / by group, us: 8190 rows in 16 groups, 2048 -> 7168, bf16 (70 tiles a group) 297 / 273
-// (1.1 GB read, XXX); gradients of 4096 rows in 16 groups, 7168 x 2048 (42) 183 / 167; by 16 rows, 3000 -> 1200, bf16, 100 rows in one group / 3 / 8 (266, 98,
+// (1.10 / 0.93 GB read); gradients of 4096 rows in 16 groups, 7168 x 2048 (42) 183 / 167; by 16 rows, 3000 -> 1200, bf16, 100 rows in one group / 3 / 8 (266, 98,
 // 49) 10.6 / 8.9, 13.8 / 8.9, 17.2 / 15.2; 200 rows in one group, 7168 -> 2048 (32) 48 / 50; 400 rows in 8 groups (14) 47 / 50; gradients of 2000 rows in
 // 32 groups, 1003 x 600 (5) 13 / 17.
 constexpr double kTogether = 40.0;

@@ -4,6 +4,7 @@ Every stage is computed from the stage before it as that was rounded, so a resul
 its n terms' magnitudes.
 """
 import os
+import re
 import sys
 
 import pytest
@@ -152,3 +153,14 @@ def test_what_arrives_is_what_was_sent(layer):
     for chunk_rows, n in ((1, 37), (4, 10), (64, 1)):
         order = torch.randperm(n).tolist() + [0, n - 1]
         assert torch.equal(layer.dispatch(rows, order, chunk_rows), rows)
+
+
+def test_readme_example_of_a_product_runs(gpu_lib):
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    code = re.findall(r"```python\n(.*?)```", text, re.S)[1]
+    ns = {"torch": torch, "uccl": gpu_lib}
+    exec(compile(code, "README.md", "exec"), ns)
+    first = ns["first"].tolist()
+    for e, (b, f) in enumerate(zip(first, first[1:])):
+        x, w = ns["x"][b:f].double(), ns["w"][e].double()
+        close(ns["y"][b:f], x @ w.T, x.abs() @ w.abs().T, ns["cols"], f"expert {e}")
