@@ -170,6 +170,7 @@ Tile choose_tile(const ProductArgs& a, bool native8) {
 // 1003 -> 777, one group in bf16, 200 rows 6.2 against 11.7; 8 groups, 200 / 400 rows 6.2 / 19 against 10.7 / 11.5.
 template <Arithmetic M>
 bool takes_few_rows(const ProductArgs& a) {
+  if ((static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 32u) > 1u << 23) return false;   // more tiles than a launch can have, where larger ones fit
   const double wide = a.wide, weights = used_groups(a) * wide, rounds = tiles_down(a, 128u) * blocks_for(a.wide, 128u) / 256.0;
   const double few = fmax(tiles_down(a, 16u) * wide * (M == kWidened ? 2.3e-5 : 2.0e-5), weights * 1.9e-5);   // 1.9e-5: 6.7 TB/s
   const double tiles = fmax(fmax(rounds, 1.0) * (M == kWidened ? 0.7 : 0.4), weights * 2.4e-5);

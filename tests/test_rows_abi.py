@@ -312,6 +312,11 @@ def product_kernels(rt):
     assert rt.launches[-1][1:3] == ((512 // 128 + 1) * 16 + 8, 512)      # a group's tiles together: an XCD's eighth may be one more
     assert rt.lib.uccl_group_product(rows(500, 700), rows(500, 2048), None, rows(5600, 2048), M, 8, None) == OK
     assert rt.launches[-1][1:3] == (3 * 6 + 6 + 8 * 6, 512)              # full tiles and those that groups end in, by eights
+    # narrow outputs of very many rows go by 16 rows while that fits a launch, and by tiles where these do
+    for n, kernel in ((1 << 26, "few_kernel"), ((1 << 29) - 1024, "tile_kernel")):
+        rt.symbols.clear()
+        assert rt.lib.uccl_group_product(rows(n, 5), rows(n, 500), None, rows(5, 500), M, 1, None) == OK
+        assert kernel in rt.symbols[0]
     rt.launches.clear()
     big = (1 << 31) - 1
     assert rt.lib.uccl_group_product(rows(big, 8 << 20), rows(big, 64), None, rows(8 << 20, 64), M, 1, None) == pkg.UCCL_ETOOBIG
