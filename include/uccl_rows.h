@@ -96,10 +96,7 @@ uint64_t uccl_norm_rows_scratch(uint32_t rows, uint32_t cols);
  *   w        read: n_groups * n rows of k columns, x's type; the n rows of a group follow each other
  *   offsets  read: n_groups + 1 int32, 4-byte aligned, in ascending order; one that is below its predecessor counts as
  *            that, below 0 as 0, above the rows of y as these
- * Sums are held in binary32 and rounded once; 8-bit operands are multiplied as they are and the sum by both scales.  Their
- * products are exact but where y is 16 bits wide, k at least 512 and the call large enough for the matrix instruction for 8 bits:
- * that adds 64 products at a time and drops of each what is below about 2^-13 of the greatest of them, which is far below what
- * rounding y to 16 bits drops.
+ * Sums are held in binary32 and rounded once; 8-bit operands are multiplied as they are, exactly, and the sum by both scales.
  * What a call is cut into depends on its sizes alone, never on the offsets' values.
  */
 int uccl_group_product(const uccl_rows* y, const uccl_rows* x, const int32_t* index, const uccl_rows* w,

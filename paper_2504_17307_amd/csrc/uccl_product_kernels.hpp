@@ -271,38 +271,15 @@ __device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row,
     if (r < rows && c < cols) store_piece<false>(a.out.data + (row + r) * a.out.stride, c / 8u, __builtin_bit_cast(Piece<uint16_t>, p), cols - c);
   }
 }
-__device__ __forceinline__ void store_blocks(const ProductArgs& a, uint64_t row, bool there, uint32_t first, uint32_t cols, f32x16 v) {
-  // one block of 32 x 32: a lane has of row lane % 32 (`there`: it is stored) columns i / 4 * 8 + lane / 32 * 4 + i % 4
-  char* at = a.out.data + row * a.out.stride;
-  const uint32_t half = threadIdx.x % 64u / 32u;
-  if (a.out_type == kOutF32) {
-#pragma unroll
-    for (uint32_t i = 0; i < 4u; ++i) {
-      const uint32_t c = first + i * 8u + half * 4u;
-      if (there && c < cols) store_piece<false>(at, c / 4u, Piece<float>{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]}, cols - c);
-    }
-    return;
-  }
-  uint32_t w[8];
-#pragma unroll
-  for (uint32_t i = 0; i < 8u; ++i)
-    w[i] = a.out_type == kOutBf16 ? narrow_pair<__bf16>(v[2 * i], v[2 * i + 1]) : narrow_pair<_Float16>(v[2 * i], v[2 * i + 1]);
-#pragma unroll
-  for (uint32_t i = 0; i < 8u; i += 4u) {
-    const u32x2 s0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(w[i], w[i + 2], false, false));
-    const u32x2 s1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(w[i + 1], w[i + 3], false, false));
-    const uint32_t c = first + i * 4u + half * 8u;
-    const Piece<uint16_t> p = __builtin_bit_cast(Piece<uint16_t>, u32x4{s0.x, s1.x, s0.y, s1.y});
-    if (there && c < cols) store_piece<false>(at, c / 8u, p, cols - c);
-  }
-}
 
 // ---- tiles through the LDS --------------------------------------------------------------------------
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-enum Arithmetic : uint32_t { kBf16, kF16, kWidened, kNative8 };   // kWidened: 8-bit operands as bf16
+// kWidened: 8-bit operands as bf16, whose products are exact and are added as those of 16 bits are; kWidenedLarge: the same in tiles of 256 columns.
+// (The instructions for 8-bit operands add 8 products at a time and drop of each what is below 2^-13 of the greatest of the 8, those for 16 bits what is
+// below 2^-24, a binary32's last place: beside 448 x 448 and its opposite, all that 8-bit instructions keep of 6 products below 24 is 0.)
+enum Arithmetic : uint32_t { kBf16, kF16, kWidened, kWidenedLarge };
 
 // A stage is 128 bytes along the sum: 64 steps of 16 bits or 128 of 8.  It is multiplied in two halves.  Rows are loaded 128 bytes at
 // a time: the L2 takes a request for 64 bytes as long as one for 128.
@@ -356,16 +333,14 @@ struct Operand {
     const uint32_t slot = threadIdx.x % PITCH, r = row(i);
     return ALONG ? slot ^ (r >> 1 & 7u) : slot ^ (turn(r) << 1);
   }
-  // The lane's part of half a stage for the SIDE16 (16 or 32) rows / columns from `first`, a multiple of 16, on: 16 bytes of one row of
-  // 16, a quarter of the wavefront the first 16 bytes, and so on; or of one row of 32, the j-th 32 bytes in halves
-  template <uint32_t SIDE16>
-  static __device__ __forceinline__ u32x4 fragment(const char* stage, uint32_t first, uint32_t half, uint32_t j) {
+  // The lane's part of half a stage for the 16 rows / columns from `first`, a multiple of 16, on: 16 bytes of one row, a quarter of the
+  // wavefront the first 16 bytes, and so on
+  static __device__ __forceinline__ u32x4 fragment(const char* stage, uint32_t first, uint32_t half) {
     const uint32_t lane = threadIdx.x & 63u;
     if constexpr (ALONG) {
-      const uint32_t r = lane % SIDE16, p = half * 4u + (SIDE16 == 16u ? lane / 16u : j * 2u + lane / 32u);
+      const uint32_t r = lane % 16u, p = half * 4u + lane / 16u;
       return *reinterpret_cast<const u32x4*>(stage + first * kStageBytes + (r * kStageBytes + ((p ^ (r >> 1 & 7u)) << 4)));
     } else {
-      static_assert(SIDE16 == 16u);
       // 16 lanes bring a block of 4 steps x 16 columns and get it transposed: a lane its column's 4 steps
       const uint32_t step = lane / 16u * 8u + lane % 16u / 4u;
       stage += half * 32u * PITCH * 16u + lane % 4u * 8u;
@@ -379,14 +354,6 @@ struct Operand {
   }
 };
 
-// What a wavefront multiplies at a time: 16 rows x 64 bytes, or 32 x 64 for the matrix instruction for 8 bits.
-template <Arithmetic M, class O>
-__device__ __forceinline__ auto fragment_of(const char* stage, uint32_t first, uint32_t half) {
-  if constexpr (M == kNative8)
-    return __builtin_bit_cast(i32x8, __builtin_shufflevector(O::template fragment<32>(stage, first, half, 0), O::template fragment<32>(stage, first, half, 1), 0, 1, 2, 3, 4, 5, 6, 7));
-  else return O::template fragment<16>(stage, first, half, 0);
-}
-
 // A workgroup computes BM x BN of the output, WR x WC wavefronts a part each.  While the matrix cores work on half a stage, the
 // next half's fragments are read from the LDS and loads straight into the LDS bring later stages, one between every few of a
 // wavefront's multiplications: loads that are issued together hold up what comes after them.  The LDS holds AHEAD + 1 stages of one
@@ -397,13 +364,12 @@ __device__ __forceinline__ auto fragment_of(const char* stage, uint32_t first, u
 // 8192^3 in bf16 864 us, 1.27 PFLOP/s (the library's product on that box 766); 8190 rows in 16 groups, 2048 -> 7168, 267 us.
 template <Arithmetic M, Product P, uint32_t BM, uint32_t BN, uint32_t WR, uint32_t WC, uint32_t AHEAD>
 __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs a) {
-  constexpr uint32_t THREADS = WR * WC * 64u, E = M == kWidened || M == kNative8 ? 1u : 2u, DEEP = kStageBytes / E;
-  constexpr uint32_t SIDE = M == kNative8 ? 32u : 16u, NA = BM / WR / SIDE, NB = BN / WC / SIDE;
+  constexpr uint32_t THREADS = WR * WC * 64u, E = M == kWidened || M == kWidenedLarge ? 1u : 2u, DEEP = kStageBytes / E;
+  constexpr uint32_t SIDE = 16u, NA = BM / WR / SIDE, NB = BN / WC / SIDE;
   constexpr bool A_ALONG = P != kGradW, B_ALONG = P == kForward;
   using A = Operand<A_ALONG, BM, THREADS>;
   using B = Operand<B_ALONG, BN, THREADS>;
   constexpr uint32_t A_STAGE = BM * kStageBytes, B_STAGE = BN * kStageBytes;
-  using Block = std::conditional_t<M == kNative8, f32x16, f32x4>;
   __shared__ __align__(1024) char lds_a[(AHEAD + 1u) * A_STAGE], lds_b[AHEAD * B_STAGE];
   const char* zeros = reinterpret_cast<const char*>(page_of_zeros);
   asm volatile("" : "+s"(zeros));   // an address in registers: not looked up again at every load
@@ -515,9 +481,8 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
   const uint32_t ra = wave / WC * (BM / WR), cb = wave % WC * (BN / WC);
   // Blocks of rows that the wavefront has in this tile, at most NA: the others are not multiplied
   const uint32_t high = __builtin_amdgcn_readfirstlane(r0 + ra < out_rows ? min((out_rows - r0 - ra + SIDE - 1u) / SIDE, NA) : 0u);
-  Block acc[NB][NA] = {};
-  using Fragment = decltype(fragment_of<M, A>(lds_a, 0, 0));
-  Fragment fa[NA], fb[2][NB];
+  f32x4 acc[NB][NA] = {};
+  u32x4 fa[NA], fb[2][NB];
   uint32_t a_slot = 0, b_slot = 0;   // stage k's, bytes
   auto after = [](uint32_t slot, uint32_t by, uint32_t end) { return slot + by >= end ? slot + by - end : slot + by; };
   // Half a stage, whose fragments are fa and fb[HALF]: multiply, and read the next half's.  `load(i)` asks for a load of a later stage,
@@ -525,11 +490,11 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
   auto multiply_half = [&](auto half, const char* next_a, const char* next_b, auto count, auto from, auto&& load) {
     constexpr uint32_t HALF = decltype(half)::value, COUNT = decltype(count)::value, FROM = decltype(from)::value;
 #pragma unroll
-    for (uint32_t n = 0; n < NB; ++n) fb[HALF ^ 1u][n] = fragment_of<M, B>(next_b, cb + n * SIDE, HALF ^ 1u);
+    for (uint32_t n = 0; n < NB; ++n) fb[HALF ^ 1u][n] = B::fragment(next_b, cb + n * SIDE, HALF ^ 1u);
 #pragma unroll
     for (uint32_t m = 0; m < NA; ++m) {
       if (m >= high) {
-      } else if constexpr (M == kWidened) {
+      } else if constexpr (E == 1u) {
         const Widened x = widen_e4m3(fa[m]);
 #pragma unroll
         for (uint32_t n = 0; n < NB; ++n) {
@@ -539,13 +504,10 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
         }
       } else {
 #pragma unroll
-        for (uint32_t n = 0; n < NB; ++n) {
-          if constexpr (M == kNative8) acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[HALF][n], fa[m], acc[n][m], 0, 0, 0, 0, 0, 0);
-          else acc[n][m] = multiply<M>(fb[HALF][n], fa[m], acc[n][m]);
-        }
+        for (uint32_t n = 0; n < NB; ++n) acc[n][m] = multiply<M>(fb[HALF][n], fa[m], acc[n][m]);
       }
       __builtin_amdgcn_sched_barrier(0);   // the next fragment takes the registers of this one
-      fa[m] = fragment_of<M, A>(next_a, ra + m * SIDE, HALF ^ 1u);
+      fa[m] = A::fragment(next_a, ra + m * SIDE, HALF ^ 1u);
       if constexpr (FROM != 0u)
         if (m + 1u == FROM) load(COUNT);   // the wait that lets the loads begin
       if (m >= FROM)
@@ -592,9 +554,9 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
     else wait_for_loads<0>();
     if (ragged && steps == 1u) trim(lds_a, lds_b);
 #pragma unroll
-    for (uint32_t n = 0; n < NB; ++n) fb[0][n] = fragment_of<M, B>(lds_b, cb + n * SIDE, 0);
+    for (uint32_t n = 0; n < NB; ++n) fb[0][n] = B::fragment(lds_b, cb + n * SIDE, 0);
 #pragma unroll
-    for (uint32_t m = 0; m < NA; ++m) fa[m] = fragment_of<M, A>(lds_a, ra + m * SIDE, 0);
+    for (uint32_t m = 0; m < NA; ++m) fa[m] = A::fragment(lds_a, ra + m * SIDE, 0);
     uint32_t k = 0;
     for (; k + AHEAD + 1u < steps; ++k) work(k, std::true_type{});
     for (; k < steps; ++k) work(k, std::false_type{});
@@ -603,10 +565,8 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
 #pragma unroll
   for (uint32_t m = 0; m < NA; ++m) {
     const uint32_t r = r0 + ra + m * SIDE + lane % SIDE;   // this lane's row of the output
-    const bool there = r < out_rows;
-    const uint64_t row = P == kGradW ? w0 + r : r;
     float sx = 1.0f;
-    if (E == 1u && there) {
+    if (E == 1u && r < out_rows) {
       const uint32_t from = a.index == nullptr ? r : static_cast<uint32_t>(a.index[r]);
       if (from < a.indexed_rows) sx = *reinterpret_cast<const float*>(a.a.scales + from * a.a.scale_stride);
     }
@@ -614,32 +574,21 @@ __global__ __launch_bounds__(WR * WC * 64) void product_tile_kernel(ProductArgs 
       if constexpr (E == 1u) return v * sx * *reinterpret_cast<const float*>(a.b.scales + (w0 + min(c, out_cols - 1u)) * a.b.scale_stride);
       else return v;
     };
-    if constexpr (SIDE == 32u) {
+    constexpr uint32_t BLOCKS = NB % 4u == 0u ? 4u : 2u;
+    const uint32_t top = r0 + ra + m * SIDE;   // of the 16 rows that the wavefront has
+    const uint32_t rows = top < out_rows ? out_rows - top : 0u;
 #pragma unroll
-      for (uint32_t n = 0; n < NB; ++n) {
-        const uint32_t first = c0 + cb + n * 32u;
-        f32x16 v = acc[n][m];
+    for (uint32_t n = 0; n < NB; n += BLOCKS) {
+      const uint32_t first = c0 + cb + n * SIDE;
+      f32x4 v[BLOCKS];
 #pragma unroll
-        for (uint32_t i = 0; i < 16u; ++i) v[i] = scaled(v[i], first + i / 4u * 8u + lane / 32u * 4u + i % 4u);
-        store_blocks(a, row, there, first, out_cols, v);
+      for (uint32_t b = 0; b < BLOCKS; ++b) {
+        v[b] = acc[n + b][m];
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; ++i) v[b][i] = scaled(v[b][i], first + b * SIDE + lane / 16u * 4u + i);
       }
-    } else {
-      constexpr uint32_t BLOCKS = NB % 4u == 0u ? 4u : 2u;
-      const uint32_t top = r0 + ra + m * 16u;   // of the 16 rows that the wavefront has
-      const uint32_t rows = top < out_rows ? out_rows - top : 0u;
-#pragma unroll
-      for (uint32_t n = 0; n < NB; n += BLOCKS) {
-        const uint32_t first = c0 + cb + n * 16u;
-        f32x4 v[BLOCKS];
-#pragma unroll
-        for (uint32_t b = 0; b < BLOCKS; ++b) {
-          v[b] = acc[n + b][m];
-#pragma unroll
-          for (uint32_t i = 0; i < 4u; ++i) v[b][i] = scaled(v[b][i], first + b * 16u + lane / 16u * 4u + i);
-        }
-        // a launch of tiles of 256 x 256 writes more than the L2s keep
-        store_blocks<BM == 256u>(a, P == kGradW ? w0 + top : top, rows, first, out_cols, v);
-      }
+      // a launch of tiles of 256 x 256 writes more than the L2s keep
+      store_blocks<BM == 256u>(a, P == kGradW ? w0 + top : top, rows, first, out_cols, v);
     }
   }
 }
