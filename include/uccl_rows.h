@@ -53,7 +53,7 @@ typedef struct uccl_rows {
  * uccl_norm_rows -- h = x + r;  s = 1 / sqrt(mean of h^2 over the row + eps);  y = h s w.
  *
  *   y        written: x's type, or UCCL_E4M3: the row's scale is max |y| / 448 (at least 2^-126) and its elements are
- *            y / scale, rounded to nearest even
+ *            y / scale, a binary32 quotient, rounded to nearest even
  *   h        written: the sum in x's type, the next residual; NULL = not wanted.  May be x or r itself
  *   rstd     written: s, one float a row, 4-byte aligned; NULL = not wanted
  *   x, r     read: UCCL_F32, UCCL_BF16 or UCCL_F16, the same; r NULL = no residual

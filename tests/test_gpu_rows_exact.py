@@ -50,3 +50,48 @@ def test_small_terms_beside_large_ones_that_cancel(uccl, shape, dtype, out):
         want = ex[index[at:at + c].long()] @ ew[e * n:(e + 1) * n].T
         assert torch.equal(y[at:at + c], want.to(T[out])), f"group {e}: off by up to {float((y[at:at + c].double() - want).abs().max())}"
         at += c
+
+
+def elements(y, scales):
+    """The e4m3 elements of binary32 rows: their binary32 quotients by the scales (a quotient in 64 bits rounds to those), to nearest even."""
+    return (y.double() / scales.double()).float().to(E8).view(torch.uint8)
+
+
+# columns that take one piece a thread, one wavefront; several; two and four pieces; rows of any length
+@pytest.mark.parametrize("cols", [256, 1024, 2048, 4096, 8192, 32768])
+@pytest.mark.parametrize("rows", [2, 520])
+def test_8_bit_outputs_are_the_quotients_by_the_scale(uccl, rows, cols):
+    """Ones have a mean square of one, and eps 0 leaves them so: y is the weight.  It holds products of a scale of few bits with the ties between e4m3 values and their
+    neighbours in binary32; the greatest, 448 times the scale, is among them."""
+    vals = torch.arange(0, 127, dtype=torch.uint8).view(E8).double()
+    ties = (vals[1:] + vals[:-1]) / 2
+    r = np.random.default_rng(cols)
+    x = aligned(rows, cols, torch.float32)
+    x.fill_(1.0)
+    y, s, rstd = aligned(rows, cols, E8), torch.zeros(rows, 1, device="cuda"), torch.zeros(rows, device="cuda")
+    for power in (0, -20, -63, -117, 100):
+        for _ in range(8):
+            scale = float(np.ldexp(r.integers(2 ** 18, 2 ** 19) | 1, power - 18))
+            v = (ties * scale).float()                       # 4 bits and 19: exact
+            v = torch.cat([v, (vals * scale).float(), torch.nextafter(v, torch.tensor(torch.inf)), torch.nextafter(v, torch.tensor(0.0))])
+            v = v[torch.from_numpy(r.integers(0, len(v), cols))] * torch.from_numpy(r.choice([-1.0, 1.0], cols)).float()
+            v[int(r.integers(0, cols))] = 448 * scale
+            w = v.cuda()
+            uccl.uccl_norm_rows(y, x, w, 0.0, rstd=rstd, scales=s)
+            assert bool((rstd == 1.0).all()) and bool((s == scale).all())
+            assert torch.equal(y.view(torch.uint8), elements(w.expand(rows, cols), s)), (power, scale)
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("rows,cols", [(3000, 2043), (1000, 7168), (40, 20000)])
+def test_8_bit_outputs_of_many_rows_are_the_quotients(uccl, dtype, rows, cols):
+    """y from the call's own 1 / root, with the kernel's two roundings."""
+    g, t = gen(cols), T[dtype]
+    x, w = aligned(rows, cols, t), aligned(1, cols, t)[0]
+    x.copy_(torch.randn(rows, cols, device="cuda", generator=g))
+    w.copy_(torch.randn(cols, device="cuda", generator=g))
+    y, s, rstd = aligned(rows, cols, E8), torch.zeros(rows, 1, device="cuda"), torch.zeros(rows, device="cuda")
+    uccl.uccl_norm_rows(y, x, w, 1e-6, rstd=rstd, scales=s)
+    e = x.float() * rstd[:, None] * w.float()
+    assert torch.equal(s, (e.abs().amax(1, keepdim=True).double() / 448.0).float())
+    assert torch.equal(y.view(torch.uint8), elements(e, s))
