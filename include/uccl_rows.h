@@ -16,7 +16,7 @@
  * match; UCCL_EALIGN; UCCL_ETOOBIG: more workgroups than one launch can have (2^32 threads: 2^22 - 1 rows of a norm, and fewer than 2^22 tiles
  * of 128 x 128 elements of a product always fit; split the call); UCCL_ELAUNCH: HIP's, the text in uccl_last_error_detail().  Nothing has
  * been enqueued then, but for uccl_norm_rows_grad: two launches, of which HIP may take the first and refuse the second.
- * uccl_time_next_launch times these calls too.
+ * uccl_time_next_launch times these calls too; uccl_norm_rows_grad has its start on the first of its launches and its stop on the last.
  *
  * The operators are no passage of the paper, which moves such rows and leaves the work on them to the application
  * (its evaluation has expert-parallel prefill and decode among the applications).

@@ -960,6 +960,8 @@ int feed_flush(uccl_feed* f) {
 
 int uccl_internal_failed(hipError_t e) { return launch_failed(e); }
 
+void* uccl_internal_stop_event() { return t_stop; }
+
 int uccl_internal_launch(const void* kernel, dim3 grid, dim3 block, hipStream_t s, void** args) {
   const hipEvent_t t0 = t_start, t1 = t_stop;
   t_start = t_stop = nullptr;

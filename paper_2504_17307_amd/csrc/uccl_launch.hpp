@@ -10,6 +10,8 @@
 // Enqueue a kernel and return UCCL_OK or UCCL_ELAUNCH, whose text uccl_last_error_detail() then has; takes the
 // calling thread's one-shot timing events (uccl_chunk.hip).
 __attribute__((visibility("hidden"))) int uccl_internal_launch(const void* kernel, dim3 grid, dim3 block, hipStream_t s, void** args);
+// The stop event that the calling thread's next launch would take: a call of several launches gives it (uccl_time_next_launch) to the last one too.
+__attribute__((visibility("hidden"))) void* uccl_internal_stop_event();
 // Load the code object of the row operators on the current device (uccl_rows.hip).
 __attribute__((visibility("hidden"))) int uccl_internal_load_rows();
 // The same for a HIP error that another call returned.

@@ -273,11 +273,13 @@ int uccl_norm_rows_grad(const uccl_rows* dx, float* dweight, const uccl_rows* dy
     if (rstd == nullptr || weight == nullptr || scratch == nullptr || scratch_bytes < uccl_norm_rows_scratch(h->rows, h->cols)) return UCCL_EINVAL;
     if (misaligned(weight, 16) || misaligned(rstd, 4) || misaligned(scratch, 16)) return UCCL_EALIGN;
     const NormGradArgs a{rows_of(dx), rows_of(dy), rows_of(h), rows_of(dh), static_cast<const char*>(weight), rstd, static_cast<float*>(scratch), h->rows, h->cols};
+    void* const stop = uccl_internal_stop_event();   // the first launch has it as well: one that HIP does not take is refused there
     e = with_type(h->dtype, [&](auto t) {
       using T = decltype(t);
       return too_large_to_keep(dx) ? norm_grad<T, true>(a, groups, s) : norm_grad<T, false>(a, groups, s);
     });
     if (e != UCCL_OK) return e;
+    (void)uccl_time_next_launch(nullptr, stop);
   }
   return launch(column_sum_kernel, sums, 1024, s, dweight, static_cast<const float*>(scratch), groups, h->cols);
 }
