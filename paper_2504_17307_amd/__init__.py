@@ -170,6 +170,14 @@ def _find_current_stream():
 _current_stream = None
 
 
+def _forget_stream():
+    global _current_stream
+    _current_stream = None
+
+
+os.register_at_fork(after_in_child=_forget_stream)   # torch refuses the GPU to a child of a process that uses it, if it is asked
+
+
 def _stream(s):
     global _current_stream
     if s is None:
