@@ -38,7 +38,8 @@ extern "C" {
  * next) a multiple of 16; `cols` may be any number of elements.  The 16-byte piece that holds a row's last element may be
  * read whole, past the row's end; nothing past the end is written, and what is there never changes a result.  8-bit rows
  * have their scales at scales + i * scale_stride, 4-byte aligned, scale_stride a multiple of 4: side by side with the values
- * they make a row that is dispatched as one piece.  A matrix of one row, or of none, may have any stride. */
+ * they make a row that is dispatched as one piece; 0 is one scale for all rows, where rows are read.  A matrix of one row, or of
+ * none, may have any stride. */
 typedef struct uccl_rows {
   void* data;
   uint64_t stride;

@@ -235,7 +235,7 @@ int uccl_norm_rows(const uccl_rows* y, const uccl_rows* h, float* rstd, const uc
   if (e == UCCL_OK && r != nullptr) e = check(r);
   if (e != UCCL_OK) return e;
   if (x->rows == 0u || x->cols == 0u) return UCCL_OK;
-  if (weight == nullptr) return UCCL_EINVAL;
+  if (weight == nullptr || (y->dtype == UCCL_E4M3 && y->rows > 1u && y->scale_stride == 0u)) return UCCL_EINVAL;   // every row writes its own scale
   if (misaligned(weight, 16) || misaligned(rstd, 4)) return UCCL_EALIGN;
   const float shrink = ldexpf(1.0f, -ilogbf(static_cast<float>(x->cols)) / 2);
   const NormArgs a{rows_of(y), rows_of(h), rows_of(x), rows_of(r), static_cast<const char*>(weight), rstd, x->rows, x->cols, opts->eps, shrink,
