@@ -57,6 +57,50 @@ def test_timing_events_span_a_call_of_two_launches(tmp_path):
     in_process("timing_events", tmp_path)
 
 
+TYPE = {F32: "IfL", BF16: "IDF16bL", F16: "IDF16_L"}
+
+
+def kernels(rt):
+    """The shapes of tests/test_gpu_rows_large.py, and what they are there for."""
+    lib = rt.lib
+    for dtype, n, cols, shape, once in (
+        (BF16, 1, 7168, "1024ELj1", 0), (BF16, 512, 7168, "1024ELj1", 0), (BF16, 513, 7168, "512ELj2", 0), (BF16, 600, 7168, "512ELj2", 0), (BF16, 2500, 7168, "512ELj2", 1),
+        (F16, 2500, 7171, "512ELj2", 1), (BF16, 4096, 7168, "512ELj2", 1), (BF16, 2340, 7168, "512ELj2", 0), (BF16, 2341, 7168, "512ELj2", 1), (BF16, 40000, 500, "64ELj1", 1),
+        (BF16, 9000, 2043, "256ELj1", 1), (BF16, 4500, 4093, "512ELj1", 1), (BF16, 1100, 16381, "512ELj4", 1), (F32, 600, 4093, "512ELj2", 0), (F32, 2100, 4093, "512ELj2", 1),
+        (F32, 1300, 7168, "512ELj4", 1), (F32, 40000, 250, "64ELj1", 1), (F32, 9000, 1021, "256ELj1", 1), (F32, 4500, 2043, "512ELj1", 1), (F32, 3, 9000, None, 0), (BF16, 3, 16385, None, 0),
+    ):
+        for out, e8 in ((rows(n, cols, dtype), 0), (q8(n, cols), 1)):
+            rt.symbols.clear()
+            x = rows(n, cols, dtype)
+            assert lib.uccl_norm_rows(out, x, None, x, None, B, EPS, None) == OK
+            t = TYPE[dtype][:-1]
+            want = f"norm_long_kernel{t}Lb{e8}E" if shape is None else f"norm_kernel{t}Lb{e8}ELj{shape}ELb{once}E"
+            assert len(rt.symbols) == 1 and want in rt.symbols[0], (want, rt.symbols)
+    # an output in 8 bits is a half or a quarter of h, which may be there or not
+    for n, once in ((4681, 0), (4682, 1)):
+        rt.symbols.clear()
+        assert lib.uccl_norm_rows(q8(n, 7168), None, None, rows(n, 7168), None, B, EPS, None) == OK and f"norm_kernelIDF16bLb1ELj512ELj2ELb{once}E" in rt.symbols[0]
+    for dtype, n, cols, shape, once in (
+        (BF16, 2, 255, "256ELj1", 0), (BF16, 9000, 2043, "256ELj1", 1), (BF16, 4500, 4093, "512ELj1", 1), (BF16, 600, 7168, "1024ELj1", 0), (BF16, 2500, 7168, "1024ELj1", 1), (F16, 2500, 7171, "1024ELj1", 1),
+        (BF16, 530, 8208, "512ELj4", 0), (BF16, 1100, 16381, "512ELj4", 1), (F32, 600, 4093, "1024ELj1", 0), (F32, 2100, 4093, "1024ELj1", 1), (F32, 1300, 7168, "512ELj4", 1), (F32, 1100, 8188, "512ELj4", 1),
+        (F32, 9000, 1021, "256ELj1", 1), (F32, 4500, 2043, "512ELj1", 1), (F32, 300, 9000, None, 0), (BF16, 300, 20000, None, 0),
+    ):
+        rt.symbols.clear(), rt.launches.clear()
+        assert norm_grad(rt, n, cols, dtype, dh=True) == OK
+        want = f"norm_grad_long_kernel{TYPE[dtype][:-1]}E" if shape is None else f"norm_grad_kernel{TYPE[dtype]}j{shape}ELb{once}E"
+        assert want in rt.symbols[0] and "column_sum_kernel" in rt.symbols[1] and rt.launches[0][1] == min(n, 256), (want, rt.symbols)
+    for dtype, tokens, slots, cols, once, once_grad in ((BF16, 2500, 2, 7168, 1, 1), (F16, 2500, 3, 7171, 1, 1), (BF16, 700, 9, 7171, 0, 1), (F32, 1300, 2, 7168, 1, 1), (F32, 400, 9, 7171, 0, 1), (BF16, 70, 4, 20, 0, 0)):
+        rt.symbols.clear()
+        y = rows(tokens * slots * 7 // 8, cols, dtype)
+        assert lib.uccl_combine_rows(rows(tokens, cols, dtype), y, M, D, slots, None, None) == OK
+        assert lib.uccl_combine_rows_grad(y, D, rows(tokens, cols, dtype), y, M, D, slots, None) == OK
+        assert f"combine_kernel{TYPE[dtype]}j128ELb{once}E" in rt.symbols[0] and f"combine_grad_kernel{TYPE[dtype]}b{once_grad}E" in rt.symbols[1], rt.symbols
+
+
+def test_which_kernel_a_row_operator_is_launched_as(tmp_path):
+    in_process("kernels", tmp_path)
+
+
 if __name__ == "__main__":
     import test_host_launches
     runtime = test_host_launches.Runtime(sys.argv[2])
