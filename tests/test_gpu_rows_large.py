@@ -1,9 +1,9 @@
-"""Row operators at the sizes that take the kernels of large calls: many rows, outputs above 32 MiB that are stored past the caches and outputs that lie
-where an input does.  tests/test_rows_launches.py has which kernel each of these shapes is launched as; tolerances are those of tests/test_gpu_rows.py."""
+"""Row operators at the sizes that take the kernels of large calls: many rows, outputs above 32 MiB that are stored past the caches, more than 64 groups in the order by group,
+and outputs that lie where an input does.  tests/test_rows_launches.py has which kernel each of these shapes is launched as; tolerances are those of tests/test_gpu_rows.py."""
 import pytest
 import torch
 
-from test_gpu_rows import E8, T, aligned, close, gen, margin, norm_reference, normal
+from test_gpu_rows import E8, T, aligned, close, gen, in_pieces, margin, norm_reference, normal, offsets_of, product_inputs
 from test_gpu_rows_exact import elements
 
 pytestmark = pytest.mark.gpu
@@ -116,3 +116,41 @@ def test_combine_of_many_rows_and_onto_the_residual(uccl, dtype, tokens, slots, 
         close(dy[pos[m, j].long()], e, e.abs(), 1, "dy")
     close(dw, torch.stack(dots, 1), torch.stack(dot_mag, 1), cols, "dweights")
     assert torch.equal(margin(dy), around)
+
+
+# more than 64 and more than 128 groups, all of a group's tiles together: rows by group, columns, depth; by 16 rows, and by tiles
+MANY_GROUPS = {"few rows": ([(5 * i) % 17 for i in range(150)], 1280, 72), "tiles": ([(29 * i) % 81 for i in range(70)], 14336, 40)}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("shape", list(MANY_GROUPS))
+def test_more_than_64_groups_by_group(uccl, shape, dtype):
+    counts, n, k = MANY_GROUPS[shape]
+    g, rows, groups, t = gen(n), sum(counts), len(counts), torch.bfloat16
+    x, xs, w, ws, ex, ew = product_inputs(g, dtype, rows, k, n, groups, 0)
+    index = torch.randperm(rows, device="cuda", generator=g).to(torch.int32)
+    y = aligned(rows, n, t, 1, fill=7.0)
+    around = margin(y)
+    uccl.uccl_group_product(y, x, w, offsets_of(counts), index=index, x_scales=xs, w_scales=ws)
+    at = 0
+    for e, c in enumerate(counts):
+        a = ex[index[at:at + c].long()]
+        in_pieces(lambda s: close(y[at:at + c, s], a @ ew[e, s].T, a.abs() @ ew[e, s].abs().T, k + 4, f"group {e}"), n, 4096)
+        at += c
+    assert torch.equal(margin(y), around)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_gradient_of_the_rows_of_more_than_64_groups_by_group(uccl, dtype):
+    counts, k, n = MANY_GROUPS["tiles"]
+    g, rows, groups, t = gen(n), sum(counts), len(counts), T[dtype]
+    dy, w = normal(g, rows, n, t), normal(g, groups * n, k, t)
+    dx = aligned(rows, k, t, 1, fill=7.0)
+    around = margin(dx)
+    uccl.uccl_group_product_grad_x(dx, dy, w.unflatten(0, (groups, n)), offsets_of(counts))
+    at = 0
+    for e, c in enumerate(counts):
+        d, v = dy[at:at + c].double(), w[e * n:(e + 1) * n].double()
+        close(dx[at:at + c], d @ v, d.abs() @ v.abs(), n + 4, f"dx, group {e}")
+        at += c
+    assert torch.equal(margin(dx), around)

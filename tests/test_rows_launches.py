@@ -57,6 +57,22 @@ def test_timing_events_span_a_call_of_two_launches(tmp_path):
     in_process("timing_events", tmp_path)
 
 
+class Seen:
+    """The stub's runtime, which also notes of every product whether it is launched with a group's tiles together."""
+
+    def __init__(self, rt):
+        self.rt, self.together, self.product = rt, [], None
+        self.was = rt._launch
+        on_launch = C.CFUNCTYPE(C.c_int, C.c_char_p, C.c_uint, C.c_uint, C.c_uint, C.c_void_p, C.POINTER(C.c_void_p), C.c_void_p, C.c_void_p)
+        self.keep = on_launch(self._launch)
+        rt.stub.stub_callbacks(self.keep, rt.keep[1])
+
+    def _launch(self, kernel, grid, block, lds, stream, args, start, stop):
+        if b"product_" in kernel:   # ProductArgs: three matrices of 32 bytes, two pointers, six numbers
+            self.together.append(C.cast(args[0] + 136, C.POINTER(C.c_uint32))[0])
+        return self.was(kernel, grid, block, lds, stream, args, start, stop)
+
+
 TYPE = {F32: "IfL", BF16: "IDF16bL", F16: "IDF16_L"}
 
 
@@ -95,6 +111,19 @@ def kernels(rt):
         assert lib.uccl_combine_rows(rows(tokens, cols, dtype), y, M, D, slots, None, None) == OK
         assert lib.uccl_combine_rows_grad(y, D, rows(tokens, cols, dtype), y, M, D, slots, None) == OK
         assert f"combine_kernel{TYPE[dtype]}j128ELb{once}E" in rt.symbols[0] and f"combine_grad_kernel{TYPE[dtype]}b{once_grad}E" in rt.symbols[1], rt.symbols
+    # more than 64 groups, together
+    seen = Seen(rt)
+    few, tiles = sum((5 * i) % 17 for i in range(150)), sum((29 * i) % 81 for i in range(70))
+    for dtype in (BF16, E4M3):
+        make = (lambda n, c: q8(n, c)) if dtype == E4M3 else (lambda n, c: rows(n, c, dtype))
+        rt.symbols.clear(), seen.together.clear()
+        assert lib.uccl_group_product(rows(few, 1280), make(few, 72), M, make(150 * 1280, 72), M, 150, None) == OK
+        assert lib.uccl_group_product(rows(tiles, 14336), make(tiles, 40), M, make(70 * 14336, 40), M, 70, None) == OK
+        assert "few_kernel" in rt.symbols[0] and "tile_kernel" in rt.symbols[1] and seen.together == [1, 1], (rt.symbols, seen.together)
+    rt.symbols.clear(), seen.together.clear()
+    assert lib.uccl_group_product_grad_x(rows(tiles, 14336), rows(tiles, 40), rows(70 * 40, 14336), M, 70, None) == OK
+    assert "tile_kernel" in rt.symbols[0] and seen.together == [1]
+    assert lib.uccl_group_product(rows(2743, 777), rows(2743, 40), None, rows(67 * 777, 40), M, 67, None) == OK and seen.together == [1, 0]
 
 
 def test_which_kernel_a_row_operator_is_launched_as(tmp_path):
