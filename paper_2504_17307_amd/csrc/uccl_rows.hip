@@ -80,7 +80,7 @@ int norm(const NormArgs& a, hipStream_t s) {
   if (pieces <= 256u) return launch(norm_kernel<T, E8, 256, 1, ONCE>, a.rows, 256, s, a);
   if (pieces <= 512u) return launch(norm_kernel<T, E8, 512, 1, ONCE>, a.rows, 512, s, a);
   if (pieces <= 1024u && a.rows > 512u) return launch(norm_kernel<T, E8, 512, 2, ONCE>, a.rows, 512, s, a);
-  if (pieces <= 1024u) return launch(norm_kernel<T, E8, 1024, 1, ONCE>, a.rows, 1024, s, a);
+  if (pieces <= 1024u) return launch(norm_kernel<T, E8, 1024, 1, false>, a.rows, 1024, s, a);   // 8 MiB at most
   if (pieces <= 2048u) return launch(norm_kernel<T, E8, 512, 4, ONCE>, a.rows, 512, s, a);
   return launch(norm_long_kernel<T, E8>, a.rows, 1024, s, a);
 }
