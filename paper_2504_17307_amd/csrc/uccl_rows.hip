@@ -129,10 +129,10 @@ int product_tiles(K kernel, uint32_t bm, uint32_t bn, uint32_t threads, ProductA
     const Slices s = slices_of(static_cast<uint32_t>(group));
     tiles = by_eights(static_cast<uint64_t>(a.groups) * s.n) * s.each;
   } else {
-    a.together = tiles_down(a, bm) * across >= kTogether * used_groups(a);
     // by group, an XCD has of every group one tile more than its eighth at most
-    tiles = a.together ? by_eights((a.rows / bm + used_groups(a)) * across) + 8ull * used_groups(a)
-                       : by_eights(a.rows / bm * across) + by_eights(used_groups(a) * across);
+    const uint64_t by_group = by_eights((a.rows / bm + used_groups(a)) * across) + 8ull * used_groups(a);
+    a.together = tiles_down(a, bm) * across >= kTogether * used_groups(a) && by_group <= 1u << 24 && fits(by_group, threads);
+    tiles = a.together ? by_group : by_eights(a.rows / bm * across) + by_eights(used_groups(a) * across);
   }
   if (tiles > 1u << 24) return UCCL_ETOOBIG;   // find_tile() counts them in 25 bits
   return launch(kernel, tiles, threads, stream, a);

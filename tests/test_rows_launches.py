@@ -130,6 +130,22 @@ def test_which_kernel_a_row_operator_is_launched_as(tmp_path):
     in_process("kernels", tmp_path)
 
 
+def largest_launches(rt):
+    """Just fewer than 2^22 tiles of 128 x 128: 65535 groups of 128 rows by 8192 columns, which the order by size has a launch for and the order by group
+    has not."""
+    seen, groups = Seen(rt), 65535
+    y, x, w = rows(128 * groups, 8192), q8(128 * groups, 496), q8(8192 * groups, 496)
+    assert rt.lib.uccl_group_product(y, x, None, w, M, groups, None) == OK
+    assert "ArithmeticE2ELNS_7ProductE0ELj128ELj128E" in rt.symbols[-1] and seen.together == [0] and rt.launches[-1][1] * rt.launches[-1][2] < 2 ** 32, (rt.symbols, seen.together)
+    seen.together.clear()
+    groups = 30000
+    assert rt.lib.uccl_group_product(rows(128 * groups, 8192), q8(128 * groups, 496), None, q8(8192 * groups, 496), M, groups, None) == OK and seen.together == [1]
+
+
+def test_the_largest_products_fit_a_launch(tmp_path):
+    in_process("largest_launches", tmp_path)
+
+
 if __name__ == "__main__":
     import test_host_launches
     runtime = test_host_launches.Runtime(sys.argv[2])
