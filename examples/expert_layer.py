@@ -4,7 +4,8 @@
 
 `dispatch` is what lies between a sender's rows and a receiver's: staged chunks, arrivals in any order and some of them twice, deduplication
 and placement.  `serve` sends rows of 8 bits with their scales and multiplies them as they arrived; `train` sends 16-bit rows and
-returns the gradients too.  Which row goes where is planned on the GPU, and nothing here waits for it.
+returns the gradients too.  Which row goes where is planned on the GPU, and nothing here reads it back; the records of what arrived come from
+the host, as a receiver's control path has them.
 
     python examples/expert_layer.py
 """

@@ -602,7 +602,7 @@ __device__ __forceinline__ void wait_for_own_loads() { asm volatile("s_waitcnt v
 // 16 rows x WIDE columns, and every wavefront a part of the sum for them, 128 bytes along it at a time in turn with the others.
 // A wavefront has a ring of its own in the LDS, loads whole 128-byte pieces of rows straight into it, and waits for no other one before
 // the parts are added up.  Bound by HBM where a group has 16 rows at most: 16 rows in 8 of 32 groups, 7168 -> 2048, in bf16 38 us, 128 rows in 32
-// groups in e4m3 78: 6.0 TB/s of weights.
+// groups in e4m3 76: 6.2 TB/s of weights.
 template <Arithmetic M, uint32_t WIDE, uint32_t WAVES>
 __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs a) {
   constexpr uint32_t THREADS = WAVES * 64u, E = M == kWidened ? 1u : 2u, HIGH = 16u, TURN = 128u, RING = 3u, NB = WIDE / 16u;

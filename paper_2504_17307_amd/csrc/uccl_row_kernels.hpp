@@ -24,7 +24,7 @@ __device__ __forceinline__ float group_reduce(float v, float* buffer) {
 
 // Quotients by one scale, as a binary32 division rounds them (Markstein's method: the product with the rounded reciprocal is off by less than
 // two steps, its remainder is exact, and what that adds rounds once).  A tiny scale is divided by as if it and the quotient's numerator were 2^64 times as large, so that
-// no remainder that can move an e4m3 value underflows.  4096 x 7168 in bf16 with a residual to e4m3: 37.3 us so, 38.7 by division, 36.8 by the reciprocal alone, which
+// no remainder that can move an e4m3 value underflows.  4096 x 7168 in bf16 with a residual to e4m3: 37.5 us so, 38.7 by division, 36.8 by the reciprocal alone, which
 // gives the neighbour beside some ties.
 struct Divisor {
   float scale, per, up;
@@ -54,7 +54,7 @@ __device__ __forceinline__ float add_square(float h, float shrink, float sum) { 
 
 // One workgroup a row.  h = x + r; s = rsqrt(mean h^2 + eps); y = h s w, from h as it was summed in 32 bits, not as it
 // is rounded for storage.  E8: y in e4m3 with a scale a row.  All loads are issued before the first is waited for: threads past
-// the row's end load its last piece.  Bound by HBM: 4096 x 7168 in bf16 with a residual to e4m3 36.8 us, 5.6 TB/s.
+// the row's end load its last piece.  Bound by HBM: 4096 x 7168 in bf16 with a residual to e4m3 37.5 us, 5.5 TB/s.
 template <class T, bool E8, uint32_t THREADS, uint32_t NV, bool ONCE>
 __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
   constexpr uint32_t N = Piece<T>::N;
