@@ -33,20 +33,24 @@ extern "C" {
 /* Element types of rows, besides UCCL_F32, UCCL_BF16 and UCCL_F16: OCP e4m3 (4 exponent bits, bias 7, no infinity, largest
  * value 448), with one binary32 scale a row: an element stands for its value times its row's scale. */
 #define UCCL_E4M3 16
+/* ... and microscaled 4 bits (OCP MXFP4): e2m1 elements, 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign above, two a byte, the earlier one in the lower half; and for
+ * every 32 of a row one byte of scale: the power of two with that number less 127 as its exponent, 255 is NaN. */
+#define UCCL_MX4 17
 
 /* A matrix by rows (HOST struct, read during the call).  `data` is 16-byte aligned and `stride` (bytes from one row to the
  * next) a multiple of 16; `cols` may be any number of elements.  The 16-byte piece that holds a row's last element may be
  * read whole, past the row's end; nothing past the end is written, and what is there never changes a result.  8-bit rows
  * have their scales at scales + i * scale_stride, 4-byte aligned, scale_stride a multiple of 4: side by side with the values
- * they make a row that is dispatched as one piece; 0 is one scale for all rows, where rows are read.  A matrix of one row, or of
+ * they make a row that is dispatched as one piece; 0 is one scale for all rows, where rows are read.  Rows of 4 bits have ceil(cols / 32) bytes of scales
+ * there, by the same rules; the aligned 4 bytes that hold a row's last scale may be read whole.  A matrix of one row, or of
  * none, may have any stride. */
 typedef struct uccl_rows {
   void* data;
   uint64_t stride;
-  void* scales;          /* UCCL_E4M3 only, NULL otherwise */
+  void* scales;          /* UCCL_E4M3 and UCCL_MX4 only, NULL otherwise */
   uint64_t scale_stride; /* bytes */
   uint32_t rows, cols;   /* at most 2^31 - 1 rows of at most 2^30 columns */
-  uint32_t dtype;        /* UCCL_F32, UCCL_BF16, UCCL_F16 or UCCL_E4M3 */
+  uint32_t dtype;        /* UCCL_F32, UCCL_BF16, UCCL_F16, UCCL_E4M3 or UCCL_MX4 */
   uint32_t reserved;     /* 0 */
 } uccl_rows;
 

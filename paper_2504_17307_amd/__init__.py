@@ -135,7 +135,7 @@ def load(path: str = None):
         if max(os.path.getmtime(f) for f in sources()) > os.path.getmtime(p):
             raise RuntimeError(f"{p} is older than its sources: rebuild (python -m paper_2504_17307_amd.build)")
     lib = C.CDLL(p)
-    for name, (res, args) in {**_SIGNATURES, **ROWS_SIGNATURES}.items():
+    for name, (res, args) in {**_SIGNATURES, **ROWS_SIGNATURES, **EXPERTS_SIGNATURES}.items():
         fn = getattr(lib, name)  # AttributeError if the library does not export it
         fn.restype, fn.argtypes = res, args
     _lib = lib
@@ -501,5 +501,8 @@ def uccl_version() -> int:
     return load().uccl_version()
 
 
-from .rows import (ROWS_HEADER_PATH, ROWS_SIGNATURES, UCCL_E4M3, uccl_combine_rows, uccl_combine_rows_grad, uccl_group_product,  # noqa: E402,F401
+from .rows import (ROWS_HEADER_PATH, ROWS_SIGNATURES, UCCL_E4M3, UCCL_MX4, uccl_combine_rows, uccl_combine_rows_grad, uccl_group_product,  # noqa: E402,F401
                    uccl_group_product_grad_w, uccl_group_product_grad_x, uccl_norm_opts, uccl_norm_rows, uccl_norm_rows_grad, uccl_norm_rows_scratch, uccl_rows)
+from .experts import (EXPERTS_HEADER_PATH, EXPERTS_SIGNATURES, uccl_balance_loss, uccl_balance_opts, uccl_clip_opts, uccl_gradient_clip,  # noqa: E402,F401
+                      uccl_gradient_norm, uccl_gradient_norm_scratch, uccl_plan_rows, uccl_plan_rows_scratch, uccl_quantise_rows, uccl_route_opts,
+                      uccl_route_rows, uccl_route_rows_grad, uccl_route_rows_scratch)

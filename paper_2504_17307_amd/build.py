@@ -7,9 +7,12 @@ import sysconfig
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
-# two translation units, which include the .hpp files beside them: the chunk data path and the row operators
+# four translation units, which include the .hpp files beside them: the chunk data path, the row operators, routing and clipping, and microscaled 4 bits
 SRC = os.path.join(CSRC, "uccl_chunk.hip")
 ROWS_SRC = os.path.join(CSRC, "uccl_rows.hip")
+EXPERTS_SRC = os.path.join(CSRC, "uccl_experts.hip")
+MX4_SRC = os.path.join(CSRC, "uccl_mx4.hip")
+ALL_SRC = (SRC, ROWS_SRC, EXPERTS_SRC, MX4_SRC)
 INC = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libuccl_chunk.so")
 # aids of bench.py (dense streaming kernels) and of the tests (the report's recount, late decisions), a library of their own
@@ -32,14 +35,14 @@ HIPCC_FLAGS = [
 def sources():
     """Every file the library is built from (kernel sources and the public headers)."""
     files = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".hip", ".hpp")))
-    return files + [os.path.join(INC, "uccl_chunk.h"), os.path.join(INC, "uccl_rows.h")]
+    return files + [os.path.join(INC, "uccl_chunk.h"), os.path.join(INC, "uccl_rows.h"), os.path.join(INC, "uccl_experts.h")]
 
 
 def build(extra_flags=(), out=LIB, verbose=False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = out + f".tmp{os.getpid()}"
-    objects = [f"{tmp}.{os.path.basename(src)}.o" for src in (SRC, ROWS_SRC)]   # linked in this order
-    cmds = [[hipcc, *HIPCC_FLAGS, *extra_flags, f"-I{INC}", f"-I{CSRC}", "-c", src, "-o", o] for src, o in zip((SRC, ROWS_SRC), objects)]
+    objects = [f"{tmp}.{os.path.basename(src)}.o" for src in ALL_SRC]   # linked in this order
+    cmds = [[hipcc, *HIPCC_FLAGS, *extra_flags, f"-I{INC}", f"-I{CSRC}", "-c", src, "-o", o] for src, o in zip(ALL_SRC, objects)]
     link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", tmp]
     try:
         if verbose:

@@ -1213,6 +1213,8 @@ int uccl_init(void) {
   if (rc == UCCL_OK) rc = device_array(g_scratch, HIP_SYMBOL(scratch), dev, &at);
   if (rc == UCCL_OK) rc = device_array(g_regions, HIP_SYMBOL(regions), dev, &at);
   if (rc == UCCL_OK) rc = uccl_internal_load_rows();
+  if (rc == UCCL_OK) rc = uccl_internal_load_experts();
+  if (rc == UCCL_OK) rc = uccl_internal_load_mx4();
   return rc;
 }
 

@@ -1,0 +1,279 @@
+// Routing, the order of rows and clipping, gfx950 (MI355X).  Host side: argument checks, the choice of the kernel, entry points of uccl_experts.h.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+#include <stdint.h>
+
+#include "uccl_experts.h"
+
+#include "uccl_gradient_kernels.hpp"
+#include "uccl_route_kernels.hpp"
+#include "uccl_row_checks.hpp"
+
+static __device__ uint32_t loaded_with_this;   // what uccl_init() looks up
+
+namespace {
+
+// A call of several launches: the calling thread's start event is on the first of them and its stop event on the last (and on the first, so that one
+// that HIP does not take is refused there).
+class Launches {
+ public:
+  template <class K, class... A>
+  int operator()(bool last, K kernel, uint64_t groups, uint32_t threads, hipStream_t s, A... a) {
+    if (first_) {
+      if (!last) stop_ = uccl_internal_stop_event();
+      first_ = false;
+    } else if (last && stop_ != nullptr) {
+      (void)uccl_time_next_launch(nullptr, stop_);
+    }
+    return launch(kernel, groups, threads, s, a...);
+  }
+
+ private:
+  bool first_ = true;
+  void* stop_ = nullptr;
+};
+
+// ---- routing ----------------------------------------------------------------------------------------
+
+constexpr uint32_t kRouteGroups = 256;   // that add up counts and probabilities, at most: one a compute unit
+
+// How many tokens a workgroup of kernels with SUMS has at a time.
+uint32_t tokens_at_a_time(uint32_t cols) { return cols <= 256u ? 32u : 8u; }
+uint32_t route_groups(uint32_t tokens, uint32_t cols) {
+  const uint32_t n = blocks_for(tokens, tokens_at_a_time(cols));
+  return n < kRouteGroups ? n : kRouteGroups;
+}
+
+// Calls f with the lanes of a token and the pieces of a lane, for rows of `cols` elements of T.
+template <class T, class F>
+int with_lanes(uint32_t cols, F f) {
+  constexpr uint32_t N = Piece<T>::N;
+  using std::integral_constant;
+  using L16 = integral_constant<uint32_t, 16>;
+  using L64 = integral_constant<uint32_t, 64>;
+  if (cols <= 16u * N) return f(L16{}, integral_constant<uint32_t, 1>{});
+  if (cols <= 32u * N) return f(L16{}, integral_constant<uint32_t, 2>{});
+  if constexpr (N == 4u)
+    if (cols <= 64u * N) return f(L16{}, integral_constant<uint32_t, 4>{});
+  if (cols <= 512u) return f(L64{}, integral_constant<uint32_t, 8u / N>{});
+  return f(L64{}, integral_constant<uint32_t, 16u / N>{});
+}
+
+int check_route(const uccl_rows* scores, const uccl_route_opts* o) {
+  const int e = check(scores);
+  if (e != UCCL_OK) return e;
+  if (!is_float(scores->dtype) || scores->cols > UCCL_MOST_EXPERTS || o == nullptr || o->reserved != 0u || o->normalise > 1u || !isfinite(o->scale)) return UCCL_EINVAL;
+  return o->slots == 0u || o->slots > scores->cols || o->slots > UCCL_MOST_SLOTS ? UCCL_EINVAL : UCCL_OK;
+}
+
+// ---- the order of rows ------------------------------------------------------------------------------
+
+constexpr uint32_t kPlanTile = 2u * kPlanThreads, kPlanGroups = 128;   // choices a workgroup has at a time, workgroups at most
+
+struct PlanShape {
+  uint32_t groups, share;
+};
+PlanShape plan_shape(uint64_t choices) {
+  const uint64_t tiles = (choices + kPlanTile - 1u) / kPlanTile, each = (tiles + kPlanGroups - 1u) / kPlanGroups;
+  if (each == 0u) return PlanShape{1u, kPlanTile};
+  return PlanShape{static_cast<uint32_t>((tiles + each - 1u) / each), static_cast<uint32_t>(each * kPlanTile)};
+}
+
+// ---- gradients --------------------------------------------------------------------------------------
+
+constexpr uint32_t kGradientGroups = 4096, kLeastShare = 1024;   // workgroups of a call, about, and pieces of a workgroup at least
+
+uint32_t pieces_of(const uccl_rows* m) { return blocks_for(row_bytes(m), 16u); }
+
+// Goes through the matrices that have elements, as many at a time as a launch takes: f(args, workgroups, whether they are the last).
+template <class F>
+int over_matrices(const uccl_rows* in, const uccl_rows* out, uint32_t n, F f) {
+  uint64_t pieces = 0;
+  uint32_t some = 0;
+  for (uint32_t i = 0; i < n; ++i) {
+    const uint64_t mine = static_cast<uint64_t>(in[i].rows) * pieces_of(in + i);
+    pieces += mine;
+    some += mine != 0u;
+  }
+  GradientArgs a{};
+  uint64_t share = (pieces / kGradientGroups + kLeastShare) / kLeastShare * kLeastShare;
+  a.share = static_cast<uint32_t>(share < 1u << 30 ? share : 1u << 30);
+  uint64_t groups = 0;
+  for (uint32_t i = 0; i < n; ++i) {
+    const uint32_t p = pieces_of(in + i);
+    const uint64_t mine = static_cast<uint64_t>(in[i].rows) * p;
+    if (mine == 0u) continue;
+    Matrix& m = a.m[a.n];
+    m = Matrix{static_cast<const char*>(in[i].data), out == nullptr ? nullptr : static_cast<char*>(out[i].data), in[i].stride, out == nullptr ? 0u : out[i].stride, in[i].rows, in[i].cols, p};
+    // rows that follow each other without a gap are one (its elements have to be counted in 32 bits)
+    const uint64_t all = static_cast<uint64_t>(in[i].rows) * in[i].cols;
+    if (in[i].rows > 1u && in[i].stride == row_bytes(in + i) && (out == nullptr || out[i].stride == in[i].stride) && all <= 0xFFFFFFFFull) {
+      m.rows = 1u;
+      m.cols = static_cast<uint32_t>(all);
+      m.pieces = static_cast<uint32_t>(mine);
+    }
+    a.dtype[a.n] = static_cast<uint8_t>(in[i].dtype == UCCL_F32 ? 0u : in[i].dtype == UCCL_BF16 ? 1u : 2u);
+    a.first[a.n++] = static_cast<uint32_t>(groups);
+    groups += (mine + a.share - 1u) / a.share;
+    --some;
+    if (a.n == kMatrices || some == 0u) {
+      const int e = f(a, groups, some == 0u);
+      if (e != UCCL_OK) return e;
+      a.n = 0u;
+      groups = 0u;
+    }
+  }
+  return UCCL_OK;
+}
+
+int check_gradients(const uccl_rows* m, uint32_t n) {
+  if ((m == nullptr && n != 0u) || n > kMost) return UCCL_EINVAL;
+  for (uint32_t i = 0; i < n; ++i) {
+    const int e = check(m + i);
+    if (e != UCCL_OK) return e;
+    if (!is_float(m[i].dtype)) return UCCL_EINVAL;
+  }
+  return UCCL_OK;
+}
+
+}  // namespace
+
+int uccl_internal_load_experts() {
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;   // another stream of the program may be under capture
+  const bool relaxed = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
+  void* at = nullptr;
+  const hipError_t e = hipGetSymbolAddress(&at, HIP_SYMBOL(loaded_with_this));
+  if (relaxed) (void)hipThreadExchangeStreamCaptureMode(&mode);
+  return e == hipSuccess ? UCCL_OK : uccl_internal_failed(e);
+}
+
+extern "C" {
+
+uint64_t uccl_route_rows_scratch(uint32_t tokens, uint32_t n_experts) {
+  const uint32_t groups = route_groups(tokens, n_experts);
+  return groups <= 1u ? 0u : (groups * 8ull * n_experts + 15u) / 16u * 16u;
+}
+
+int uccl_route_rows(int32_t* experts, float* weights, int32_t* counts, float* sums, const uccl_rows* scores, const float* bias,
+                    const uccl_route_opts* opts, void* scratch, uint64_t scratch_bytes, void* stream) {
+  const int e = check_route(scores, opts);
+  if (e != UCCL_OK) return e;
+  if (scores->rows != 0u && (experts == nullptr || weights == nullptr)) return UCCL_EINVAL;
+  if (misaligned(experts, 4) || misaligned(weights, 4) || misaligned(counts, 4) || misaligned(sums, 4) || misaligned(bias, 4)) return UCCL_EALIGN;
+  const bool wanted = counts != nullptr || sums != nullptr;
+  if (scores->rows == 0u && !wanted) return UCCL_OK;
+  const uint32_t groups = route_groups(scores->rows, scores->cols);
+  if (wanted && groups > 1u) {
+    if (scratch == nullptr || scratch_bytes < uccl_route_rows_scratch(scores->rows, scores->cols)) return UCCL_EINVAL;
+    if (misaligned(scratch, 16)) return UCCL_EALIGN;
+  }
+  const RouteArgs a{experts, weights, counts, sums, groups > 1u ? static_cast<uint32_t*>(scratch) : nullptr, rows_of(scores), bias, scores->rows, scores->cols, opts->slots, opts->normalise, opts->scale};
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  Launches go;
+  if (scores->rows == 0u) return go(true, route_sum_kernel, blocks_for(scores->cols, 16u), 256, s, counts, sums, static_cast<const uint32_t*>(nullptr), 0u, scores->cols);
+  return with_type(scores->dtype, [&](auto t) {
+    using T = decltype(t);
+    return with_lanes<T>(scores->cols, [&](auto lanes, auto pieces) -> int {
+      constexpr uint32_t L = decltype(lanes)::value, K = decltype(pieces)::value;
+      if (!wanted) return go(true, route_kernel<T, L, K, false>, blocks_for(scores->rows, 256u / L), 256, s, a);
+      const int first = go(groups == 1u, route_kernel<T, L, K, true>, groups, 512, s, a);
+      if (first != UCCL_OK || groups == 1u) return first;
+      return go(true, route_sum_kernel, blocks_for(scores->cols, 16u), 256, s, counts, sums, static_cast<const uint32_t*>(a.parts), groups, scores->cols);
+    });
+  });
+}
+
+int uccl_route_rows_grad(const uccl_rows* dscores, const uccl_rows* scores, const int32_t* experts, const float* dweights, const float* dsums,
+                         const uccl_route_opts* opts, void* stream) {
+  int e = check_route(scores, opts);
+  if (e == UCCL_OK) e = check(dscores);
+  if (e != UCCL_OK) return e;
+  if (dscores->dtype != scores->dtype || !same_shape(dscores, scores)) return UCCL_EINVAL;
+  if (scores->rows != 0u && (experts == nullptr) != (dweights == nullptr)) return UCCL_EINVAL;
+  if (misaligned(experts, 4) || misaligned(dweights, 4) || misaligned(dsums, 4)) return UCCL_EALIGN;
+  if (scores->rows == 0u) return UCCL_OK;
+  const RouteGradArgs a{rows_of(dscores), rows_of(scores), experts, dweights, dsums, scores->rows, scores->cols, opts->slots, opts->normalise, opts->scale};
+  return with_type(scores->dtype, [&](auto t) {
+    using T = decltype(t);
+    return with_lanes<T>(scores->cols, [&](auto lanes, auto pieces) {
+      constexpr uint32_t L = decltype(lanes)::value, K = decltype(pieces)::value;
+      return launch(route_grad_kernel<T, L, K>, blocks_for(scores->rows, 256u / L), 256, static_cast<hipStream_t>(stream), a);
+    });
+  });
+}
+
+int uccl_balance_loss(float* loss, float* dsums, const int32_t* counts, const float* sums, uint32_t n_experts, const uccl_balance_opts* o, void* stream) {
+  if (o == nullptr || o->tokens == 0u || o->slots == 0u || !isfinite(o->coef) || n_experts > kMost || (n_experts != 0u && (counts == nullptr || sums == nullptr))) return UCCL_EINVAL;
+  if (misaligned(loss, 4) || misaligned(dsums, 4) || misaligned(counts, 4) || misaligned(sums, 4)) return UCCL_EALIGN;
+  if (loss == nullptr && (dsums == nullptr || n_experts == 0u)) return UCCL_OK;
+  const double tokens = static_cast<double>(o->tokens), factor = static_cast<double>(o->coef) * n_experts / (o->slots * tokens * tokens);
+  return launch(balance_kernel, 1, 256, static_cast<hipStream_t>(stream), loss, dsums, counts, sums, n_experts, factor);
+}
+
+uint64_t uccl_plan_rows_scratch(uint64_t choices, uint32_t n_experts) {
+  const uint32_t groups = plan_shape(choices).groups;
+  return groups == 1u ? 0u : (groups * 4ull * n_experts + 15u) / 16u * 16u;
+}
+
+int uccl_plan_rows(int32_t* index, int32_t* offsets, int32_t* pos, const int32_t* experts, uint32_t tokens, uint32_t slots, uint32_t n_experts,
+                   void* scratch, uint64_t scratch_bytes, void* stream) {
+  const uint64_t choices = static_cast<uint64_t>(tokens) * slots;
+  if (choices > kMost || n_experts == 0u || n_experts > UCCL_MOST_EXPERTS || offsets == nullptr || (experts == nullptr && choices != 0u)) return UCCL_EINVAL;
+  if (index != nullptr && (index == experts || index == pos)) return UCCL_EINVAL;
+  if (misaligned(index, 4) || misaligned(offsets, 4) || misaligned(pos, 4) || misaligned(experts, 4)) return UCCL_EALIGN;
+  const PlanShape shape = plan_shape(choices);
+  if (shape.groups > 1u) {
+    if (scratch == nullptr || scratch_bytes < uccl_plan_rows_scratch(choices, n_experts)) return UCCL_EINVAL;
+    if (misaligned(scratch, 16)) return UCCL_EALIGN;
+  }
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  Launches go;
+  uint32_t* const counts = shape.groups > 1u ? static_cast<uint32_t*>(scratch) : nullptr;
+  const PlanArgs a{index, offsets, pos, experts, counts, static_cast<uint32_t>(choices), slots, n_experts, shape.share};
+  if (counts != nullptr) {
+    const int e = go(false, plan_count_kernel, shape.groups, kPlanThreads, s, counts, experts, a.choices, n_experts, shape.share);
+    if (e != UCCL_OK) return e;
+  }
+  return go(true, plan_kernel<kPlanTile / kPlanThreads>, shape.groups, kPlanThreads, s, a);
+}
+
+// kGradientGroups and one more for every matrix, whose last workgroup may have less than its share.
+uint64_t uccl_gradient_norm_scratch(uint32_t n) { return ((kGradientGroups + static_cast<uint64_t>(n)) * 8u + 15u) / 16u * 16u; }
+
+int uccl_gradient_norm(float* norm, const uccl_rows* grads, uint32_t n, void* scratch, uint64_t scratch_bytes, void* stream) {
+  const int e = check_gradients(grads, n);
+  if (e != UCCL_OK) return e;
+  if (norm == nullptr || scratch == nullptr || scratch_bytes < uccl_gradient_norm_scratch(n)) return UCCL_EINVAL;
+  if (misaligned(norm, 4) || misaligned(scratch, 16)) return UCCL_EALIGN;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  Launches go;
+  double* const parts = static_cast<double*>(scratch);
+  uint64_t done = 0;
+  const int code = over_matrices(grads, nullptr, n, [&](GradientArgs& a, uint64_t groups, bool) {
+    a.parts = parts + done;
+    done += groups;
+    return go(false, square_sum_kernel, groups, kGradientThreads, s, a);
+  });
+  return code != UCCL_OK ? code : go(true, square_root_kernel, 1, 1024, s, norm, static_cast<const double*>(parts), static_cast<uint32_t>(done));
+}
+
+int uccl_gradient_clip(const uccl_rows* out, const uccl_rows* grads, uint32_t n, const float* norm, const uccl_clip_opts* opts, void* stream) {
+  int e = check_gradients(grads, n);
+  if (e == UCCL_OK) e = check_gradients(out, n);
+  if (e != UCCL_OK) return e;
+  if (opts == nullptr || !(opts->most > 0.0f) || isinf(opts->most) || opts->reserved[0] || opts->reserved[1] || opts->reserved[2]) return UCCL_EINVAL;
+  for (uint32_t i = 0; i < n; ++i)
+    if (out[i].dtype != grads[i].dtype || !same_shape(out + i, grads + i)) return UCCL_EINVAL;
+  if (n == 0u) return UCCL_OK;
+  if (norm == nullptr) return UCCL_EINVAL;
+  if (misaligned(norm, 4)) return UCCL_EALIGN;
+  Launches go;
+  return over_matrices(grads, out, n, [&](GradientArgs& a, uint64_t groups, bool last) {
+    a.norm = norm;
+    a.most = opts->most;
+    return go(last, gradient_clip_kernel, groups, kGradientThreads, static_cast<hipStream_t>(stream), a);
+  });
+}
+
+}  // extern "C"

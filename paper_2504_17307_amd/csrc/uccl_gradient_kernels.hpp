@@ -1,0 +1,133 @@
+// The norm of many matrices together, and their scaling to it (device code).  Internal to the library.
+#pragma once
+
+#include "uccl_row_elements.hpp"
+
+namespace {
+
+// The matrices of a launch.  A workgroup has `share` pieces of 16 bytes of one of them: matrix i has the workgroups from first[i] on.
+constexpr uint32_t kMatrices = 64;
+struct Matrix {
+  const char* in;
+  char* out;
+  uint64_t in_stride, out_stride;
+  uint32_t rows, cols, pieces;   // pieces of a row
+};
+struct GradientArgs {
+  uint32_t first[kMatrices];
+  uint8_t dtype[kMatrices];
+  Matrix m[kMatrices];
+  uint32_t n, share;
+  double* parts;                 // the norm: a workgroup's sum
+  const float* norm;             // the clipping
+  float most;
+};
+
+constexpr uint32_t kGradientThreads = 256, kGradientUnroll = 4;
+
+// Which of them a workgroup's is: the last one that begins at it or before.
+__device__ __forceinline__ uint32_t matrix_of(const GradientArgs& a, uint32_t group) {
+  const uint32_t lane = threadIdx.x % 64u;
+  return __popcll(__ballot(lane < a.n && a.first[lane] <= group)) - 1u;
+}
+
+// Calls f(row, piece, valid elements of it) for every piece of the workgroup's that is the thread's, kGradientUnroll at a time: load() first, then use().
+template <class T, class L, class U>
+__device__ __forceinline__ void over_pieces(const Matrix& m, uint64_t begin, uint32_t share, L load, U use) {
+  constexpr uint32_t N = Piece<T>::N;
+  const uint64_t all = static_cast<uint64_t>(m.rows) * m.pieces, end = min(begin + share, all);
+  for (uint64_t at = begin + threadIdx.x; at < end; at += kGradientThreads * kGradientUnroll) {
+    Piece<T> p[kGradientUnroll];
+    uint64_t row[kGradientUnroll];
+    uint32_t piece[kGradientUnroll];
+#pragma unroll
+    for (uint32_t u = 0; u < kGradientUnroll; ++u) {
+      const uint64_t mine = min(at + u * kGradientThreads, end - 1u);
+      row[u] = m.rows == 1u ? 0u : mine / m.pieces;
+      piece[u] = static_cast<uint32_t>(mine - row[u] * m.pieces);
+      p[u] = load(row[u], piece[u]);
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < kGradientUnroll; ++u)
+      if (at + u * kGradientThreads < end) use(row[u], piece[u], p[u], m.cols - piece[u] * N);
+  }
+}
+
+template <class T, bool ONCE>
+__device__ __forceinline__ double square_sum(const Matrix& m, uint64_t begin, uint32_t share) {
+  double sum = 0.0;
+  over_pieces<T>(m, begin, share,
+    [&](uint64_t row, uint32_t piece) { return ONCE ? load_piece_once<T>(m.in + row * m.in_stride, piece) : load_piece<T>(m.in + row * m.in_stride, piece); },
+    [&](uint64_t, uint32_t, Piece<T>& p, uint32_t valid) {
+      blank(p, valid);
+#pragma unroll
+      for (uint32_t i = 0; i < Piece<T>::N; ++i) sum = __builtin_fma(static_cast<double>(widen(p.v[i])), static_cast<double>(widen(p.v[i])), sum);
+    });
+  return sum;
+}
+
+__device__ __forceinline__ double wave_sum_64(double v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// Squares in binary64, which has them exactly and does not overflow.
+__global__ __launch_bounds__(kGradientThreads) void square_sum_kernel(GradientArgs a) {
+  __shared__ double buffer[kGradientThreads / 64u];
+  const uint32_t i = __builtin_amdgcn_readfirstlane(matrix_of(a, blockIdx.x));
+  const Matrix m = a.m[i];
+  const uint64_t begin = static_cast<uint64_t>(blockIdx.x - a.first[i]) * a.share;
+  double sum = a.dtype[i] == 0u ? square_sum<float, false>(m, begin, a.share) : a.dtype[i] == 1u ? square_sum<__bf16, false>(m, begin, a.share) : square_sum<_Float16, false>(m, begin, a.share);
+  sum = wave_sum_64(sum);
+  if (threadIdx.x % 64u == 0u) buffer[threadIdx.x / 64u] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0u) return;
+#pragma unroll
+  for (uint32_t w = 1; w < kGradientThreads / 64u; ++w) sum += buffer[w];
+  a.parts[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(1024) void square_root_kernel(float* norm, const double* parts, uint32_t n) {
+  __shared__ double buffer[16];
+  double sum = 0.0;
+#pragma unroll 4
+  for (uint32_t i = threadIdx.x; i < n; i += 1024u) sum += parts[i];
+  sum = wave_sum_64(sum);
+  if (threadIdx.x % 64u == 0u) buffer[threadIdx.x / 64u] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0u) return;
+#pragma unroll
+  for (uint32_t w = 1; w < 16u; ++w) sum += buffer[w];
+  *norm = static_cast<float>(sqrt(sum));
+}
+
+template <class T>
+__device__ __forceinline__ void scale_pieces(const Matrix& m, uint64_t begin, uint32_t share, float by) {
+  over_pieces<T>(m, begin, share,
+    [&](uint64_t row, uint32_t piece) { return load_piece<T>(m.in + row * m.in_stride, piece); },
+    [&](uint64_t row, uint32_t piece, Piece<T>& p, uint32_t valid) {
+#pragma unroll
+      for (uint32_t i = 0; i < Piece<T>::N; ++i) {
+        float v = widen(p.v[i]) * by;
+        asm("" : "+v"(v));   // a product in binary32 for f16 too, not an instruction that rounds the exact one to 16 bits
+        p.v[i] = static_cast<T>(v);
+      }
+      store_piece<false>(m.out + row * m.out_stride, piece, p, valid);
+    });
+}
+
+// The last workgroups' pieces first: they are what the norm has read last, and the caches have.
+__global__ __launch_bounds__(kGradientThreads) void gradient_clip_kernel(GradientArgs a) {
+  const uint32_t group = gridDim.x - 1u - blockIdx.x;
+  const uint32_t i = __builtin_amdgcn_readfirstlane(matrix_of(a, group));
+  const Matrix m = a.m[i];
+  const float norm = *a.norm, by = norm <= a.most ? 1.0f : a.most / norm;   // NaN of NaN
+  if (by == 1.0f && m.in == m.out && m.in_stride == m.out_stride) return;
+  const uint64_t begin = static_cast<uint64_t>(group - a.first[i]) * a.share;
+  if (a.dtype[i] == 0u) scale_pieces<float>(m, begin, a.share, by);
+  else if (a.dtype[i] == 1u) scale_pieces<__bf16>(m, begin, a.share, by);
+  else scale_pieces<_Float16>(m, begin, a.share, by);
+}
+
+}  // namespace

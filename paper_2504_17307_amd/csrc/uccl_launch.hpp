@@ -14,6 +14,9 @@ __attribute__((visibility("hidden"))) int uccl_internal_launch(const void* kerne
 __attribute__((visibility("hidden"))) void* uccl_internal_stop_event();
 // Load the code object of the row operators on the current device (uccl_rows.hip).
 __attribute__((visibility("hidden"))) int uccl_internal_load_rows();
+// The same of routing and clipping (uccl_experts.hip), and of microscaled 4 bits (uccl_mx4.hip).
+__attribute__((visibility("hidden"))) int uccl_internal_load_experts();
+__attribute__((visibility("hidden"))) int uccl_internal_load_mx4();
 // The same for a HIP error that another call returned.
 __attribute__((visibility("hidden"))) int uccl_internal_failed(hipError_t e);
 

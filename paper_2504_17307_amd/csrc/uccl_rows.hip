@@ -7,65 +7,12 @@
 
 #include "uccl_rows.h"
 
-#include "uccl_launch.hpp"
 #include "uccl_product_kernels.hpp"
+#include "uccl_product_launch.hpp"
+#include "uccl_row_checks.hpp"
 #include "uccl_row_kernels.hpp"
 
 namespace {
-
-constexpr uint32_t kMost = 0x7FFFFFFFu, kMostCols = 1u << 30;   // rows, slots, groups; columns
-
-bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
-
-uint32_t element_bytes(uint32_t dtype) {
-  switch (dtype) {
-    case UCCL_F32: return 4;
-    case UCCL_BF16: case UCCL_F16: return 2;
-    case UCCL_E4M3: return 1;
-    default: return 0;
-  }
-}
-bool is_16(uint32_t dtype) { return dtype == UCCL_BF16 || dtype == UCCL_F16; }
-bool is_float(uint32_t dtype) { return dtype == UCCL_F32 || is_16(dtype); }
-bool same_shape(const uccl_rows* a, const uccl_rows* b) { return a->rows == b->rows && a->cols == b->cols; }
-
-// What holds for every matrix by itself.
-int check(const uccl_rows* m) {
-  if (m == nullptr || m->reserved != 0u || element_bytes(m->dtype) == 0u || m->rows > kMost || m->cols > kMostCols) return UCCL_EINVAL;
-  if ((m->dtype == UCCL_E4M3) != (m->scales != nullptr) && m->rows != 0u) return UCCL_EINVAL;
-  if (m->rows == 0u || m->cols == 0u) return UCCL_OK;
-  if (m->data == nullptr) return UCCL_EINVAL;
-  if (m->rows > 1u && m->stride < static_cast<uint64_t>(m->cols) * element_bytes(m->dtype)) return UCCL_EINVAL;   // rows would overlap
-  if (misaligned(m->data, 16) || (m->rows > 1u && m->stride % 16u != 0u)) return UCCL_EALIGN;
-  if (m->scales != nullptr && (misaligned(m->scales, 4) || (m->rows > 1u && m->scale_stride % 4u != 0u))) return UCCL_EALIGN;
-  return UCCL_OK;
-}
-template <class... M>
-int check(const uccl_rows* first, const M*... others) {
-  const int e = check(first);
-  return e != UCCL_OK ? e : check(others...);
-}
-
-Rows rows_of(const uccl_rows* m) {
-  if (m == nullptr) return Rows{nullptr, 0, nullptr, 0};
-  return Rows{static_cast<char*>(m->data), m->stride, static_cast<char*>(m->scales), m->scale_stride};
-}
-
-uint32_t blocks_for(uint64_t n, uint32_t each) { return static_cast<uint32_t>((n + each - 1) / each); }
-
-// A grid of `groups` workgroups; HIP takes fewer than 2^32 threads a launch.
-bool fits(uint64_t groups, uint32_t threads) { return groups <= 0xFFFFFFFFull / threads; }
-
-template <class K, class... A>
-int launch(K kernel, uint64_t groups, uint32_t threads, hipStream_t s, A... a) {
-  return fits(groups, threads) ? enqueue(kernel, dim3(static_cast<uint32_t>(groups)), threads, s, a...) : static_cast<int>(UCCL_ETOOBIG);
-}
-
-// Calls f with a value of the element type of 16- or 32-bit rows.
-template <class F>
-int with_type(uint32_t dtype, F f) {
-  return dtype == UCCL_F32 ? f(float{}) : dtype == UCCL_BF16 ? f(__bf16{}) : f(_Float16{});
-}
 
 // Outputs of more than this do not stay in the L2s (8 of 4 MiB) until they are read, and are stored past them: norm of 4096 x 7168 in
 // bf16 to e4m3 48 -> 39 us (loads past them too), combination of 8 x 4096 rows 104 -> 86.
@@ -101,42 +48,6 @@ int norm_grad(const NormGradArgs& a, uint32_t groups, hipStream_t s) {
 }
 
 OutType out_type(const uccl_rows* m) { return m->dtype == UCCL_F32 ? kOutF32 : m->dtype == UCCL_BF16 ? kOutBf16 : kOutF16; }
-
-uint32_t used_groups(const ProductArgs& a) { return a.groups < a.rows ? a.groups : a.rows; }   // that have rows, at most
-
-// How many tiles of so many rows the groups are cut into: the last one of a group is half empty on average.
-double tiles_down(const ProductArgs& a, uint32_t high) {
-  return a.groups == 1u ? blocks_for(a.rows, high) : static_cast<double>(a.rows) / high + 0.5 * used_groups(a);
-}
-
-// A launch over tiles of BM x BN: a workgroup for each that there could be whatever the offsets are, by eights.
-//
-// The tiles of products by rows come in one of two orders.  Full ones first keep the last round short; all of a group's together read its
-// weights once, which pays where a group has many.  Measured, by size / by group, us: 8190 rows in 16 groups, 2048 -> 7168, bf16 (70 tiles a group) 297 / 273
-// (1.10 / 0.93 GB read); gradients of 4096 rows in 16 groups, 7168 x 2048 (42) 183 / 167; by 16 rows, 3000 -> 1200, bf16, 100 rows in one group / 3 / 8 (266, 98,
-// 49) 10.6 / 8.9, 13.8 / 8.9, 17.2 / 15.2; 200 rows in one group, 7168 -> 2048 (32) 48 / 50; 400 rows in 8 groups (14) 47 / 50; gradients of 2000 rows in
-// 32 groups, 1003 x 600 (5) 13 / 17.
-constexpr double kTogether = 40.0;
-
-template <Product P, class K>
-int product_tiles(K kernel, uint32_t bm, uint32_t bn, uint32_t threads, ProductArgs a, hipStream_t stream) {
-  const uint64_t across = blocks_for(P == kForward ? a.wide : a.cols, bn);
-  auto by_eights = [](uint64_t n) { return (n + 7u) / 8u * 8u; };
-  uint64_t tiles;
-  if (P == kGradW) {
-    const uint64_t group = blocks_for(a.wide, bm) * across;
-    if (group > 1u << 24) return UCCL_ETOOBIG;
-    const Slices s = slices_of(static_cast<uint32_t>(group));
-    tiles = by_eights(static_cast<uint64_t>(a.groups) * s.n) * s.each;
-  } else {
-    // by group, an XCD has of every group one tile more than its eighth at most
-    const uint64_t by_group = by_eights((a.rows / bm + used_groups(a)) * across) + 8ull * used_groups(a);
-    a.together = tiles_down(a, bm) * across >= kTogether * used_groups(a) && by_group <= 1u << 24 && fits(by_group, threads);
-    tiles = a.together ? by_group : by_eights(a.rows / bm * across) + by_eights(used_groups(a) * across);
-  }
-  if (tiles > 1u << 24) return UCCL_ETOOBIG;   // find_tile() counts them in 25 bits
-  return launch(kernel, tiles, threads, stream, a);
-}
 
 // What a tile costs is about the same whether one compute unit works or all do, and whether all of its rows are there or a few, and
 // a launch of few tiles takes as long as the compute units that get one more than others.  256 x 256 does the most work for what
@@ -298,14 +209,15 @@ int uccl_group_product(const uccl_rows* y, const uccl_rows* x, const int32_t* in
   int e = check(y, x, w);
   if (e != UCCL_OK) return e;
   uint32_t wide = 0;
-  if (!is_float(y->dtype) || !(is_16(x->dtype) || x->dtype == UCCL_E4M3) || w->dtype != x->dtype || w->cols != x->cols) return UCCL_EINVAL;
+  const bool mx4 = w->dtype == UCCL_MX4 && (x->dtype == UCCL_MX4 || is_16(x->dtype));
+  if (!is_float(y->dtype) || !(mx4 || ((is_16(x->dtype) || x->dtype == UCCL_E4M3) && w->dtype == x->dtype)) || w->cols != x->cols) return UCCL_EINVAL;
   e = check_product(y, w, index, offsets, n_groups, &wide);
   if (e != UCCL_OK) return e;
   if ((n_groups != 0u && y->cols != wide) || (index == nullptr && x->rows < y->rows)) return UCCL_EINVAL;
   if (n_groups == 0u || y->rows == 0u || y->cols == 0u) return UCCL_OK;
   const uint32_t depth = x->rows == 0u ? 0u : x->cols;   // no row of x: nothing to add
   const ProductArgs a{rows_of(y), rows_of(x), rows_of(w), index, offsets, n_groups, y->rows, x->rows, wide, depth, out_type(y), 0};
-  return product<kForward>(a, x->dtype, static_cast<hipStream_t>(stream));
+  return mx4 ? uccl_internal_product_mx4(&a, x->dtype, static_cast<hipStream_t>(stream)) : product<kForward>(a, x->dtype, static_cast<hipStream_t>(stream));
 }
 
 int uccl_group_product_grad_x(const uccl_rows* dx, const uccl_rows* dy, const uccl_rows* w, const int32_t* offsets, uint32_t n_groups, void* stream) {

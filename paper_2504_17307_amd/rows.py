@@ -10,7 +10,7 @@ import ctypes as C
 import os
 import struct
 
-UCCL_E4M3 = 16
+UCCL_E4M3, UCCL_MX4 = 16, 17
 ROWS_HEADER_PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "uccl_rows.h")
 
 
@@ -48,14 +48,15 @@ def _type(dtype):
         import torch
         from . import UCCL_BF16, UCCL_F16, UCCL_F32
         _types.update({torch.float32: (UCCL_F32, 4), torch.bfloat16: (UCCL_BF16, 2), torch.float16: (UCCL_F16, 2),
-                       torch.float8_e4m3fn: (UCCL_E4M3, 1), "scale": torch.float32})
+                       torch.float8_e4m3fn: (UCCL_E4M3, 1), torch.float4_e2m1fn_x2: (UCCL_MX4, 1), "scale": torch.float32, "block": torch.float8_e8m0fnu})
     if dtype not in _types:
         raise ValueError(f"rows of {dtype} are not supported")
     return _types[dtype]
 
 
-def _rows(t, scales=None):
-    """The bytes of a HOST uccl_rows for a tensor, as an argument; None for None."""
+def _rows(t, scales=None, cols_in_4_bits=None):
+    """The bytes of a HOST uccl_rows for a tensor, as an argument; None for None.  Rows of 4 bits have two elements in each of the tensor's, or
+    one in the last, if ``cols_in_4_bits`` says so."""
     if t is None:
         return None
     number, size = _types.get(t.dtype) or _type(t.dtype)
@@ -79,6 +80,8 @@ def _rows(t, scales=None):
         raise ValueError("a tensor of rows has fewer than 2^32 rows and columns")
     if scales is None:
         return _pack_rows(t.data_ptr(), step * size, 0, 0, rows, cols, number, 0)
+    if number == UCCL_MX4:
+        return _rows_in_4_bits(t, step, rows, cols, scales, cols_in_4_bits)
     if scales.dtype is not _types["scale"] or scales.numel() != rows:
         raise ValueError("scales are float32, one for every row")
     lengths, apart = scales.shape, scales.stride()
@@ -88,6 +91,20 @@ def _rows(t, scales=None):
         raise ValueError("scales have to be the same distance apart throughout")
     between = 0 if not lengths else 4 * (apart[0] if lengths[-1] == 1 else apart[-1])
     return _pack_rows(t.data_ptr(), step * size, scales.data_ptr(), between, rows, cols, number, 0)
+
+
+def _rows_in_4_bits(t, step, rows, pairs, scales, cols):
+    cols = 2 * pairs if cols is None else cols
+    blocks = -(-cols // 32)
+    if (cols + 1) // 2 != pairs:
+        raise ValueError(f"{cols} elements are {(cols + 1) // 2} pairs in 4 bits")
+    lengths, apart = scales.shape, scales.stride()
+    if scales.dtype is not _types["block"] or len(lengths) not in (2, 3) or scales.numel() != rows * blocks or lengths[-1] != blocks:
+        raise ValueError("scales are float8_e8m0fnu, one for every 32 elements of a row")
+    if (apart[-1] != 1 and blocks > 1) or len(lengths) == 3 and lengths[0] > 1 and lengths[1] > 1 and apart[0] != lengths[1] * apart[1]:
+        raise ValueError("a row's scales have to be contiguous, and the rows' the same distance apart throughout")
+    between = apart[0] if lengths[-2] == 1 else apart[-2]
+    return _pack_rows(t.data_ptr(), step, scales.data_ptr(), between, rows, cols, UCCL_MX4, 0)
 
 
 def _vector(t, kind, n, what):
@@ -130,7 +147,8 @@ def uccl_norm_rows_grad(dx, dweight, dy, h, rstd, weight, scratch, dh=None, stre
 
 def uccl_group_product(y, x, w, offsets, index=None, x_scales=None, w_scales=None, stream=None):
     """y[i] = x[index[i]] @ w[g].T for the rows offsets[g] <= i < offsets[g + 1]; ``w``: groups x n x k."""
-    _call("uccl_group_product", _rows(y), _rows(x, x_scales), _vector(index, "i", _count(y), "index"), _rows(w, w_scales),
+    cols = x.shape[-1] if w_scales is not None and x_scales is None else None   # 16-bit rows with weights in 4 bits
+    _call("uccl_group_product", _rows(y), _rows(x, x_scales), _vector(index, "i", _count(y), "index"), _rows(w, w_scales, cols),
           _vector(offsets, "i", w.shape[0] + 1, "offsets"), w.shape[0], _stream(stream))
 
 
