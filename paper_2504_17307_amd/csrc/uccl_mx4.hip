@@ -12,9 +12,42 @@
 
 namespace {
 
+// How long a launch of `tiles` takes that has room for `room` at a time, in rounds.  (The tiles are estimated: a little more than a round may be one.)
+double rounds_of(double tiles, double room) {
+  const double rounds = tiles / room;
+  return rounds <= 1.05 ? 1.0 : rounds <= 2.0 ? 2.0 : rounds + 0.5;
+}
+
+// Rows of 4 bits, in us for 256 elements of the sum.  Few rows: 2.0e-5 for 16 rows of a column, 2.6e-5 for a column's weights where they are read once;
+// tiles of 128 x 128, two on a compute unit: 1.7 a round, 1 where most of them are idle.  Measured, 16 rows at a time / 128 x 128, 7168 -> 2048, us: one group, 1 / 100 rows, 8.0 / 10.4 against
+// 23 / 28; 8 of 32 groups, 16 rows, 13.3 against 28; 32 groups, 128 rows, 49 against 54; 8 groups, 300 rows, 26 against 29; 16 groups, 1000 rows, 81 against 47.
+// Tiles: in units of one of 256 x 256 (67 us with a depth of 7168, one a compute unit) 128 x 128 costs 0.62, two on a compute unit.  Measured, 256 x 256 / 128 x 128, us: 4096 rows in 16 ragged groups,
+// 7168 -> 2048, 84 / 95; 2048 rows 79 / 67; 1000 rows 65 / 47; 4000 rows in 4 groups 67 / 53; 8190 rows in 16 groups, 2048 -> 7168, 133 / 144; 512 rows in one group, 2048 -> 2048, 21 / 11; 8192^3 339 / 457.
+// (128 x 256, of which one fits a compute unit, takes 52 where 128 x 128 takes 53, and more elsewhere.)
+int product_4(const ProductArgs& a, hipStream_t s) {
+  const double wide = a.wide, small_tiles = tiles_down(a, 128u) * blocks_for(a.wide, 128u);
+  const double few = fmax(tiles_down(a, 16u) * wide * 2.0e-5, used_groups(a) * wide * 2.6e-5);
+  const double tiles = fmax(rounds_of(small_tiles, 512.0) * (1.0 + 0.7 * fmin(1.0, small_tiles / 256.0)), used_groups(a) * wide * 3.0e-5);
+  if (few < tiles && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 32u) <= 1u << 23)
+    return product_tiles<kForward>(mx4_few_kernel<kRows4, 32, 4, 3>, 16, 32, 256, a, s);
+  if (rounds_of(tiles_down(a, 256u) * blocks_for(a.wide, 256u), 256.0) <= 0.62 * rounds_of(small_tiles, 512.0)) return product_tiles<kForward>(mx4_tile_kernel<256, 256, 2, 4>, 256, 256, 512, a, s);
+  return product_tiles<kForward>(mx4_tile_kernel<128, 128, 2, 4>, 128, 128, 512, a, s);
+}
+
+// Rows of 16 bits, the same.  Few rows by 64 columns: 2.9e-5 for 16 rows of a column, 3.3e-5 for a column's weights; by 16 columns where that would leave most compute units idle; tiles of 128 x 128: 2.4 a
+// round.  Measured in bf16, by 64 columns / 16 columns / 128 x 128 / 128 x 256, 7168 -> 2048, us: one group, 1 / 100 rows, 11.1 / 14.7, 7.4 / 32, - / 61, - / 92; 8 of 32 groups, 16 rows, 15 / 28 / 57 / 73; 32 groups, 128 rows,
+// 65 / 100 / 122 / 93; 8 groups, 300 rows, 40 / 87 / 61 / 79; 16 groups, 1000 rows, 122 / 269 / 74 / 107; 4096 rows 429 / - / 207 / 215; 4000 rows in 4 groups - / - / 142 / 122; 2999 rows in 24 groups, 2043 -> 1003,
+// 80 / - / 45 / 36; 8192^3 3510 / - / 1330 / 1020.
 template <Mx4Rows X>
-int product(const ProductArgs& a, hipStream_t s) {
-  return product_tiles<kForward>(mx4_simple_kernel<X>, 16, 16, 64, a, s);
+int product_16(const ProductArgs& a, hipStream_t s) {
+  const double wide = a.wide, small_tiles = tiles_down(a, 128u) * blocks_for(a.wide, 128u), few_tiles = fmax(tiles_down(a, 16u), used_groups(a));
+  const double few = fmax(tiles_down(a, 16u) * wide * 2.9e-5, used_groups(a) * wide * 3.3e-5);
+  if (few < 2.4 * rounds_of(small_tiles, 256.0) && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 16u) <= 1u << 23) {
+    if (few_tiles * blocks_for(a.wide, 64u) <= 64.0) return product_tiles<kForward>(mx4_few_kernel<X, 16, 4, 3>, 16, 16, 256, a, s);
+    return product_tiles<kForward>(mx4_few_kernel<X, 64, 4, 2>, 16, 64, 256, a, s);
+  }
+  if (rounds_of(tiles_down(a, 128u) * blocks_for(a.wide, 256u), 256.0) <= 0.58 * rounds_of(small_tiles, 256.0)) return product_tiles<kForward>(mx4_wide_kernel<X == kRowsF16, 128, 256, 5>, 128, 256, 512, a, s);
+  return product_tiles<kForward>(mx4_wide_kernel<X == kRowsF16, 128, 128, 5>, 128, 128, 512, a, s);
 }
 
 }  // namespace
@@ -30,7 +63,7 @@ int uccl_internal_load_mx4() {
 
 int uccl_internal_product_mx4(const void* product_args, uint32_t x_dtype, hipStream_t s) {
   const ProductArgs& a = *static_cast<const ProductArgs*>(product_args);
-  return x_dtype == UCCL_MX4 ? product<kRows4>(a, s) : x_dtype == UCCL_BF16 ? product<kRowsBf16>(a, s) : product<kRowsF16>(a, s);
+  return x_dtype == UCCL_MX4 ? product_4(a, s) : x_dtype == UCCL_BF16 ? product_16<kRowsBf16>(a, s) : product_16<kRowsF16>(a, s);
 }
 
 extern "C" {

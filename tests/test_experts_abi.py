@@ -242,3 +242,98 @@ def test_kernels_use_no_scratch_memory(tmp_path):
         notes, = [b for b in blocks if part in b]
         assert set(re.findall(r"\.private_segment_fixed_size: +(\d+)", notes)) == {"0"}
         assert set(re.findall(r"\.vgpr_spill_count: +(\d+)", notes)) == {"0"}
+
+
+# ---- what the library is asked to launch: the HIP runtime of tests/hip_stub.c reports it, nothing runs --------------------------------
+
+START, STOP, BAD = 0x6000, 0x7000, 0x5000
+SHAPES = [(1500, 2, 1030, 4000), (700, 5, 520, 2600), (4500, 3, 2060, 1300), (90, 3, 200, 5000), (1300, 1, 4100, 1500), (400, 1, 1900, 3000), (6000, 1, 4200, 900)]   # of tests/test_gpu_experts.py
+
+
+def in_process(scenario, tmp_path):
+    stub = str(tmp_path / "libamdhip64.so.7")
+    subprocess.check_call(["gcc", "-O1", "-shared", "-fPIC", "-w", "-I/opt/rocm/include", "-Wl,-soname,libamdhip64.so.7", os.path.join(HERE, "hip_stub.c"), "-o", stub])
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), scenario, stub], cwd=os.path.dirname(HERE), capture_output=True, text=True, timeout=110)
+    assert r.returncode == 0 and "SCENARIO DONE" in r.stdout, r.stdout[-2000:] + r.stderr[-4000:]
+    return r.stdout
+
+
+def product(rt, kind, n, groups, wide, cols):
+    make = {"mx4": q4, "bf16": rows, "f16": lambda n, c: rows(n, c, F16)}[kind]
+    rt.symbols.clear()
+    assert rt.lib.uccl_group_product(rows(n, wide), make(n, cols), None, q4(groups * wide, cols), M, groups, None) == OK
+    (symbol,), shape = rt.symbols, re.compile(r"(few|tile|wide)_kernelI(?:LNS_7Mx4RowsE\d|Lb\d)?E?Lj(\d+)ELj(\d+)E")
+    return shape.search(symbol).groups()
+
+
+def product_kernels(rt):
+    """Rows of a tile, or columns of one of 16 rows, by what is multiplied; the shapes of the GPU's tests and those that were measured."""
+    few, small, large, wide = ("few", "32", "4"), ("tile", "128", "128"), ("tile", "256", "256"), ("wide", "128", "256")
+    few16, few64, square = ("few", "16", "4"), ("few", "64", "4"), ("wide", "128", "128")
+    for shape, four, sixteen in zip(SHAPES, (small, few, large, few, small, few, large), (square, few64, square, few16, wide, few64, wide)):
+        assert [product(rt, kind, *shape) for kind in ("mx4", "bf16", "f16")] == [four, sixteen, sixteen], shape
+    for shape, four, sixteen in (((16, 32, 2048, 7168), few, few64), ((128, 32, 2048, 7168), few, few64), ((1, 1, 2048, 7168), few, few16), ((300, 8, 2048, 7168), few, few64), ((1000, 16, 2048, 7168), small, square),
+                                 ((4096, 16, 2048, 7168), large, square), ((4000, 4, 2048, 7168), small, wide), ((8190, 16, 7168, 2048), large, wide), ((2999, 24, 1003, 2044), small, wide), ((8192, 1, 8192, 8192), large, wide)):
+        assert [product(rt, kind, *shape) for kind in ("mx4", "bf16")] == [four, sixteen], (shape, product(rt, "mx4", *shape), product(rt, "bf16", *shape))
+    # narrow outputs of very many rows: by 16 rows while that fits a launch, by tiles where these do, refused where nothing does
+    for n, kind in ((1 << 26, "few"), ((1 << 29) - 1024, None)):
+        for x in ("mx4", "bf16"):
+            assert (product(rt, x, n, 1, 5, 500)[0] == "few") == (kind == "few")
+    rt.launches.clear()
+    big = (1 << 31) - 1
+    assert rt.lib.uccl_group_product(rows(big, 8 << 20), q4(big, 64), None, q4(8 << 20, 64), M, 1, None) == TOOBIG and rt.launches == []
+
+
+def test_which_kernel_a_product_is_launched_as(tmp_path):
+    in_process("product_kernels", tmp_path)
+
+
+def timing_events(rt):
+    """A call's start event is on its first launch and its stop on its last; what HIP refuses comes back."""
+    events = []
+    rt.refuse = lambda kernel, stream, start, stop: bool(events.append((start, stop)))
+    lib, grads = rt.lib, many(*[rows(5, 8) for _ in range(130)])
+    calls = {
+        "route": (1, lambda: lib.uccl_route_rows(M, D, None, None, rows(9000, 8), None, route(), None, 0, None)),
+        "route, one group's sums": (1, lambda: lib.uccl_route_rows(M, D, M, D, rows(9, 8), None, route(), None, 0, None)),
+        "route with sums": (2, lambda: lib.uccl_route_rows(M, D, M, D, rows(9000, 8), None, route(), B, 1 << 20, None)),
+        "sums of nothing": (1, lambda: lib.uccl_route_rows(None, None, M, D, rows(0, 8), None, route(), None, 0, None)),
+        "route_grad": (1, lambda: lib.uccl_route_rows_grad(rows(9, 8), rows(9, 8), M, D, None, route(), None)),
+        "balance": (1, lambda: lib.uccl_balance_loss(M, D, M, D, 8, balance(), None)),
+        "plan": (1, lambda: lib.uccl_plan_rows(M, B, D, A, 9, 2, 8, None, 0, None)),
+        "plan of many": (2, lambda: lib.uccl_plan_rows(M, B, D, A, 90000, 2, 8, S, 1 << 20, None)),
+        "quantise": (1, lambda: lib.uccl_quantise_rows(q4(9, 70), None, rows(9, 70), None)),
+        "product": (1, lambda: lib.uccl_group_product(rows(9, 3), q4(9, 64), None, q4(12, 64), M, 4, None)),
+        "norm": (4, lambda: lib.uccl_gradient_norm(M, grads, 130, B, 1 << 20, None)),
+        "norm of nothing": (1, lambda: lib.uccl_gradient_norm(M, None, 0, B, 1 << 20, None)),
+        "clip": (3, lambda: lib.uccl_gradient_clip(grads, grads, 130, M, clip(), None)),
+    }
+    for name, (launches, call) in calls.items():
+        events.clear()
+        assert lib.uccl_time_next_launch(START, STOP) == OK and call() == OK, name
+        assert len(events) == launches and events[0][0] == START and events[-1][1] == STOP and not any(start for start, _ in events[1:]), (name, events)
+        events.clear()
+        assert call() == OK and not any(map(any, events)), (name, events)   # once only
+    rt.refuse = lambda kernel, stream, start, stop: BAD in (start, stop)
+    for name, (launches, call) in calls.items():
+        for start, stop in ((START, BAD), (BAD, STOP)):
+            rt.launches.clear()
+            assert lib.uccl_time_next_launch(start, stop) == OK and call() == pkg.UCCL_ELAUNCH and not rt.launches, name
+    rt.refuse = lambda *a: True
+    for name, (_, call) in calls.items():
+        assert call() == pkg.UCCL_ELAUNCH, name
+    assert b"as the test asked" in lib.uccl_last_error_detail()
+
+
+def test_timing_events_span_a_call_of_several_launches(tmp_path):
+    in_process("timing_events", tmp_path)
+
+
+if __name__ == "__main__":
+    import test_host_launches
+    runtime = test_host_launches.Runtime(sys.argv[2])
+    for name, (res, args) in {**pkg.ROWS_SIGNATURES, **pkg.EXPERTS_SIGNATURES}.items():
+        fn = getattr(runtime.lib, name)
+        fn.restype, fn.argtypes = res, args
+    globals()[sys.argv[1]](runtime)
+    print("SCENARIO DONE")

@@ -481,6 +481,29 @@ def test_product(uccl, kind, rows, groups, wide, cols):
         assert torch.equal(margin(y), around) and torch.equal(y[rows:].view(torch.uint8), end.view(torch.uint8))
 
 
+# sums long enough for every kernel's steady state, by every kernel (tests/test_experts_abi.py has which): rows, groups, columns, depth
+DEEP = [(1500, 2, 1030, 4000), (700, 5, 520, 2600), (4500, 3, 2060, 1300), (90, 3, 200, 5000), (1300, 1, 4100, 1500), (400, 1, 1900, 3000), (6000, 1, 4200, 900)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,groups,wide,cols", DEEP)
+def test_product_of_long_sums(uccl, kind, rows, groups, wide, cols):
+    g = gen(rows + wide)
+    w, ws = random_mx4(g, groups * wide, cols)
+    dw = decode(w, ws, cols).view(groups, wide, cols)
+    w, ws = w.view(torch.uint8).unflatten(0, (groups, wide)).view(E2M1), ws.view(torch.uint8).unflatten(0, (groups, wide)).view(E8M0)
+    x, xs, dx = make_x(g, kind, rows, cols)
+    index = torch.randperm(rows, device="cuda", generator=g).to(torch.int32)
+    index[::17] = -1
+    ends = ends_of(rows, groups, rows)
+    offsets, y, again = torch.tensor(ends, dtype=torch.int32, device="cuda"), aligned(rows, wide, torch.float32), aligned(rows, wide, torch.float32)
+    for out in (y, again):
+        uccl.uccl_group_product(out, x, w, offsets, index=index, x_scales=xs, w_scales=ws)
+    want, mag = product_reference(dx, dw, index, ends)
+    close(y, want, mag, cols, kind)
+    assert torch.equal(y, again)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_product_of_an_odd_number_of_columns_by_the_struct(uccl, kind):
     """The half byte behind the last element holds anything."""
