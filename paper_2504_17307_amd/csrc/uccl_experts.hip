@@ -83,42 +83,57 @@ PlanShape plan_shape(uint64_t choices) {
 // ---- gradients --------------------------------------------------------------------------------------
 
 constexpr uint32_t kGradientGroups = 4096, kLeastShare = 1024;   // workgroups of a call, about, and pieces of a workgroup at least
+constexpr uint64_t kStayInCaches = 32ull << 20;                  // outputs of more than this are stored past them
 
 uint32_t pieces_of(const uccl_rows* m) { return blocks_for(row_bytes(m), 16u); }
 
-// Goes through the matrices that have elements, as many at a time as a launch takes: f(args, workgroups, whether they are the last).
-template <class F>
-int over_matrices(const uccl_rows* in, const uccl_rows* out, uint32_t n, F f) {
+// How a call's matrices are shared out: pieces of a workgroup, and how many matrices that have elements are one row, and are not.
+struct Shares {
+  uint32_t share, flat, strided;
+  uint64_t bytes;
+};
+// Rows that follow each other without a gap are one (whose elements have to be counted in 32 bits).
+bool is_flat(const uccl_rows* in, const uccl_rows* out) {
+  if (in->rows == 1u) return true;
+  return in->stride == row_bytes(in) && (out == nullptr || out->stride == in->stride) && static_cast<uint64_t>(in->rows) * in->cols <= 0xFFFFFFFFull;
+}
+Shares shares_of(const uccl_rows* in, const uccl_rows* out, uint32_t n) {
   uint64_t pieces = 0;
-  uint32_t some = 0;
+  Shares s{};
   for (uint32_t i = 0; i < n; ++i) {
     const uint64_t mine = static_cast<uint64_t>(in[i].rows) * pieces_of(in + i);
     pieces += mine;
-    some += mine != 0u;
+    if (mine != 0u) ++(is_flat(in + i, out == nullptr ? nullptr : out + i) ? s.flat : s.strided);
   }
-  GradientArgs a{};
-  uint64_t share = (pieces / kGradientGroups + kLeastShare) / kLeastShare * kLeastShare;
-  a.share = static_cast<uint32_t>(share < 1u << 30 ? share : 1u << 30);
+  const uint64_t share = (pieces / kGradientGroups + kLeastShare) / kLeastShare * kLeastShare;
+  s.share = static_cast<uint32_t>(share < 1u << 30 ? share : 1u << 30);
+  s.bytes = pieces * 16u;
+  return s;
+}
+
+// Goes through those of one kind, as many at a time as a launch takes: f(args, workgroups, whether they are the last of `left`).
+template <bool FLAT, class F>
+int over_matrices(const uccl_rows* in, const uccl_rows* out, uint32_t n, uint32_t share, uint32_t left, F f) {
+  GradientArgs<FLAT> a{};
+  a.share = share;
   uint64_t groups = 0;
-  for (uint32_t i = 0; i < n; ++i) {
-    const uint32_t p = pieces_of(in + i);
-    const uint64_t mine = static_cast<uint64_t>(in[i].rows) * p;
-    if (mine == 0u) continue;
-    Matrix& m = a.m[a.n];
-    m = Matrix{static_cast<const char*>(in[i].data), out == nullptr ? nullptr : static_cast<char*>(out[i].data), in[i].stride, out == nullptr ? 0u : out[i].stride, in[i].rows, in[i].cols, p};
-    // rows that follow each other without a gap are one (its elements have to be counted in 32 bits)
-    const uint64_t all = static_cast<uint64_t>(in[i].rows) * in[i].cols;
-    if (in[i].rows > 1u && in[i].stride == row_bytes(in + i) && (out == nullptr || out[i].stride == in[i].stride) && all <= 0xFFFFFFFFull) {
-      m.rows = 1u;
-      m.cols = static_cast<uint32_t>(all);
-      m.pieces = static_cast<uint32_t>(mine);
-    }
+  for (uint32_t i = 0; i < n && left != 0u; ++i) {
+    const uint64_t mine = static_cast<uint64_t>(in[i].rows) * pieces_of(in + i);
+    if (mine == 0u || is_flat(in + i, out == nullptr ? nullptr : out + i) != FLAT) continue;
+    a.in[a.n] = static_cast<const char*>(in[i].data);
+    a.out[a.n] = out == nullptr ? nullptr : static_cast<char*>(out[i].data);
     a.dtype[a.n] = static_cast<uint8_t>(in[i].dtype == UCCL_F32 ? 0u : in[i].dtype == UCCL_BF16 ? 1u : 2u);
+    a.cols[a.n] = FLAT ? static_cast<uint32_t>(static_cast<uint64_t>(in[i].rows) * in[i].cols) : in[i].cols;
+    if constexpr (!FLAT) {
+      a.in_stride[a.n] = in[i].stride;
+      a.out_stride[a.n] = out == nullptr ? 0u : out[i].stride;
+      a.rows[a.n] = in[i].rows;
+    }
     a.first[a.n++] = static_cast<uint32_t>(groups);
-    groups += (mine + a.share - 1u) / a.share;
-    --some;
-    if (a.n == kMatrices || some == 0u) {
-      const int e = f(a, groups, some == 0u);
+    groups += (mine + share - 1u) / share;
+    const bool last = --left == 0u;
+    if (a.n == GradientArgs<FLAT>::MOST || last) {
+      const int e = f(a, groups, last);
       if (e != UCCL_OK) return e;
       a.n = 0u;
       groups = 0u;
@@ -250,11 +265,14 @@ int uccl_gradient_norm(float* norm, const uccl_rows* grads, uint32_t n, void* sc
   Launches go;
   double* const parts = static_cast<double*>(scratch);
   uint64_t done = 0;
-  const int code = over_matrices(grads, nullptr, n, [&](GradientArgs& a, uint64_t groups, bool) {
+  const Shares shares = shares_of(grads, nullptr, n);
+  auto add = [&](auto& a, uint64_t groups, auto kernel) {
     a.parts = parts + done;
     done += groups;
-    return go(false, square_sum_kernel, groups, kGradientThreads, s, a);
-  });
+    return go(false, kernel, groups, kGradientThreads, s, a);
+  };
+  int code = over_matrices<true>(grads, nullptr, n, shares.share, shares.flat, [&](auto& a, uint64_t groups, bool) { return add(a, groups, square_sum_kernel<true>); });
+  if (code == UCCL_OK) code = over_matrices<false>(grads, nullptr, n, shares.share, shares.strided, [&](auto& a, uint64_t groups, bool) { return add(a, groups, square_sum_kernel<false>); });
   return code != UCCL_OK ? code : go(true, square_root_kernel, 1, 1024, s, norm, static_cast<const double*>(parts), static_cast<uint32_t>(done));
 }
 
@@ -269,10 +287,21 @@ int uccl_gradient_clip(const uccl_rows* out, const uccl_rows* grads, uint32_t n,
   if (norm == nullptr) return UCCL_EINVAL;
   if (misaligned(norm, 4)) return UCCL_EALIGN;
   Launches go;
-  return over_matrices(grads, out, n, [&](GradientArgs& a, uint64_t groups, bool last) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const Shares shares = shares_of(grads, out, n);
+  const bool once = shares.bytes > kStayInCaches;
+  auto clip = [&](auto& a, uint64_t groups, bool last, auto kernel) {
     a.norm = norm;
     a.most = opts->most;
-    return go(last, gradient_clip_kernel, groups, kGradientThreads, static_cast<hipStream_t>(stream), a);
+    return go(last, kernel, groups, kGradientThreads, s, a);
+  };
+  e = over_matrices<true>(grads, out, n, shares.share, shares.flat, [&](auto& a, uint64_t groups, bool last) {
+    last = last && shares.strided == 0u;
+    return once ? clip(a, groups, last, gradient_clip_kernel<true, true>) : clip(a, groups, last, gradient_clip_kernel<true, false>);
+  });
+  if (e != UCCL_OK) return e;
+  return over_matrices<false>(grads, out, n, shares.share, shares.strided, [&](auto& a, uint64_t groups, bool last) {
+    return once ? clip(a, groups, last, gradient_clip_kernel<false, true>) : clip(a, groups, last, gradient_clip_kernel<false, false>);
   });
 }
 

@@ -309,7 +309,7 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
 // wavefront has had its last fragment of the step, a quarter into its products, the step AHEAD further takes its place.
 template <bool F16, uint32_t BM, uint32_t BN, uint32_t AHEAD>
 __global__ __launch_bounds__(512) void mx4_wide_kernel(ProductArgs a) {
-  constexpr uint32_t THREADS = 512, SIDE = 16u, NA = BM / 32u, NB = BN / 64u, A_LOADS = BM / 64u, B_LOADS = BN / 64u, FROM = NA / 4u == 0u ? 1u : NA / 4u;
+  constexpr uint32_t SIDE = 16u, NA = BM / 32u, NB = BN / 64u, A_LOADS = BM / 64u, B_LOADS = BN / 64u, FROM = NA / 4u == 0u ? 1u : NA / 4u;
   constexpr uint32_t A_STEP = BM * 128u, B_STAGE = BN * 128u, S_STAGE = 2048u;   // scales: 8 bytes of 256 rows
   static_assert(AHEAD >= 3u && AHEAD <= 5u);
   __shared__ __align__(1024) char lds_a[AHEAD * A_STEP], lds_b[2u * B_STAGE], lds_s[2u * S_STAGE];

@@ -293,6 +293,7 @@ def timing_events(rt):
     events = []
     rt.refuse = lambda kernel, stream, start, stop: bool(events.append((start, stop)))
     lib, grads = rt.lib, many(*[rows(5, 8) for _ in range(130)])
+    most, gaps = many(*[rows(5, 8) for _ in range(320)]), many(rows(1, 9), *[rows(5, 8, stride=32) for _ in range(130)])
     calls = {
         "route": (1, lambda: lib.uccl_route_rows(M, D, None, None, rows(9000, 8), None, route(), None, 0, None)),
         "route, one group's sums": (1, lambda: lib.uccl_route_rows(M, D, M, D, rows(9, 8), None, route(), None, 0, None)),
@@ -304,9 +305,12 @@ def timing_events(rt):
         "plan of many": (2, lambda: lib.uccl_plan_rows(M, B, D, A, 90000, 2, 8, S, 1 << 20, None)),
         "quantise": (1, lambda: lib.uccl_quantise_rows(q4(9, 70), None, rows(9, 70), None)),
         "product": (1, lambda: lib.uccl_group_product(rows(9, 3), q4(9, 64), None, q4(12, 64), M, 4, None)),
-        "norm": (4, lambda: lib.uccl_gradient_norm(M, grads, 130, B, 1 << 20, None)),
+        "norm": (2, lambda: lib.uccl_gradient_norm(M, grads, 130, B, 1 << 20, None)),
         "norm of nothing": (1, lambda: lib.uccl_gradient_norm(M, None, 0, B, 1 << 20, None)),
-        "clip": (3, lambda: lib.uccl_gradient_clip(grads, grads, 130, M, clip(), None)),
+        "clip": (1, lambda: lib.uccl_gradient_clip(grads, grads, 130, M, clip(), None)),
+        "norm of many": (4, lambda: lib.uccl_gradient_norm(M, most, 320, B, 1 << 20, None)),
+        "clip of many": (3, lambda: lib.uccl_gradient_clip(most, most, 320, M, clip(), None)),
+        "clip of rows with gaps": (4, lambda: lib.uccl_gradient_clip(gaps, gaps, 131, M, clip(), None)),
     }
     for name, (launches, call) in calls.items():
         events.clear()
