@@ -75,11 +75,17 @@ int uccl_quantise_rows(const uccl_rows* q, const uccl_rows* values, const uccl_r
   if (q->dtype != UCCL_MX4 || !is_float(x->dtype) || !same_shape(q, x) || (values != nullptr && (values->dtype != x->dtype || !same_shape(values, x)))) return UCCL_EINVAL;
   if (x->rows == 0u || x->cols == 0u) return UCCL_OK;
   if (q->rows > 1u && q->scale_stride < blocks_for(q->cols, kMx4Block)) return UCCL_EINVAL;   // every row writes its own scales
+  const hipStream_t s = static_cast<hipStream_t>(stream);
   return with_type(x->dtype, [&](auto t) {
     using T = decltype(t);
-    const uint32_t pieces = blocks_for(x->cols, Piece<T>::N), groups = blocks_for(pieces, 256u);
-    const QuantiseArgs a{rows_of(q), rows_of(values), rows_of(x), x->rows, x->cols, pieces, groups};
-    return launch(quantise_kernel<T, false>, static_cast<uint64_t>(x->rows) * groups, 256, static_cast<hipStream_t>(stream), a);
+    constexpr uint32_t share = kMx4Block / Piece<T>::N;
+    const uint32_t pieces = blocks_for(x->cols, Piece<T>::N), padded = (pieces + share - 1u) / share * share;
+    const QuantiseArgs a{rows_of(q), rows_of(values), rows_of(x), x->cols, pieces, padded, 256u / padded, 256u % padded, static_cast<uint64_t>(x->rows) * padded};
+    const uint64_t groups = (a.all + 255u) / 256u;
+    // few pieces: one a thread, so that all compute units have some
+    if (groups <= 1024u) return launch(quantise_kernel<T, 1, false>, groups, 256, s, a);
+    if (values != nullptr && row_bytes(values) * values->rows > 32ull << 20) return launch(quantise_kernel<T, 4, true>, (groups + 3u) / 4u, 256, s, a);
+    return launch(quantise_kernel<T, 4, false>, (groups + 3u) / 4u, 256, s, a);
   });
 }
 

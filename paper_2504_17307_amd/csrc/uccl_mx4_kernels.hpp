@@ -7,54 +7,122 @@ namespace {
 
 constexpr uint32_t kMx4Block = 32;
 
+// Four bytes, two elements each, times 2^(byte - 127) as eight bf16: exact, for bf16 has all these powers.
+__device__ __forceinline__ u32x4 widen_e2m1(uint32_t eight, float scale) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 3))};
+}
+
+// The same as eight f16, which is exact for scales of 2^-23 to 2^13 (a half of 2^-23 is f16's least number, 6 x 2^13 below its greatest) and NaN.
+__device__ __forceinline__ u32x4 widen_e2m1_f16(uint32_t eight, float scale) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(eight, scale, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(eight, scale, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(eight, scale, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(eight, scale, 3))};
+}
 struct QuantiseArgs {
-  Rows q, values, x;   // values.data: nullptr if there is none
-  uint32_t rows, cols, pieces, groups;   // pieces of a row of x, workgroups of a row
+  Rows q, values, x;      // values.data: nullptr if there is none
+  uint32_t cols, pieces;  // pieces of a row of x
+  uint32_t padded, down, along;   // pieces of a row with those that would complete its last block; how many rows and pieces further 256 pieces are
+  uint64_t all;           // rows padded
 };
 
-// A lane has 16 bytes of a row, and the neighbours that share a block (4 of 16-bit elements, 8 of 32-bit) its greatest element.  x / s is exact:
-// s is a power of two.  What is below the smallest normal number then is 0 in 4 bits all the same.
-template <class T, bool ONCE>
+// The greatest magnitude of a piece, as a binary32's bits.
+__device__ __forceinline__ uint32_t greatest(const Piece<float>& p) {
+  const u32x4 v = __builtin_bit_cast(u32x4, p) & 0x7FFFFFFFu;
+  return max(max(v.x, v.y), max(v.z, v.w));
+}
+template <class T>
+__device__ __forceinline__ uint32_t greatest(const Piece<T>& p) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  const u32x4 v = __builtin_bit_cast(u32x4, p) & 0x7FFF7FFFu;
+  auto pairs = [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y))); };
+  const uint32_t both = pairs(pairs(v.x, v.y), pairs(v.z, v.w));
+  return __builtin_bit_cast(uint32_t, widen(__builtin_bit_cast(T, static_cast<uint16_t>(max(both >> 16, both & 0xFFFFu)))));
+}
+
+// Elements divided by s, as the instructions for it round them: to nearest even, 6 at most.  s as a binary32's bits: an exponent of 0 is 2^-127 to them.
+__device__ __forceinline__ uint32_t to_e2m1(const Piece<float>& p, float s) {
+  uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, p.v[0], p.v[1], s, 0);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, p.v[2], p.v[3], s, 1);
+}
+__device__ __forceinline__ uint32_t to_e2m1(const Piece<__bf16>& p, float s) {
+  uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, bf16x2{p.v[0], p.v[1]}, s, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, bf16x2{p.v[2], p.v[3]}, s, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, bf16x2{p.v[4], p.v[5]}, s, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, bf16x2{p.v[6], p.v[7]}, s, 3);
+}
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t to_e2m1(const Piece<_Float16>& p, float s) {
+  uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(0u, f16x2{p.v[0], p.v[1]}, s, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, f16x2{p.v[2], p.v[3]}, s, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, f16x2{p.v[4], p.v[5]}, s, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, f16x2{p.v[6], p.v[7]}, s, 3);
+}
+
+// What codes stand for: exact in f32 and bf16, which have all these powers of two, and in f16, whose elements are multiples of 2^-24 below 2^16.
+__device__ __forceinline__ void from_e2m1(uint32_t codes, float s, Piece<float>& p) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 1);
+  p.v[0] = a.x;
+  p.v[1] = a.y;
+  p.v[2] = b.x;
+  p.v[3] = b.y;
+}
+__device__ __forceinline__ void from_e2m1(uint32_t codes, float s, Piece<__bf16>& p) { p = __builtin_bit_cast(Piece<__bf16>, widen_e2m1(codes, s)); }
+__device__ __forceinline__ void from_e2m1(uint32_t codes, float s, Piece<_Float16>& p) { p = __builtin_bit_cast(Piece<_Float16>, widen_e2m1_f16(codes, s)); }
+
+// A lane has 16 bytes of a row, and the neighbours that share a block (4 of 16-bit elements, 8 of 32-bit) its greatest element; NV of them a lane, every load
+// issued before the first is waited for.
+template <class T, uint32_t NV, bool ONCE>
 __global__ __launch_bounds__(256) void quantise_kernel(QuantiseArgs a) {
   constexpr uint32_t N = Piece<T>::N, SHARE = kMx4Block / N;
-  const uint64_t row = blockIdx.x / a.groups;
-  const uint32_t piece = blockIdx.x % a.groups * 256u + threadIdx.x;
-  Piece<T> x = load_piece_once<T>(a.x.data + row * a.x.stride, min(piece, a.pieces - 1u));
-  const uint32_t valid = valid_of<T>(piece, a.pieces, a.cols);
-  blank(x, valid);
-  uint32_t most = 0u;
+  const uint64_t first = blockIdx.x * static_cast<uint64_t>(256u * NV) + threadIdx.x;
+  uint64_t row = first >> 32 == 0u ? static_cast<uint32_t>(first) / a.padded : first / a.padded;
+  uint32_t at = static_cast<uint32_t>(first - row * a.padded);
+  Piece<T> x[NV];
+  uint64_t rows[NV];
+  uint32_t pieces[NV];
 #pragma unroll
-  for (uint32_t i = 0; i < N; ++i) most = max(most, __builtin_bit_cast(uint32_t, widen(x.v[i])) & 0x7FFFFFFFu);
-#pragma unroll
-  for (uint32_t d = 1; d < SHARE; d <<= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), static_cast<int>(d))));
-  const bool finite = most < 0x7F800000u;
-  const uint32_t exponent = most >> 23, byte = !finite ? 255u : exponent < 2u ? 0u : exponent - 2u;
-  const float by = finite ? __builtin_bit_cast(float, (254u - byte) << 23) : 0.0f;                                    // 1 / s
-  const float s = !finite ? __builtin_nanf("") : byte == 0u ? 0x1p-127f : __builtin_bit_cast(float, byte << 23);
-  uint32_t codes = 0u;
-  Piece<T> out;
-#pragma unroll
-  for (uint32_t i = 0; i < N; ++i) {
-    const float v = finite ? widen(x.v[i]) * by : 0.0f, m = fminf(fabsf(v), 6.0f);
-    // the steps are 0.5 below 2, 1 below 4, 2 above
-    const uint32_t number = m < 2.0f ? static_cast<uint32_t>(__builtin_rintf(m * 2.0f)) : m < 4.0f ? static_cast<uint32_t>(__builtin_rintf(m)) + 2u : static_cast<uint32_t>(__builtin_rintf(m * 0.5f)) + 4u;
-    const uint32_t sign = __builtin_bit_cast(uint32_t, v) >> 31;
-    codes |= (number | sign << 3) << (4u * i);
-    const float value = number < 4u ? number * 0.5f : number == 4u ? 2.0f : number == 5u ? 3.0f : number == 6u ? 4.0f : 6.0f;
-    out.v[i] = static_cast<T>((sign != 0u ? -value : value) * s);
+  for (uint32_t k = 0; k < NV; ++k) {
+    rows[k] = row;
+    pieces[k] = first + k * 256u < a.all ? at : 0xFFFFFFFFu;   // behind the last row: nothing
+    if (pieces[k] < a.pieces) x[k] = load_piece_once<T>(a.x.data + row * a.x.stride, at);
+    else x[k] = Piece<T>{};
+    row += a.down;
+    at += a.along;
+    if (at >= a.padded) {
+      at -= a.padded;
+      ++row;
+    }
   }
-  if (valid == 0u) return;
-  char* q = a.q.data + row * a.q.stride + piece * static_cast<uint64_t>(N / 2u);
-  if (valid >= N) {
-    if constexpr (N == 8u) *reinterpret_cast<uint32_t*>(q) = codes;
-    else *reinterpret_cast<uint16_t*>(q) = static_cast<uint16_t>(codes);
-  } else {
 #pragma unroll
-    for (uint32_t i = 0; i < N; i += 2u)
-      if (i < valid) q[i / 2u] = static_cast<char>(codes >> (4u * i));
+  for (uint32_t k = 0; k < NV; ++k) {
+    const uint32_t valid = valid_of<T>(pieces[k], a.pieces, a.cols);
+    blank(x[k], valid);
+    uint32_t most = greatest(x[k]);
+    most = max(most, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(most), 0xB1, 0xF, 0xF, true)));   // a neighbour's
+    most = max(most, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(most), 0x4E, 0xF, 0xF, true)));   // the other pair's
+    if constexpr (SHARE == 8u) most = max(most, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(most), 0x141, 0xF, 0xF, true)));   // of 8 lanes, the other end's
+    const bool finite = most < 0x7F800000u;
+    const uint32_t exponent = most >> 23, byte = !finite ? 255u : exponent < 2u ? 0u : exponent - 2u;
+    const float s = __builtin_bit_cast(float, byte << 23);
+    const uint32_t codes = finite ? to_e2m1(x[k], s) : 0u;
+    if (valid == 0u) continue;
+    char* q = a.q.data + rows[k] * a.q.stride + pieces[k] * static_cast<uint64_t>(N / 2u);
+    if (valid >= N) {
+      if constexpr (N == 8u) *reinterpret_cast<uint32_t*>(q) = codes;
+      else *reinterpret_cast<uint16_t*>(q) = static_cast<uint16_t>(codes);
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < N; i += 2u)
+        if (i < valid) q[i / 2u] = static_cast<char>(codes >> (4u * i));
+    }
+    if (threadIdx.x % SHARE == 0u) reinterpret_cast<uint8_t*>(a.q.scales + rows[k] * a.q.scale_stride)[pieces[k] / SHARE] = static_cast<uint8_t>(byte);
+    if (a.values.data != nullptr) {
+      Piece<T> out;
+      from_e2m1(codes, s, out);
+      store_piece<ONCE>(a.values.data + rows[k] * a.values.stride, pieces[k], out, valid);
+    }
   }
-  if (threadIdx.x % SHARE == 0u) reinterpret_cast<uint8_t*>(a.q.scales + row * a.q.scale_stride)[piece / SHARE] = static_cast<uint8_t>(byte);
-  if (a.values.data != nullptr) store_piece<ONCE>(a.values.data + row * a.values.stride, piece, out, valid);
 }
 
 // ---- products ---------------------------------------------------------------------------------------
@@ -66,12 +134,6 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // Rows in 4 bits too: the matrix instruction for them takes the blocks' scales.  It has the products of a block exactly and adds the four
 // blocks one after the other in binary32.
 enum Mx4Rows : uint32_t { kRows4, kRowsBf16, kRowsF16 };
-
-// Four bytes, two elements each, times 2^(byte - 127) as eight bf16: exact, for bf16 has all these powers.
-__device__ __forceinline__ u32x4 widen_e2m1(uint32_t eight, float scale) {
-  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 1)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 3))};
-}
 
 // f16 has 11 bits, which are two bf16 exactly: the nearest one and what is left.
 __device__ __forceinline__ void split_f16(u32x4 v, u32x4& high, u32x4& low) {
@@ -98,11 +160,7 @@ __device__ __forceinline__ void load_word_to_lds(const char* from, uint32_t to) 
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "m0");
 }
 
-// The same as eight f16, which is exact for scales of 2^-23 to 2^13 (a half of 2^-23 is f16's least number, 6 x 2^13 below its greatest) and NaN.
-__device__ __forceinline__ u32x4 widen_e2m1_f16(uint32_t eight, float scale) {
-  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(eight, scale, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(eight, scale, 1)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(eight, scale, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(eight, scale, 3))};
-}
+// Scales by which weights are exact as f16.
 __device__ __forceinline__ bool exact_in_f16(uint32_t scale) { return scale - (127u - 23u) <= 36u || scale == 255u; }
 
 // ---- tiles, rows in 4 bits --------------------------------------------------------------------------

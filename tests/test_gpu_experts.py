@@ -409,8 +409,27 @@ def test_quantise_of_every_middle_and_its_neighbours(uccl):
         assert torch.equal(s.view(torch.uint8).cpu().long(), byte) and torch.equal(codes_of(q, 32).cpu().long(), number), e
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_quantise_of_every_16_bit_value(uccl, dtype):
+    """Beside a greatest element of every exponent: all values up to twice that."""
+    t = T[dtype]
+    every = torch.arange(65536, dtype=torch.int32).to(torch.uint16).view(t).cuda()
+    every = every[every.isfinite()]
+    for e in [None] + list(range(-130, 128, 3) if dtype == "bf16" else range(-24, 16)):
+        most = torch.tensor(0.0 if e is None else 2.0 ** e, device="cuda").to(t)
+        v = every[every.abs() < 2 * most] if e is not None else every
+        x = torch.zeros(v.numel(), 32, dtype=t, device="cuda")
+        x[:, 31], x[:, 3] = most, v
+        _, q, s = mx4_rows(v.numel(), 32)
+        values = torch.zeros_like(x)
+        uccl.uccl_quantise_rows(q, s, x, values=values)
+        number, byte = quantise_reference(x)
+        assert torch.equal(s.view(torch.uint8).cpu().long(), byte) and torch.equal(codes_of(q, 32).cpu().long(), number), e
+        assert torch.equal(values.double(), decode(q, s, 32)), e
+
+
 def test_quantise_many_rows_and_few_columns(uccl):
-    for rows, cols in ((5000, 33), (70000, 1), (3, 40000)):
+    for rows, cols in ((5000, 33), (70000, 1), (3, 40000), (4000, 999), (300, 7171), (9, 32)):
         x = normal(gen(rows), rows, cols, torch.bfloat16)
         _, q, s = mx4_rows(rows, cols)
         uccl.uccl_quantise_rows(q, s, x)
