@@ -383,6 +383,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   constexpr uint32_t TILE = kPlanThreads * ROUNDS;
   __shared__ uint32_t seen[kPlanWaves][kMostExperts];   // of the tile, by wavefront; then the first place of each wavefront
   __shared__ uint32_t next[kMostExperts];               // the place of the workgroup's next choice of an expert
+  __shared__ uint32_t totals[kMostExperts];
   __shared__ uint32_t sums[kPlanWaves];
   const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
   const uint64_t begin = static_cast<uint64_t>(blockIdx.x) * a.share, end = min(begin + a.share, static_cast<uint64_t>(a.choices));
@@ -417,6 +418,24 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   read_tile(begin);
   rank_tile();
   __syncthreads();
+  // what the experts have in all, and in earlier workgroups
+  if (a.counts != nullptr) {
+    const uint32_t all = gridDim.x * a.n_experts, earlier = blockIdx.x * a.n_experts, further = kPlanThreads % a.n_experts;
+    for (uint32_t e = threadIdx.x; e < a.n_experts; e += kPlanThreads) totals[e] = next[e] = 0u;
+    __syncthreads();
+    uint32_t e = threadIdx.x % a.n_experts;
+#pragma unroll 8
+    for (uint32_t i = threadIdx.x; i < all; i += kPlanThreads) {
+      const uint32_t n = a.counts[i];
+      if (n != 0u) {
+        atomicAdd(&totals[e], n);
+        if (i < earlier) atomicAdd(&next[e], n);
+      }
+      e += further;
+      if (e >= a.n_experts) e -= a.n_experts;
+    }
+    __syncthreads();
+  }
   // the experts' first rows: two neighbouring experts a thread
   uint32_t total[2], before[2];
 #pragma unroll
@@ -425,11 +444,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     total[i] = before[i] = 0u;
     if (e < a.n_experts) {
       if (a.counts != nullptr) {
-        for (uint32_t b = 0; b < gridDim.x; ++b) {
-          const uint32_t n = a.counts[static_cast<uint64_t>(b) * a.n_experts + e];
-          total[i] += n;
-          if (b < blockIdx.x) before[i] += n;
-        }
+        total[i] = totals[e];
+        before[i] = next[e];
       } else {
 #pragma unroll
         for (uint32_t w = 0; w < kPlanWaves; ++w) total[i] += seen[w][e];
