@@ -38,26 +38,36 @@ class Launches {
 
 constexpr uint32_t kRouteGroups = 256;   // that add up counts and probabilities, at most: one a compute unit
 
-// How many tokens a workgroup of kernels with SUMS has at a time.
-uint32_t tokens_at_a_time(uint32_t cols) { return cols <= 256u ? 32u : 8u; }
-uint32_t route_groups(uint32_t tokens, uint32_t cols) {
-  const uint32_t n = blocks_for(tokens, tokens_at_a_time(cols));
-  return n < kRouteGroups ? n : kRouteGroups;
-}
+// Few tokens: as many lanes for each as it has pieces, up to 64; many, which fill the machine: 16, where what goes over the lanes is done for four tokens at once.  Measured, 16 / as many,
+// 256 experts, with 8 slots, us: f32, 1 / 512 / 4096 / 32768 tokens, 4.8 / 5.2 / 5.5 / 20 against 3.5 / 3.6 / 6.8 / 31; the gradient 4.5 / 4.8 / 5.4 / 16 against 3.2 / 3.6 / 5.6 / 20; bf16, 6.1 / 6.2 / 6.5 / 23
+// against 4.2 / 4.7 / 6.5 / 22.5.
+bool takes_16_lanes(uint32_t tokens, uint32_t cols) { return cols <= 256u && tokens > 2048u; }
 
 // Calls f with the lanes of a token and the pieces of a lane, for rows of `cols` elements of T.
 template <class T, class F>
-int with_lanes(uint32_t cols, F f) {
+auto with_lanes(uint32_t tokens, uint32_t cols, F f) {
   constexpr uint32_t N = Piece<T>::N;
   using std::integral_constant;
+  using One = integral_constant<uint32_t, 1>;
+  using Two = integral_constant<uint32_t, 2>;
   using L16 = integral_constant<uint32_t, 16>;
   using L64 = integral_constant<uint32_t, 64>;
-  if (cols <= 16u * N) return f(L16{}, integral_constant<uint32_t, 1>{});
-  if (cols <= 32u * N) return f(L16{}, integral_constant<uint32_t, 2>{});
+  if (cols <= 16u * N) return f(L16{}, One{});
+  if (takes_16_lanes(tokens, cols)) {
+    if (cols <= 32u * N) return f(L16{}, Two{});
+    if constexpr (N == 4u) return f(L16{}, integral_constant<uint32_t, 4>{});
+  }
+  if (cols <= 32u * N) return f(integral_constant<uint32_t, 32>{}, One{});
+  if (cols <= 64u * N) return f(L64{}, One{});
   if constexpr (N == 4u)
-    if (cols <= 64u * N) return f(L16{}, integral_constant<uint32_t, 4>{});
-  if (cols <= 512u) return f(L64{}, integral_constant<uint32_t, 8u / N>{});
+    if (cols <= 512u) return f(L64{}, Two{});
   return f(L64{}, integral_constant<uint32_t, 16u / N>{});
+}
+
+// Workgroups of kernels that add up counts and probabilities.  (As many as any type needs: a call's scratch memory does not go by the type.)
+uint32_t route_groups(uint32_t tokens, uint32_t cols) {
+  const uint32_t lanes = cols <= 64u || takes_16_lanes(tokens, cols) ? 16u : cols <= 128u ? 32u : 64u, n = blocks_for(tokens, kRouteSumThreads / lanes);
+  return n < kRouteGroups ? n : kRouteGroups;
 }
 
 int check_route(const uccl_rows* scores, const uccl_route_opts* o) {
@@ -69,15 +79,18 @@ int check_route(const uccl_rows* scores, const uccl_route_opts* o) {
 
 // ---- the order of rows ------------------------------------------------------------------------------
 
-constexpr uint32_t kPlanTile = 2u * kPlanThreads, kPlanGroups = 128;   // choices a workgroup has at a time, workgroups at most
+constexpr uint32_t kPlanGroups = 128;   // workgroups, at most
 
+// How the choices are shared out.  A workgroup has 1024 or 2048 at a time: more of them at a time are fewer workgroups, each of which reads the others' counts.  Measured, 1024 / 2048 at a
+// time, 256 experts, us: 1024 choices 4.1 / 5.2, 2048 6.6 / 5.5 (one launch), 4096 7.6 / 8.7, 32768 11.6 / 11.2, 131072 26.5 / 18.6.
 struct PlanShape {
-  uint32_t groups, share;
+  uint32_t rounds, groups, share;
 };
-PlanShape plan_shape(uint64_t choices) {
-  const uint64_t tiles = (choices + kPlanTile - 1u) / kPlanTile, each = (tiles + kPlanGroups - 1u) / kPlanGroups;
-  if (each == 0u) return PlanShape{1u, kPlanTile};
-  return PlanShape{static_cast<uint32_t>((tiles + each - 1u) / each), static_cast<uint32_t>(each * kPlanTile)};
+PlanShape plan_shape(uint64_t choices, uint32_t n_experts) {
+  const uint32_t rounds = choices <= 1024u || (choices > 2048u && (choices + 1023u) / 1024u * n_experts <= 4096u) ? 2u : 4u, tile = rounds * kPlanThreads;
+  const uint64_t tiles = (choices + tile - 1u) / tile, each = (tiles + kPlanGroups - 1u) / kPlanGroups;
+  if (each == 0u) return PlanShape{rounds, 1u, tile};
+  return PlanShape{rounds, static_cast<uint32_t>((tiles + each - 1u) / each), static_cast<uint32_t>(each * tile)};
 }
 
 // ---- gradients --------------------------------------------------------------------------------------
@@ -186,15 +199,15 @@ int uccl_route_rows(int32_t* experts, float* weights, int32_t* counts, float* su
   const RouteArgs a{experts, weights, counts, sums, groups > 1u ? static_cast<uint32_t*>(scratch) : nullptr, rows_of(scores), bias, scores->rows, scores->cols, opts->slots, opts->normalise, opts->scale};
   const hipStream_t s = static_cast<hipStream_t>(stream);
   Launches go;
-  if (scores->rows == 0u) return go(true, route_sum_kernel, blocks_for(scores->cols, 16u), 256, s, counts, sums, static_cast<const uint32_t*>(nullptr), 0u, scores->cols);
+  if (scores->rows == 0u) return go(true, route_sum_kernel, blocks_for(scores->cols, 16u), 1024, s, counts, sums, static_cast<const uint32_t*>(nullptr), 0u, scores->cols);
   return with_type(scores->dtype, [&](auto t) {
     using T = decltype(t);
-    return with_lanes<T>(scores->cols, [&](auto lanes, auto pieces) -> int {
+    return with_lanes<T>(scores->rows, scores->cols, [&](auto lanes, auto pieces) -> int {
       constexpr uint32_t L = decltype(lanes)::value, K = decltype(pieces)::value;
       if (!wanted) return go(true, route_kernel<T, L, K, false>, blocks_for(scores->rows, 256u / L), 256, s, a);
-      const int first = go(groups == 1u, route_kernel<T, L, K, true>, groups, 512, s, a);
+      const int first = go(groups == 1u, route_kernel<T, L, K, true>, groups, kRouteSumThreads, s, a);
       if (first != UCCL_OK || groups == 1u) return first;
-      return go(true, route_sum_kernel, blocks_for(scores->cols, 16u), 256, s, counts, sums, static_cast<const uint32_t*>(a.parts), groups, scores->cols);
+      return go(true, route_sum_kernel, blocks_for(scores->cols, 16u), 1024, s, counts, sums, static_cast<const uint32_t*>(a.parts), groups, scores->cols);
     });
   });
 }
@@ -211,7 +224,7 @@ int uccl_route_rows_grad(const uccl_rows* dscores, const uccl_rows* scores, cons
   const RouteGradArgs a{rows_of(dscores), rows_of(scores), experts, dweights, dsums, scores->rows, scores->cols, opts->slots, opts->normalise, opts->scale};
   return with_type(scores->dtype, [&](auto t) {
     using T = decltype(t);
-    return with_lanes<T>(scores->cols, [&](auto lanes, auto pieces) {
+    return with_lanes<T>(scores->rows, scores->cols, [&](auto lanes, auto pieces) {
       constexpr uint32_t L = decltype(lanes)::value, K = decltype(pieces)::value;
       return launch(route_grad_kernel<T, L, K>, blocks_for(scores->rows, 256u / L), 256, static_cast<hipStream_t>(stream), a);
     });
@@ -227,7 +240,7 @@ int uccl_balance_loss(float* loss, float* dsums, const int32_t* counts, const fl
 }
 
 uint64_t uccl_plan_rows_scratch(uint64_t choices, uint32_t n_experts) {
-  const uint32_t groups = plan_shape(choices).groups;
+  const uint32_t groups = plan_shape(choices, n_experts).groups;
   return groups == 1u ? 0u : (groups * 4ull * n_experts + 15u) / 16u * 16u;
 }
 
@@ -237,7 +250,7 @@ int uccl_plan_rows(int32_t* index, int32_t* offsets, int32_t* pos, const int32_t
   if (choices > kMost || n_experts == 0u || n_experts > UCCL_MOST_EXPERTS || offsets == nullptr || (experts == nullptr && choices != 0u)) return UCCL_EINVAL;
   if (index != nullptr && (index == experts || index == pos)) return UCCL_EINVAL;
   if (misaligned(index, 4) || misaligned(offsets, 4) || misaligned(pos, 4) || misaligned(experts, 4)) return UCCL_EALIGN;
-  const PlanShape shape = plan_shape(choices);
+  const PlanShape shape = plan_shape(choices, n_experts);
   if (shape.groups > 1u) {
     if (scratch == nullptr || scratch_bytes < uccl_plan_rows_scratch(choices, n_experts)) return UCCL_EINVAL;
     if (misaligned(scratch, 16)) return UCCL_EALIGN;
@@ -250,7 +263,7 @@ int uccl_plan_rows(int32_t* index, int32_t* offsets, int32_t* pos, const int32_t
     const int e = go(false, plan_count_kernel, shape.groups, kPlanThreads, s, counts, experts, a.choices, n_experts, shape.share);
     if (e != UCCL_OK) return e;
   }
-  return go(true, plan_kernel<kPlanTile / kPlanThreads>, shape.groups, kPlanThreads, s, a);
+  return shape.rounds == 2u ? go(true, plan_kernel<2>, shape.groups, kPlanThreads, s, a) : go(true, plan_kernel<4>, shape.groups, kPlanThreads, s, a);
 }
 
 // kGradientGroups and one more for every matrix, whose last workgroup may have less than its share.

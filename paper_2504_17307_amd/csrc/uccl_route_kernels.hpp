@@ -8,7 +8,7 @@ namespace {
 // ---- a token's experts ------------------------------------------------------------------------------
 //
 // LANES neighbouring lanes have a token, and a lane K pieces of 16 bytes of its scores, LANES pieces apart: element i of piece k is expert
-// (k LANES + lane) N + i.  With 16 lanes a wavefront has four tokens, and what goes over a token's lanes is four DPP operations for all of them.
+// (k LANES + lane) N + i.  As many lanes as there are pieces, if they are at most 64: the choice is a chain of operations, whose length goes by what a lane has.
 
 template <uint32_t BY>
 __device__ __forceinline__ uint32_t turned(uint32_t v) { return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x120 + BY, 0xF, 0xF, true)); }   // within 16 lanes
@@ -16,14 +16,18 @@ __device__ __forceinline__ uint32_t turned(uint32_t v) { return static_cast<uint
 // Reduce over a token's lanes; every lane has the result.
 template <uint32_t LANES, class F>
 __device__ __forceinline__ uint32_t over_lanes(uint32_t v, F f) {
-  static_assert(LANES == 16u || LANES == 64u);
+  static_assert(LANES == 16u || LANES == 32u || LANES == 64u);
   v = f(v, turned<8>(v));
   v = f(v, turned<4>(v));
   v = f(v, turned<2>(v));
   v = f(v, turned<1>(v));
+  if constexpr (LANES >= 32u) {   // the neighbouring 16 lanes'
+    const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(v, v, false, false));
+    v = f(w[0], w[1]);
+  }
   if constexpr (LANES == 64u) {
-    v = f(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 16)));
-    v = f(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 32)));
+    const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
+    v = f(w[0], w[1]);
   }
   return v;
 }
@@ -43,6 +47,51 @@ __device__ __forceinline__ uint32_t ordered(float key) {
   const uint32_t b = bits_of(key + 0.0f);
   return key > -INFINITY ? b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u) : 0u;
 }
+// A key and its expert as one binary64, 2^52 and 42 bits: of equal keys the lower expert's is the greater, and the greatest of two is one instruction.
+__device__ __forceinline__ double ranked(uint32_t key, uint32_t expert) {
+  return __builtin_bit_cast(double, 0x4330000000000000ull | static_cast<uint64_t>(key) << 10 | (1023u - expert));
+}
+// (fmax would quiet NaNs first, which are none here.)
+__device__ __forceinline__ double greater(double a, double b) {
+  double r;
+  asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+template <uint32_t BY>
+__device__ __forceinline__ double greater_turned(double v) {
+  const u32x2 w = __builtin_bit_cast(u32x2, v);
+  return greater(v, __builtin_bit_cast(double, u32x2{turned<BY>(w[0]), turned<BY>(w[1])}));
+}
+template <uint32_t LANES>
+__device__ __forceinline__ double greatest_of_lanes(double v) {
+  v = greater_turned<8>(v);
+  v = greater_turned<4>(v);
+  v = greater_turned<2>(v);
+  v = greater_turned<1>(v);
+  if constexpr (LANES >= 32u) {
+    const u32x2 w = __builtin_bit_cast(u32x2, v), x = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(w[0], w[0], false, false)),
+                y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(w[1], w[1], false, false));
+    v = greater(__builtin_bit_cast(double, u32x2{x[0], y[0]}), __builtin_bit_cast(double, u32x2{x[1], y[1]}));
+  }
+  if constexpr (LANES == 64u) {
+    const u32x2 w = __builtin_bit_cast(u32x2, v), x = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(w[0], w[0], false, false)),
+                y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(w[1], w[1], false, false));
+    v = greater(__builtin_bit_cast(double, u32x2{x[0], y[0]}), __builtin_bit_cast(double, u32x2{x[1], y[1]}));
+  }
+  return v;
+}
+// The greatest of N, two by two.
+template <uint32_t N>
+__device__ __forceinline__ double greatest_of(const double (&v)[N]) {
+  double w[N];
+#pragma unroll
+  for (uint32_t i = 0; i < N; ++i) w[i] = v[i];
+#pragma unroll
+  for (uint32_t n = N / 2u; n != 0u; n /= 2u)
+#pragma unroll
+    for (uint32_t i = 0; i < n; ++i) w[i] = greater(w[i], w[i + n]);
+  return w[0];
+}
 
 struct RouteArgs {
   int32_t* experts;
@@ -61,17 +110,24 @@ template <class T, uint32_t LANES, uint32_t K>
 struct Scores {
   static constexpr uint32_t N = Piece<T>::N, V = K * N;
   float z[V], most;
-  __device__ __forceinline__ Scores(const Rows& rows, uint64_t row, uint32_t cols) {
-    const uint32_t lane = threadIdx.x % LANES, pieces = (cols + N - 1u) / N;
+  struct Loaded {
     Piece<T> p[K];
+  };
+  static __device__ __forceinline__ Loaded load(const Rows& rows, uint64_t row, uint32_t cols) {
+    const uint32_t lane = threadIdx.x % LANES, pieces = (cols + N - 1u) / N;
+    Loaded l;
 #pragma unroll
-    for (uint32_t k = 0; k < K; ++k) p[k] = load_piece<T>(rows.data + row * rows.stride, min(k * LANES + lane, pieces - 1u));
+    for (uint32_t k = 0; k < K; ++k) l.p[k] = load_piece<T>(rows.data + row * rows.stride, min(k * LANES + lane, pieces - 1u));
+    return l;
+  }
+  __device__ __forceinline__ Scores(const Loaded& l, uint32_t cols) {
+    const uint32_t lane = threadIdx.x % LANES;
     most = -INFINITY;
 #pragma unroll
     for (uint32_t k = 0; k < K; ++k)
 #pragma unroll
       for (uint32_t i = 0; i < N; ++i) {
-        const float v = (k * LANES + lane) * N + i < cols ? widen(p[k].v[i]) : -INFINITY;
+        const float v = (k * LANES + lane) * N + i < cols ? widen(l.p[k].v[i]) : -INFINITY;
         z[k * N + i] = v;
         most = fmaxf(most, v);
       }
@@ -83,15 +139,18 @@ struct Scores {
 // 1 / (sum of exp(z - most)); 0 for a token whose scores are all -infinity.
 __device__ __forceinline__ float per_sum(float sum) { return sum == 0.0f ? 0.0f : 1.0f / sum; }
 
-// The `slots` greatest keys one after the other: the greatest of the lane's own, of the token's lanes', and the lowest expert that has it.
+// The `slots` greatest keys one after the other: the greatest of the lane's own, then of the token's lanes'.
 // SUMS: workgroups take tokens in turn, and add up counts and probabilities in their order.
+constexpr uint32_t kRouteSumThreads = 512;
+
 template <class T, uint32_t LANES, uint32_t K, bool SUMS>
-__global__ __launch_bounds__(512) void route_kernel(RouteArgs a) {
+__global__ __launch_bounds__(SUMS ? kRouteSumThreads : 256) void route_kernel(RouteArgs a) {
   using S = Scores<T, LANES, K>;
-  constexpr uint32_t N = S::N, V = S::V, KEEP = 32u / LANES == 0u ? 1u : 32u / LANES, THREADS = SUMS ? 512u : 256u, EACH = THREADS / LANES;
+  constexpr uint32_t N = S::N, V = S::V, KEEP = 32u / LANES == 0u ? 1u : 32u / LANES, THREADS = SUMS ? kRouteSumThreads : 256u, EACH = THREADS / LANES;
   constexpr uint32_t WAVES = THREADS / 64u, MOST = LANES * V;
   __shared__ uint32_t counted[SUMS ? MOST : 1u];
   __shared__ float added[SUMS ? WAVES : 1u][SUMS ? MOST : 1u];
+  __shared__ float scores[EACH][MOST];
   const uint32_t lane = threadIdx.x % LANES;
   if constexpr (SUMS) {
     for (uint32_t e = threadIdx.x; e < MOST; e += THREADS) counted[e] = 0u;
@@ -101,19 +160,24 @@ __global__ __launch_bounds__(512) void route_kernel(RouteArgs a) {
 #pragma unroll
   for (uint32_t v = 0; v < V; ++v) {
     const uint32_t e = (v / N * LANES + lane) * N + v % N;
-    bias[v] = a.bias != nullptr && e < a.cols ? a.bias[e] : 0.0f;
+    bias[v] = a.bias != nullptr ? a.bias[min(e, a.cols - 1u)] : 0.0f;
     total[v] = 0.0f;
   }
+  typename S::Loaded next;
+  if (blockIdx.x * EACH < a.tokens) next = S::load(a.scores, min(blockIdx.x * EACH + threadIdx.x / LANES, a.tokens - 1u), a.cols);
   for (uint32_t first = blockIdx.x * EACH; first < a.tokens; first += gridDim.x * EACH) {
     const uint32_t at = first + threadIdx.x / LANES;
     const bool here = at < a.tokens;
     const uint64_t token = min(at, a.tokens - 1u);
-    const S s(a.scores, token, a.cols);
-    uint32_t key[V];
+    const S s(next, a.cols);
+    if constexpr (SUMS) next = S::load(a.scores, min(static_cast<uint64_t>(at) + gridDim.x * EACH, a.tokens - 1ull), a.cols);   // (the last once more, for nothing)
+    double key[V];
     float sum = 0.0f, p[V];
 #pragma unroll
     for (uint32_t v = 0; v < V; ++v) {
-      key[v] = ordered(s.z[v] + bias[v]);
+      const uint32_t e = (v / N * LANES + lane) * N + v % N;
+      scores[threadIdx.x / LANES][e] = s.z[v];
+      key[v] = ranked(ordered(s.z[v] + bias[v]), e);
       p[v] = expf(s.z[v] - s.most);
       sum += p[v];
     }
@@ -127,26 +191,19 @@ __global__ __launch_bounds__(512) void route_kernel(RouteArgs a) {
 #pragma unroll
     for (uint32_t k = 0; k < KEEP; ++k) mine[k] = -1;
     for (uint32_t j = 0; j < a.slots; ++j) {
-      uint32_t best = 0u;
+      const uint64_t found = __builtin_bit_cast(uint64_t, greatest_of_lanes<LANES>(greatest_of(key)));
+      const uint32_t low = static_cast<uint32_t>(found);   // the expert's number is in it, so no other key has it
 #pragma unroll
-      for (uint32_t v = 0; v < V; ++v) best = max(best, key[v]);
-      best = over_lanes<LANES>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
-      uint32_t expert = 0x7FFFFFFFu;
-#pragma unroll
-      for (uint32_t v = V; v-- > 0u;) expert = key[v] == best ? v / N * LANES * N + v % N : expert;
-      expert = over_lanes<LANES>(expert == 0x7FFFFFFFu ? expert : expert + lane * N, [](uint32_t x, uint32_t y) { return min(x, y); });
-      const uint32_t own = expert - lane * N;
-#pragma unroll
-      for (uint32_t v = 0; v < V; ++v) key[v] = own == v / N * LANES * N + v % N ? 0u : key[v];
+      for (uint32_t v = 0; v < V; ++v) key[v] = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, key[v])) == low ? 0.0 : key[v];
 #pragma unroll
       for (uint32_t k = 0; k < KEEP; ++k)
-        if (j == k * LANES + lane && best != 0u) mine[k] = static_cast<int32_t>(expert);
+        if (j == k * LANES + lane && found >= 0x4330000000000400ull) mine[k] = static_cast<int32_t>(1023u - (low & 1023u));
     }
     // a lane has the token's slots lane, lane + LANES
     float z[KEEP], most = -INFINITY, some = 0.0f;
 #pragma unroll
     for (uint32_t k = 0; k < KEEP; ++k) {
-      z[k] = mine[k] < 0 ? -INFINITY : widen(reinterpret_cast<const T*>(a.scores.data + token * a.scores.stride)[mine[k]]);
+      z[k] = mine[k] < 0 ? -INFINITY : scores[threadIdx.x / LANES][mine[k]];   // its own wavefront's
       most = fmaxf(most, z[k]);
     }
     // normalised, relative to the greatest of the chosen: a bias may choose experts all of whose p are 0 in binary32
@@ -173,10 +230,9 @@ __global__ __launch_bounds__(512) void route_kernel(RouteArgs a) {
     const uint32_t wave = threadIdx.x / 64u;
 #pragma unroll
     for (uint32_t v = 0; v < V; ++v) {
-      if constexpr (LANES == 16u) {   // the wavefront's four tokens
-        total[v] += __shfl_xor(total[v], 16);
-        total[v] += __shfl_xor(total[v], 32);
-      }
+      // the wavefront's four tokens, or two
+      if constexpr (LANES == 16u) total[v] += __shfl_xor(total[v], 16);
+      if constexpr (LANES <= 32u) total[v] += __shfl_xor(total[v], 32);
       if (threadIdx.x % 64u < LANES) added[wave][(v / N * LANES + lane) * N + v % N] = total[v];
     }
     __syncthreads();
@@ -196,26 +252,37 @@ __global__ __launch_bounds__(512) void route_kernel(RouteArgs a) {
   }
 }
 
-// The workgroups' counts and sums, 16 of them at a time for 16 experts.
-__global__ __launch_bounds__(256) void route_sum_kernel(int32_t* counts, float* sums, const uint32_t* parts, uint32_t n, uint32_t cols) {
-  __shared__ uint32_t counted[16][16];
-  __shared__ float added[16][16];
-  const uint32_t e = blockIdx.x * 16u + threadIdx.x % 16u, turn = threadIdx.x / 16u;
+// The workgroups' counts and sums, 64 of them at a time for 16 experts.
+__global__ __launch_bounds__(1024) void route_sum_kernel(int32_t* counts, float* sums, const uint32_t* parts, uint32_t n, uint32_t cols) {
+  __shared__ uint32_t counted[64][16];
+  __shared__ float added[64][16];
+  const uint32_t at = threadIdx.x % 16u, e = blockIdx.x * 16u + at, turn = threadIdx.x / 16u;
   uint32_t c = 0u;
   float s = 0.0f;
   if (e < cols)
-    for (uint32_t i = turn; i < n; i += 16u) {
+#pragma unroll 4
+    for (uint32_t i = turn; i < n; i += 64u) {
       c += parts[(i * 2ull) * cols + e];
       s += float_of(parts[(i * 2ull + 1u) * cols + e]);
     }
-  counted[turn][threadIdx.x % 16u] = c;
-  added[turn][threadIdx.x % 16u] = s;
+  counted[turn][at] = c;
+  added[turn][at] = s;
+  __syncthreads();
+  if (turn < 8u) {
+#pragma unroll
+    for (uint32_t i = 8; i < 64u; i += 8u) {
+      c += counted[turn + i][at];
+      s += added[turn + i][at];
+    }
+    counted[turn][at] = c;
+    added[turn][at] = s;
+  }
   __syncthreads();
   if (turn != 0u || e >= cols) return;
 #pragma unroll
-  for (uint32_t i = 1; i < 16u; ++i) {
-    c += counted[i][threadIdx.x];
-    s += added[i][threadIdx.x];
+  for (uint32_t i = 1; i < 8u; ++i) {
+    c += counted[i][at];
+    s += added[i][at];
   }
   if (counts != nullptr) counts[e] = static_cast<int32_t>(c);
   if (sums != nullptr) sums[e] = s;
@@ -236,6 +303,7 @@ template <class T, uint32_t LANES, uint32_t K>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
   using S = Scores<T, LANES, K>;
   constexpr uint32_t N = S::N, V = S::V, KEEP = 32u / LANES == 0u ? 1u : 32u / LANES, EACH = 256u / LANES;
+  __shared__ float part[EACH][LANES * V];
   const uint32_t lane = threadIdx.x % LANES, at = blockIdx.x * EACH + threadIdx.x / LANES;
   const bool here = at < a.tokens;
   const uint64_t token = min(at, a.tokens - 1u);
@@ -256,9 +324,9 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
 #pragma unroll
   for (uint32_t v = 0; v < V; ++v) {
     const uint32_t e = (v / N * LANES + lane) * N + v % N;
-    d[v] = a.dsums != nullptr && e < a.cols ? a.dsums[e] : 0.0f;
+    d[v] = a.dsums != nullptr ? a.dsums[min(e, a.cols - 1u)] : 0.0f;   // (behind the last expert p is 0)
   }
-  const S s(a.scores, token, a.cols);
+  const S s(S::load(a.scores, token, a.cols), a.cols);
   float p[V], sum = 0.0f;
 #pragma unroll
   for (uint32_t v = 0; v < V; ++v) {
@@ -300,19 +368,19 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
   for (uint32_t v = 0; v < V; ++v) p[v] *= d[v] - along;
 #pragma unroll
   for (uint32_t k = 0; k < KEEP; ++k) q[k] *= a.normalise != 0u ? g[k] - chosen : g[k];
-  for (uint32_t j = 0; j < a.slots; ++j) {
-    float add = q[0];
-    int32_t expert = mine[0];
-    if constexpr (KEEP == 2u) {
-      add = j < LANES ? add : q[KEEP - 1u];
-      expert = j < LANES ? expert : mine[KEEP - 1u];
-    }
-    add = __shfl(add, static_cast<int>(j % LANES), LANES);
-    expert = __shfl(expert, static_cast<int>(j % LANES), LANES);
-    const uint32_t own = static_cast<uint32_t>(expert) - lane * N;
-    if (expert >= 0)
+  // the chosen ones' part lies in the LDS by expert; slots follow each other, so one that names an expert again adds to it in a fixed order
+  float* const chosen_part = part[threadIdx.x / LANES];
+  if (a.experts != nullptr) {
 #pragma unroll
-      for (uint32_t v = 0; v < V; ++v) p[v] += own == v / N * LANES * N + v % N ? add : 0.0f;
+    for (uint32_t v = 0; v < V; ++v) chosen_part[(v / N * LANES + lane) * N + v % N] = 0.0f;
+#pragma unroll
+    for (uint32_t k = 0; k < KEEP; ++k) {
+      const uint32_t n = a.slots > k * LANES ? min(a.slots - k * LANES, LANES) : 0u;
+      for (uint32_t j = 0; j < n; ++j)
+        if (lane == j && mine[k] >= 0) chosen_part[mine[k]] += q[k];
+    }
+#pragma unroll
+    for (uint32_t v = 0; v < V; ++v) p[v] += chosen_part[(v / N * LANES + lane) * N + v % N];
   }
   if (!here) return;
 #pragma unroll
@@ -420,19 +488,20 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   __syncthreads();
   // what the experts have in all, and in earlier workgroups
   if (a.counts != nullptr) {
-    const uint32_t all = gridDim.x * a.n_experts, earlier = blockIdx.x * a.n_experts, further = kPlanThreads % a.n_experts;
+    const uint32_t slices = a.n_experts < kPlanThreads ? kPlanThreads / a.n_experts : 1u;   // threads that share an expert's groups
     for (uint32_t e = threadIdx.x; e < a.n_experts; e += kPlanThreads) totals[e] = next[e] = 0u;
     __syncthreads();
-    uint32_t e = threadIdx.x % a.n_experts;
+    for (uint32_t i = threadIdx.x; i < a.n_experts * slices; i += kPlanThreads) {
+      const uint32_t slice = i / a.n_experts, e = i - slice * a.n_experts;
+      uint32_t all = 0u, earlier = 0u;
 #pragma unroll 8
-    for (uint32_t i = threadIdx.x; i < all; i += kPlanThreads) {
-      const uint32_t n = a.counts[i];
-      if (n != 0u) {
-        atomicAdd(&totals[e], n);
-        if (i < earlier) atomicAdd(&next[e], n);
+      for (uint32_t b = slice; b < gridDim.x; b += slices) {
+        const uint32_t n = a.counts[b * a.n_experts + e];
+        all += n;
+        earlier += b < blockIdx.x ? n : 0u;
       }
-      e += further;
-      if (e >= a.n_experts) e -= a.n_experts;
+      atomicAdd(&totals[e], all);
+      atomicAdd(&next[e], earlier);
     }
     __syncthreads();
   }
