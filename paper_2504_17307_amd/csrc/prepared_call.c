@@ -147,8 +147,8 @@ static PyTypeObject prepared_type = {
     .tp_weaklistoffset = offsetof(Prepared, weak),
     .tp_new = prepared_new,
 };
-/* Lists of tensors as rows (uccl_gradient_norm, uccl_gradient_clip): asking a tensor for its address, size and type through the interpreter
- * takes 0.1 us each, and there may be hundreds.  The DLPack standard's table of C functions (its version 1, which tensor types offer as
+/* Tensors as arguments of the row operators: asking one for its address, sizes and type through the interpreter takes 0.1 us each, and a call has
+ * several, or a list of hundreds (uccl_gradient_norm, uccl_gradient_clip).  The DLPack standard's table of C functions (its version 1, which tensor types offer as
  * __dlpack_c_exchange_api__) has one that fills in a struct for a tensor.  300 tensors: 18 us so, 1400 in Python. */
 typedef struct { int32_t type, id; } DlDevice;
 typedef struct { uint8_t code, bits; uint16_t lanes; } DlType;
@@ -218,7 +218,52 @@ static PyObject* contiguous_rows(PyObject* self, PyObject* const* args, Py_ssize
   return bytes;
 }
 
-static PyMethodDef methods[] = {{"contiguous_rows", (PyCFunction)(void (*)(void))contiguous_rows, METH_FASTCALL, NULL}, {NULL, NULL, 0, NULL}};
+static const DlFunctions* functions_of(PyObject* capsule) {
+  const DlFunctions* const f = PyCapsule_CheckExact(capsule) ? (const DlFunctions*)PyCapsule_GetPointer(capsule, PyCapsule_GetName(capsule)) : NULL;
+  return f != NULL && f->major == 1 ? f : NULL;
+}
+
+/* vector_address(functions, tensor, whether it is float32 and not int32, elements): where it is, or None: it is not contiguous, of another type or length. */
+static PyObject* vector_address(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
+  (void)self;
+  const DlFunctions* const f = n_args == 4 ? functions_of(args[0]) : NULL;
+  DlTensor t;
+  int64_t elements;
+  if (f == NULL || f->tensor_from_object(args[1], &t) != 0 || t.dtype.bits != 32 || t.dtype.lanes != 1 || t.dtype.code != (args[2] == Py_True ? 2 : 0) || !contiguous(&t, &elements) ||
+      elements != PyLong_AsLongLong(args[3])) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  return PyLong_FromUnsignedLongLong((uint64_t)(uintptr_t)t.data + t.byte_offset);
+}
+
+/* matrix_rows(functions, tensor): the bytes of its uccl_rows, or None: it is of a type with scales, or not a matrix by rows of fewer than 2^32 rows and columns. */
+static PyObject* matrix_rows(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
+  (void)self;
+  const DlFunctions* const f = n_args == 2 ? functions_of(args[0]) : NULL;
+  DlTensor t;
+  if (f != NULL && f->tensor_from_object(args[1], &t) == 0 && t.strides != NULL && t.dtype.lanes == 1 && (t.ndim == 2 || t.ndim == 3)) {
+    const int f32 = t.dtype.code == 2 && t.dtype.bits == 32, f16 = t.dtype.code == 2 && t.dtype.bits == 16, bf16 = t.dtype.code == 4 && t.dtype.bits == 16;
+    const int64_t groups = t.ndim == 3 ? t.shape[0] : 1, each = t.shape[t.ndim - 2], cols = t.shape[t.ndim - 1], last = t.strides[t.ndim - 1];
+    int64_t step = t.strides[t.ndim - 2];
+    const int small = groups <= 0xFFFFFFFF && each <= 0xFFFFFFFF && cols <= 0xFFFFFFFF && (each == 0 || groups <= 0xFFFFFFFF / each);
+    int fits = small && (f32 || f16 || bf16) && (last == 1 || cols <= 1);
+    if (fits && t.ndim == 3) {
+      if (each == 1) step = t.strides[0];
+      else if (groups > 1 && each != 0 && cols != 0 && t.strides[0] != each * step) fits = 0;
+    }
+    if (fits && step >= 0) {
+      const RowsStruct r = {(uint64_t)(uintptr_t)t.data + t.byte_offset, (uint64_t)step * (t.dtype.bits / 8), 0, 0, (uint32_t)(groups * each), (uint32_t)cols, f32 ? 0u : bf16 ? 1u : 2u, 0};
+      return PyBytes_FromStringAndSize((const char*)&r, sizeof r);
+    }
+  }
+  PyErr_Clear();
+  Py_RETURN_NONE;
+}
+
+static PyMethodDef methods[] = {{"vector_address", (PyCFunction)(void (*)(void))vector_address, METH_FASTCALL, NULL},
+                                {"matrix_rows", (PyCFunction)(void (*)(void))matrix_rows, METH_FASTCALL, NULL},
+                                {"contiguous_rows", (PyCFunction)(void (*)(void))contiguous_rows, METH_FASTCALL, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_prepared", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__prepared(void) {

@@ -9,7 +9,8 @@ import ctypes as C
 import os
 import struct
 
-from .rows import UCCL_MX4, _count, _rows, _vector, uccl_rows
+from . import rows
+from .rows import _count, _find_tables, _rows, _vector
 
 EXPERTS_HEADER_PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "uccl_experts.h")
 
@@ -111,32 +112,15 @@ def uccl_quantise_rows(q, scales, x, values=None, stream=None):
 
 
 _LONGEST = 1 << 30   # columns of a matrix
-_table = None        # DLPack's functions of torch's tensors, False: not to be had
-
-
-def _find_table():
-    """The table, if the extension reads what this function does from it."""
-    global _table
-    import torch
-    from . import _load_extension
-    extension, table = _load_extension(), getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
-    _table = False
-    if extension and table is not None:
-        probe = [torch.zeros(3, 5, dtype=torch.bfloat16), torch.zeros(7)]
-        want = b"".join(_rows(t.view(1, -1)) for t in probe)
-        read = extension.contiguous_rows(table, probe, probe, _LONGEST)
-        if read is not None and read[:8] == want[:8] and read[32:56] == want[32:56] and read[80:] == want[80:]:
-            _table = extension, table
-    return _table
 
 
 def _matrices(tensors, like=None):
     """The bytes of a HOST array of uccl_rows, and how many there are; a contiguous tensor is one row, or whole rows and what is left.  Tensors are
     cut as those of ``like`` are, if there are any."""
     if type(tensors) is list and (like is None or type(like) is list):
-        found = _find_table() if _table is None else _table
-        if found:
-            made = found[0].contiguous_rows(found[1], tensors, tensors if like is None else like, _LONGEST)
+        tables = _find_tables() if rows._tables is None else rows._tables
+        if tables:
+            made = tables[0].contiguous_rows(tables[1], tensors, tensors if like is None else like, _LONGEST)
             if made is not None:
                 return made, len(tensors)
     made = []
