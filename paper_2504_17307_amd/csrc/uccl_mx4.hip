@@ -21,17 +21,20 @@ double rounds_of(double tiles, double room) {
 // Rows of 4 bits, in us for 256 elements of the sum.  Few rows: 2.0e-5 for 16 rows of a column, 2.6e-5 for a column's weights where they are read once;
 // tiles of 128 x 128, two on a compute unit: 1.7 a round, 1 where most of them are idle.  Measured, 16 rows at a time / 128 x 128, 7168 -> 2048, us: one group, 1 / 100 rows, 8.0 / 10.4 against
 // 23 / 28; 8 of 32 groups, 16 rows, 13.3 against 28; 32 groups, 128 rows, 49 against 54; 8 groups, 300 rows, 26 against 29; 16 groups, 1000 rows, 81 against 47.
-// Tiles: in units of one of 256 x 256 (67 us with a depth of 7168, one a compute unit) 128 x 128 costs 0.62, two on a compute unit.  Measured, 256 x 256 / 128 x 128, us: 4096 rows in 16 ragged groups,
-// 7168 -> 2048, 84 / 95; 2048 rows 79 / 67; 1000 rows 65 / 47; 4000 rows in 4 groups 67 / 53; 8190 rows in 16 groups, 2048 -> 7168, 133 / 144; 512 rows in one group, 2048 -> 2048, 21 / 11; 8192^3 339 / 457.
-// (128 x 256, of which one fits a compute unit, takes 52 where 128 x 128 takes 53, and more elsewhere.)
+// Tiles: in units of one of 256 x 256 (67 us with a depth of 7168, one a compute unit) 192 x 256 costs 0.91, and 128 x 128 0.62, two on a compute unit.  Measured, 256 x 256 / 192 x 256 / 128 x 128, us:
+// 4096 rows in 16 ragged groups, 7168 -> 2048, 83 / 76 / 93; 2048 rows 77 / 73 / 66; 1000 rows 63 / 61 / 44; 4000 rows in 4 groups 67 / 61 / 51; 8192 rows in 8 groups 80 / 135 / 110; 8190 rows in 16 groups,
+// 2048 -> 7168, 131 / 139 / 137; 8192^3 313 / 367 / 429.  (128 x 256, of which one fits a compute unit, takes 52 where 128 x 128 takes 51, and more elsewhere.)
 int product_4(const ProductArgs& a, hipStream_t s) {
   const double wide = a.wide, small_tiles = tiles_down(a, 128u) * blocks_for(a.wide, 128u);
   const double few = fmax(tiles_down(a, 16u) * wide * 2.0e-5, used_groups(a) * wide * 2.6e-5);
   const double tiles = fmax(rounds_of(small_tiles, 512.0) * (1.0 + 0.7 * fmin(1.0, small_tiles / 256.0)), used_groups(a) * wide * 3.0e-5);
   if (few < tiles && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 32u) <= 1u << 23)
     return product_tiles<kForward>(mx4_few_kernel<kRows4, 32, 4, 3>, 16, 32, 256, a, s);
-  if (rounds_of(tiles_down(a, 256u) * blocks_for(a.wide, 256u), 256.0) <= 0.62 * rounds_of(small_tiles, 512.0)) return product_tiles<kForward>(mx4_tile_kernel<256, 256, 2, 4>, 256, 256, 512, a, s);
-  return product_tiles<kForward>(mx4_tile_kernel<128, 128, 2, 4>, 128, 128, 512, a, s);
+  const double across = blocks_for(a.wide, 256u), large = rounds_of(tiles_down(a, 256u) * across, 256.0), middle = 0.91 * rounds_of(tiles_down(a, 192u) * across, 256.0);
+  const double small = 0.62 * rounds_of(small_tiles, 512.0);
+  if (large <= middle && large <= small) return product_tiles<kForward>(mx4_tile_kernel<256, 256, 2, 4, 6>, 256, 256, 512, a, s);
+  if (middle <= small) return product_tiles<kForward>(mx4_tile_kernel<192, 256, 2, 4, 5>, 192, 256, 512, a, s);
+  return product_tiles<kForward>(mx4_tile_kernel<128, 128, 2, 4, 3>, 128, 128, 512, a, s);
 }
 
 // Rows of 16 bits, the same.  Few rows by 64 columns: 2.9e-5 for 16 rows of a column, 3.3e-5 for a column's weights; by 16 columns where that would leave most compute units idle; tiles of 128 x 128: 2.4 a

@@ -167,10 +167,11 @@ __device__ __forceinline__ bool exact_in_f16(uint32_t scale) { return scale - (1
 
 // As product_tile_kernel: a stage is 128 bytes along the sum, 256 elements, and is multiplied in two halves; a half is one matrix instruction for
 // 16 x 16 of the output.  The LDS holds two stages of each operand.  When every wavefront has read its last fragments of a stage, a little into its
-// second half, the stage after the next one is asked for in its place.
+// second half, the stage after the next one is asked for in its place, by loads that SPREAD rows of blocks have between them; the barrier there, which the
+// next stage's arrival is waited for at too, is the only one in a stage.
 // Scales come 32 bytes of a row at a time, for four stages, into one of two places: a load of 64 words touches as few rows as one of 64 pieces does.  (4 bytes of
 // 64 rows at every stage: 8192^3 388 us, 306 without them.)
-template <uint32_t BM, uint32_t BN, uint32_t WR, uint32_t WC>
+template <uint32_t BM, uint32_t BN, uint32_t WR, uint32_t WC, uint32_t SPREAD>
 __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
   constexpr uint32_t THREADS = WR * WC * 64u, SIDE = 16u, NA = BM / WR / SIDE, NB = BN / WC / SIDE, EACH = THREADS / 8u;   // rows of a load
   constexpr uint32_t A_LOADS = BM / EACH, B_LOADS = BN / EACH, LOADS = A_LOADS + B_LOADS, S_LOADS = (LOADS + 1u) / 2u;   // of scales, in the first two of four stages
@@ -287,41 +288,49 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
   // STEADY: stage k + 2 is there to be asked for, and is not the last
   auto work = [&](uint32_t k, auto steady) {
     constexpr bool STEADY = decltype(steady)::value;
-    constexpr uint32_t FROM = NA / 4u == 0u ? 1u : NA / 4u, ALL = LOADS + S_LOADS;
+    constexpr uint32_t FROM = NA / 4u == 0u ? 1u : NA / 4u, ALL = LOADS + S_LOADS, OVER = SPREAD;
     const bool more = STEADY || k + 2u < steps, last = !STEADY && k + 3u == steps, scales = k % 4u < 2u && (k / 4u + 1u) * 4u < steps;
+    // the first half's fragments are fa and fb[0]: multiply, and read the second half's
+    Places p = places(k, 1);
 #pragma unroll
-    for (uint32_t half = 0; half < 2u; ++half) {   // its fragments are fa and fb[half]: multiply, and read the next half's
-      const uint32_t then = k + half, other = half ^ 1u;
-      if (half == 1u) {
-        if (STEADY || k + 1u < steps) wait_for_loads<0>();
+    for (uint32_t n = 0; n < NB; ++n) read_b(p, 1, n);
+#pragma unroll
+    for (uint32_t m = 0; m < NA; ++m) {
+      if (m < high)
+#pragma unroll
+        for (uint32_t n = 0; n < NB; ++n) acc[n][m] = multiply_4(fb[0][n], sb[0][n], fa[m], sa[m], acc[n][m]);
+      __builtin_amdgcn_sched_barrier(0);   // the next fragment takes the registers of this one
+      read_a(p, m);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    p = places(k + 1u, 0);
+#pragma unroll
+    for (uint32_t m = 0; m < NA; ++m) {
+      if (m < high)
+#pragma unroll
+        for (uint32_t n = 0; n < NB; ++n) acc[n][m] = multiply_4(fb[1][n], sb[1][n], fa[m], sa[m], acc[n][m]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (m + 1u == FROM) {
+        // every wavefront has its last fragments of the stage, and the next stage is there
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (!STEADY && ragged && k + 2u == steps) trim();
+#pragma unroll
+        for (uint32_t n = 0; n < NB; ++n) read_b(p, 0, n);   // behind the last stage: read, and not used
+#pragma unroll
+        for (uint32_t i = 0; i < FROM; ++i) read_a(p, i);
       }
-      const Places p = places(then, other);   // behind the last stage: read, and not used
+      if (m >= FROM) read_a(p, m);
 #pragma unroll
-      for (uint32_t n = 0; n < NB; ++n) read_b(p, other, n);
-#pragma unroll
-      for (uint32_t m = 0; m < NA; ++m) {
-        if (m < high)
-#pragma unroll
-          for (uint32_t n = 0; n < NB; ++n) acc[n][m] = multiply_4(fb[half][n], sb[half][n], fa[m], sa[m], acc[n][m]);
-        __builtin_amdgcn_sched_barrier(0);   // the next fragment takes the registers of this one
-        read_a(p, m);
-        if (half == 1u) {
-          // the loads may begin: what is newer than the stage's last reads are this half's, of w's fragments at least
-          if (m + 1u == FROM && (more || scales)) wait_for_reads<NB>();
-#pragma unroll
-          for (uint32_t i = 0; i < ALL; ++i)
-            if (m + 1u >= FROM && i * (NA + 1u - FROM) / ALL == m + 1u - FROM) {
-              if (i < LOADS) {
-                if (more) load(k + 2u, i, last);
-              } else if (scales) {
-                if (k % 4u == 0u) load_scales(k / 4u + 1u, i - LOADS);
-                else if (i - LOADS + S_LOADS < LOADS) load_scales(k / 4u + 1u, i - LOADS + S_LOADS);
-              }
-            }
+      for (uint32_t i = 0; i < ALL; ++i)
+        if (m + 1u >= FROM && i * OVER / ALL == m + 1u - FROM) {
+          if (i < LOADS) {
+            if (more) load(k + 2u, i, last);
+          } else if (scales) {
+            if (k % 4u == 0u) load_scales(k / 4u + 1u, i - LOADS);
+            else if (i - LOADS + S_LOADS < LOADS) load_scales(k / 4u + 1u, i - LOADS + S_LOADS);
+          }
         }
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   if (steps != 0u) {
@@ -354,7 +363,7 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
       f32x4 v[BLOCKS];
 #pragma unroll
       for (uint32_t b = 0; b < BLOCKS; ++b) v[b] = acc[n + b][m];
-      store_blocks<BM == 256u>(a, top, rows, c0 + cb + n * SIDE, a.wide, v);
+      store_blocks<(BM > 128u)>(a, top, rows, c0 + cb + n * SIDE, a.wide, v);
     }
   }
 }

@@ -501,7 +501,7 @@ def test_product(uccl, kind, rows, groups, wide, cols):
 
 
 # sums long enough for every kernel's steady state, by every kernel (tests/test_experts_abi.py has which): rows, groups, columns, depth
-DEEP = [(1500, 2, 1030, 4000), (700, 5, 520, 2600), (4500, 3, 2060, 1300), (90, 3, 200, 5000), (1300, 1, 4100, 1500), (400, 1, 1900, 3000), (6000, 1, 4200, 900)]
+DEEP = [(1500, 2, 1030, 4000), (700, 5, 520, 2600), (4500, 3, 2060, 1300), (90, 3, 200, 5000), (1300, 1, 4100, 1500), (400, 1, 1900, 3000), (6000, 1, 4200, 900), (4300, 2, 2040, 1000)]
 
 
 @pytest.mark.parametrize("kind", KINDS)
