@@ -160,8 +160,8 @@ __device__ __forceinline__ void load_word_to_lds(const char* from, uint32_t to) 
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "m0");
 }
 
-// Scales by which weights are exact as f16.
-__device__ __forceinline__ bool exact_in_f16(uint32_t scale) { return scale - (127u - 23u) <= 36u || scale == 255u; }
+// Scales by which weights are exact as f16.  (That of NaN is left to the other way.)
+__device__ __forceinline__ bool exact_in_f16(uint32_t scale) { return scale - (127u - 23u) <= 36u; }
 
 // ---- tiles, rows in 4 bits --------------------------------------------------------------------------
 
@@ -388,17 +388,19 @@ __global__ __launch_bounds__(512) void mx4_wide_kernel(ProductArgs a) {
   if (!find_tile(a, BM, across, g, r0, c0)) return;
   c0 *= BN;
   const uint64_t w0 = static_cast<uint64_t>(g.index) * a.wide;
-  const char* const x_data = a.a.data;
-  const uint64_t x_stride = a.a.stride, w_stride = a.b.stride;
-  const uint32_t x_rows = a.indexed_rows, cols = a.cols, w_bytes = (cols + 1u) / 2u, words = (cols + 127u) / 128u, steps = (cols + 63u) / 64u, stages = (cols + 255u) / 256u;
+  const uint64_t w_stride = a.b.stride;
+  const uint32_t cols = a.cols, w_bytes = (cols + 1u) / 2u, words = (cols + 127u) / 128u, steps = (cols + 63u) / 64u, stages = (cols + 255u) / 256u;
 
   // Load i of an operand is of rows 64 i + thread / 8, a piece of 16 bytes each.  Rows and columns past the tile's end stand for its last ones.
   const uint32_t own_row = threadIdx.x / 8u, own_piece = (threadIdx.x % 8u ^ (own_row >> 1 & 7u)) * 16u;
-  uint32_t row[A_LOADS];   // of x; one that it has not stands for zeros
+  const char* la[A_LOADS];
+  uint32_t still = 0u;   // bit i: the piece of load i is of a row of zeros and stays where it is
 #pragma unroll
   for (uint32_t i = 0; i < A_LOADS; ++i) {
-    row[i] = min(r0 + i * 64u + own_row, g.end - 1u);
-    if (a.index != nullptr) row[i] = static_cast<uint32_t>(a.index[row[i]]);
+    uint32_t r = min(r0 + i * 64u + own_row, g.end - 1u);
+    if (a.index != nullptr) r = static_cast<uint32_t>(a.index[r]);
+    la[i] = r < a.indexed_rows ? a.a.data + r * a.a.stride + own_piece : zeros;
+    still |= r < a.indexed_rows ? 0u : 1u << i;
   }
   const char* lb = a.b.data + (w0 + min(c0 + own_row, a.wide - 1u)) * w_stride + own_piece;
   const char* ls = a.b.scales + (w0 + min(c0 + min(threadIdx.x / 2u, BN - 1u), a.wide - 1u)) * a.b.scale_stride + threadIdx.x % 2u * 4u;
@@ -407,21 +409,20 @@ __global__ __launch_bounds__(512) void mx4_wide_kernel(ProductArgs a) {
   for (uint32_t i = 0; i < B_LOADS; ++i) columns |= c0 + i * 64u + own_row < a.wide ? 1u << i : 0u;
   const uint32_t mine = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63u);
   const uint32_t here_a = lds_address(lds_a) + mine * 16u, here_b = lds_address(lds_b) + mine * 16u, here_s = lds_address(lds_s) + mine * 4u;
-  auto load_a = [&](uint32_t t, uint32_t slot, uint32_t i) {
-    uint32_t r = row[i];
-    asm volatile("" : "+v"(r));   // (a row's number is all that is kept of it from one load to the next)
-    const char* from = x_data + t * 128ull + r * x_stride + own_piece;
-    if (r >= x_rows || t * 64u + own_piece / 2u >= cols) from = zeros;
+  auto load_a = [&](uint32_t t, uint32_t slot, uint32_t i, bool inside) {   // inside: not the last step, whose end may lie in it
+    const char* from = la[i];
+    if (!inside && t * 64u + own_piece / 2u >= cols) from = zeros;
     load_to_lds(from, __builtin_amdgcn_readfirstlane(here_a + slot * A_STEP + i * 8192u));
+    la[i] += still >> i & 1u ? 0u : 128u;
   };
-  auto load_b = [&](uint32_t k, uint32_t i) {   // the last one of a stage is of its scales
+  auto load_b = [&](uint32_t k, uint32_t i, bool inside) {   // the last one of a stage is of its scales
     if (i < B_LOADS) {
       const char* from = columns >> i & 1u ? lb + i * 64u * w_stride : lb;
-      if (k * 128u + own_piece >= w_bytes) from = zeros;
+      if (!inside && k * 128u + own_piece >= w_bytes) from = zeros;
       load_to_lds(from, __builtin_amdgcn_readfirstlane(here_b + k % 2u * B_STAGE + i * 8192u));
       if (i + 1u == B_LOADS) lb += 128u;
     } else {
-      load_word_to_lds(k * 2u + threadIdx.x % 2u < words ? ls : zeros, __builtin_amdgcn_readfirstlane(here_s + k % 2u * S_STAGE));
+      load_word_to_lds(inside || k * 2u + threadIdx.x % 2u < words ? ls : zeros, __builtin_amdgcn_readfirstlane(here_s + k % 2u * S_STAGE));
       ls += 8u;
     }
   };
@@ -532,12 +533,12 @@ __global__ __launch_bounds__(512) void mx4_wide_kernel(ProductArgs a) {
       if (m + 1u == FROM || NA == 1u) {
         if (more) {
 #pragma unroll
-          for (uint32_t i = 0; i < A_LOADS; ++i) load_a(t + AHEAD, slot, i);
+          for (uint32_t i = 0; i < A_LOADS; ++i) load_a(t + AHEAD, slot, i, STEADY);
         }
       }
       if (m + 1u == NA && more_b) {
 #pragma unroll
-        for (uint32_t i = 0; i <= B_LOADS; ++i) load_b(t / 4u + 2u, i);
+        for (uint32_t i = 0; i <= B_LOADS; ++i) load_b(t / 4u + 2u, i, STEADY);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -546,16 +547,16 @@ __global__ __launch_bounds__(512) void mx4_wide_kernel(ProductArgs a) {
   if (steps != 0u) {
     // in the order in which steps before the first would have asked for them, by which the waits count
 #pragma unroll
-    for (uint32_t i = 0; i <= B_LOADS; ++i) load_b(0, i);
+    for (uint32_t i = 0; i <= B_LOADS; ++i) load_b(0, i, false);
 #pragma unroll
     for (uint32_t t = 0; t < AHEAD; ++t)
       if (t < steps) {
 #pragma unroll
-        for (uint32_t i = 0; i < A_LOADS; ++i) load_a(t, t, i);
+        for (uint32_t i = 0; i < A_LOADS; ++i) load_a(t, t, i, false);
       }
     if (stages > 1u) {
 #pragma unroll
-      for (uint32_t i = 0; i <= B_LOADS; ++i) load_b(1, i);
+      for (uint32_t i = 0; i <= B_LOADS; ++i) load_b(1, i, false);
     }
     if (steps > 4u && steps >= AHEAD) wait_for_loads<(AHEAD - 1u) * A_LOADS + B_LOADS + 1u>();
     else wait_for_loads<0>();
@@ -592,7 +593,7 @@ __global__ __launch_bounds__(512) void mx4_wide_kernel(ProductArgs a) {
       f32x4 v[BLOCKS];
 #pragma unroll
       for (uint32_t b = 0; b < BLOCKS; ++b) v[b] = acc[n + b][m];
-      store_blocks<BM == 256u>(a, top, rows, c0 + cb + n * SIDE, a.wide, v);
+      store_blocks<false>(a, top, rows, c0 + cb + n * SIDE, a.wide, v);
     }
   }
 }
