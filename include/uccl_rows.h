@@ -95,13 +95,15 @@ uint64_t uccl_norm_rows_scratch(uint32_t rows, uint32_t cols);
  * uccl_group_product -- y[i] = x[index[i]] . w[g]^T for the rows i of every group g: offsets[g] <= i < offsets[g + 1].
  *
  *   y        written: n columns, UCCL_F32, UCCL_BF16 or UCCL_F16.  Rows of no group are left alone
- *   x        read: k columns, UCCL_BF16, UCCL_F16 or UCCL_E4M3
+ *   x        read: k columns, UCCL_BF16, UCCL_F16, UCCL_E4M3 or UCCL_MX4
  *   index    read: the row of x for every row of y, int32, 4-byte aligned; NULL = row i itself.  A row may be named any
  *            number of times; a number that is no row of x stands for a row of zeros
- *   w        read: n_groups * n rows of k columns, x's type; the n rows of a group follow each other
+ *   w        read: n_groups * n rows of k columns, x's type, or UCCL_MX4 beside rows in 16 bits; the n rows of a group follow each other
  *   offsets  read: n_groups + 1 int32, 4-byte aligned, in ascending order; one that is below its predecessor counts as
  *            that, below 0 as 0, above the rows of y as these
- * Sums are held in binary32 and rounded once; 8-bit operands are multiplied as they are, exactly, and the sum by both scales.
+ * Sums are held in binary32 and rounded once; 8-bit operands are multiplied as they are, exactly, and the sum by both scales.  Operands in 4 bits stand
+ * for their values with their blocks' scales: of two of them a block's 32 products are added exactly; beside rows in 16 bits they are what
+ * bf16 holds exactly, or f16.
  * What a call is cut into depends on its sizes alone, never on the offsets' values.
  */
 int uccl_group_product(const uccl_rows* y, const uccl_rows* x, const int32_t* index, const uccl_rows* w,

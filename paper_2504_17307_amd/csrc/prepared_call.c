@@ -180,37 +180,62 @@ static int contiguous(const DlTensor* t, int64_t* n) {
   return dense || all == 0;
 }
 
-/* contiguous_rows(functions, tensors, like, most): the bytes of one uccl_rows for every tensor of the list, or None: one of them is not contiguous, of a type
+static const DlFunctions* functions;
+static PyTypeObject* tensor_types[2];   /* torch.Tensor and torch.nn.Parameter: what another object would be taken for is not known */
+
+/* read_tensors(functions, torch.Tensor, torch.nn.Parameter): whether tensors can be read by the functions below. */
+static PyObject* read_tensors(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
+  (void)self;
+  functions = NULL;
+  if (n_args != 3 || !PyCapsule_CheckExact(args[0]) || !PyType_Check(args[1]) || !PyType_Check(args[2])) Py_RETURN_FALSE;
+  const DlFunctions* const f = (const DlFunctions*)PyCapsule_GetPointer(args[0], PyCapsule_GetName(args[0]));
+  if (f == NULL) return NULL;
+  if (f->major != 1 || f->tensor_from_object == NULL) Py_RETURN_FALSE;
+  for (int i = 0; i < 2; ++i) {
+    Py_INCREF(args[i + 1]);
+    Py_XDECREF(tensor_types[i]);
+    tensor_types[i] = (PyTypeObject*)args[i + 1];
+  }
+  Py_INCREF(args[0]);   /* for the process's life */
+  functions = f;
+  Py_RETURN_TRUE;
+}
+
+static int read_tensor(PyObject* object, DlTensor* t) {
+  if (functions == NULL || (Py_TYPE(object) != tensor_types[0] && Py_TYPE(object) != tensor_types[1])) return 0;
+  if (functions->tensor_from_object(object, t) == 0) return 1;
+  PyErr_Clear();
+  return 0;
+}
+
+/* contiguous_rows(tensors, like, most): the bytes of one uccl_rows for every tensor of the list, or None: one of them is not contiguous, of a type
  * without rows, of more than `most` elements, or not of the shape, type and layout of the one beside it in `like`. */
 static PyObject* contiguous_rows(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
   (void)self;
-  if (n_args != 4 || !PyCapsule_CheckExact(args[0]) || !PyList_CheckExact(args[1]) || !PyList_CheckExact(args[2])) Py_RETURN_NONE;
-  const DlFunctions* const f = (const DlFunctions*)PyCapsule_GetPointer(args[0], PyCapsule_GetName(args[0]));
-  const long long most = PyLong_AsLongLong(args[3]);
-  if (f == NULL || PyErr_Occurred()) return NULL;
-  const Py_ssize_t n = PyList_GET_SIZE(args[1]);
-  if (f->major != 1 || f->tensor_from_object == NULL || PyList_GET_SIZE(args[2]) != n) Py_RETURN_NONE;
-  PyTypeObject* const type = n == 0 ? NULL : Py_TYPE(PyList_GET_ITEM(args[1], 0));
+  if (n_args != 3 || !PyList_CheckExact(args[0]) || !PyList_CheckExact(args[1])) Py_RETURN_NONE;
+  const long long most = PyLong_AsLongLong(args[2]);
+  if (PyErr_Occurred()) return NULL;
+  const Py_ssize_t n = PyList_GET_SIZE(args[0]);
+  if (PyList_GET_SIZE(args[1]) != n) Py_RETURN_NONE;
   PyObject* const bytes = PyBytes_FromStringAndSize(NULL, n * (Py_ssize_t)sizeof(RowsStruct));
   if (bytes == NULL) return NULL;
   RowsStruct* const out = (RowsStruct*)PyBytes_AS_STRING(bytes);
   for (Py_ssize_t i = 0; i < n; ++i) {
-    PyObject *const a = PyList_GET_ITEM(args[1], i), *const b = PyList_GET_ITEM(args[2], i);
+    PyObject *const a = PyList_GET_ITEM(args[0], i), *const b = PyList_GET_ITEM(args[1], i);
     DlTensor t, u;
     int64_t elements, others;
-    int fits = Py_TYPE(a) == type && Py_TYPE(b) == type && f->tensor_from_object(a, &t) == 0;
+    int fits = read_tensor(a, &t);
     if (fits) {
       fits = contiguous(&t, &elements) && elements <= most && t.dtype.lanes == 1;
       const int f32 = t.dtype.code == 2 && t.dtype.bits == 32, f16 = t.dtype.code == 2 && t.dtype.bits == 16, bf16 = t.dtype.code == 4 && t.dtype.bits == 16;
       fits = fits && (f32 || f16 || bf16);
-      if (fits) out[i] = (RowsStruct){(uint64_t)(uintptr_t)t.data + t.byte_offset, (uint64_t)elements * (t.dtype.bits / 8), 0, 0, 1, (uint32_t)elements, f32 ? 0u : bf16 ? 1u : 2u, 0};
+      if (fits) out[i] = (RowsStruct){(uint64_t)(uintptr_t)t.data + t.byte_offset, (uint64_t)(elements == 0 ? 1 : elements) * (t.dtype.bits / 8), 0, 0, 1, (uint32_t)elements, f32 ? 0u : bf16 ? 1u : 2u, 0};
     }
     if (fits && a != b) {
-      fits = f->tensor_from_object(b, &u) == 0 && u.ndim == t.ndim && u.dtype.code == t.dtype.code && u.dtype.bits == t.dtype.bits && contiguous(&u, &others);
+      fits = read_tensor(b, &u) && u.ndim == t.ndim && u.dtype.code == t.dtype.code && u.dtype.bits == t.dtype.bits && contiguous(&u, &others);
       for (int32_t d = 0; fits && d < t.ndim; ++d) fits = u.shape[d] == t.shape[d];
     }
     if (!fits) {
-      PyErr_Clear();
       Py_DECREF(bytes);
       Py_RETURN_NONE;
     }
@@ -218,31 +243,24 @@ static PyObject* contiguous_rows(PyObject* self, PyObject* const* args, Py_ssize
   return bytes;
 }
 
-static const DlFunctions* functions_of(PyObject* capsule) {
-  const DlFunctions* const f = PyCapsule_CheckExact(capsule) ? (const DlFunctions*)PyCapsule_GetPointer(capsule, PyCapsule_GetName(capsule)) : NULL;
-  return f != NULL && f->major == 1 ? f : NULL;
-}
-
-/* vector_address(functions, tensor, whether it is float32 and not int32, elements): where it is, or None: it is not contiguous, of another type or length. */
+/* vector_address(tensor, whether it is float32 and not int32, elements): where it is, or None: it is not contiguous, of another type or length. */
 static PyObject* vector_address(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
   (void)self;
-  const DlFunctions* const f = n_args == 4 ? functions_of(args[0]) : NULL;
   DlTensor t;
   int64_t elements;
-  if (f == NULL || f->tensor_from_object(args[1], &t) != 0 || t.dtype.bits != 32 || t.dtype.lanes != 1 || t.dtype.code != (args[2] == Py_True ? 2 : 0) || !contiguous(&t, &elements) ||
-      elements != PyLong_AsLongLong(args[3])) {
+  if (n_args != 3 || !read_tensor(args[0], &t) || t.dtype.bits != 32 || t.dtype.lanes != 1 || t.dtype.code != (args[1] == Py_True ? 2 : 0) || !contiguous(&t, &elements) ||
+      elements != PyLong_AsLongLong(args[2])) {
     PyErr_Clear();
     Py_RETURN_NONE;
   }
   return PyLong_FromUnsignedLongLong((uint64_t)(uintptr_t)t.data + t.byte_offset);
 }
 
-/* matrix_rows(functions, tensor): the bytes of its uccl_rows, or None: it is of a type with scales, or not a matrix by rows of fewer than 2^32 rows and columns. */
+/* matrix_rows(tensor): the bytes of its uccl_rows, or None: it is of a type with scales, or not a matrix by rows of fewer than 2^32 rows and columns. */
 static PyObject* matrix_rows(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
   (void)self;
-  const DlFunctions* const f = n_args == 2 ? functions_of(args[0]) : NULL;
   DlTensor t;
-  if (f != NULL && f->tensor_from_object(args[1], &t) == 0 && t.strides != NULL && t.dtype.lanes == 1 && (t.ndim == 2 || t.ndim == 3)) {
+  if (n_args == 1 && read_tensor(args[0], &t) && t.strides != NULL && t.dtype.lanes == 1 && (t.ndim == 2 || t.ndim == 3)) {
     const int f32 = t.dtype.code == 2 && t.dtype.bits == 32, f16 = t.dtype.code == 2 && t.dtype.bits == 16, bf16 = t.dtype.code == 4 && t.dtype.bits == 16;
     const int64_t groups = t.ndim == 3 ? t.shape[0] : 1, each = t.shape[t.ndim - 2], cols = t.shape[t.ndim - 1], last = t.strides[t.ndim - 1];
     int64_t step = t.strides[t.ndim - 2];
@@ -257,11 +275,11 @@ static PyObject* matrix_rows(PyObject* self, PyObject* const* args, Py_ssize_t n
       return PyBytes_FromStringAndSize((const char*)&r, sizeof r);
     }
   }
-  PyErr_Clear();
   Py_RETURN_NONE;
 }
 
-static PyMethodDef methods[] = {{"vector_address", (PyCFunction)(void (*)(void))vector_address, METH_FASTCALL, NULL},
+static PyMethodDef methods[] = {{"read_tensors", (PyCFunction)(void (*)(void))read_tensors, METH_FASTCALL, NULL},
+                                {"vector_address", (PyCFunction)(void (*)(void))vector_address, METH_FASTCALL, NULL},
                                 {"matrix_rows", (PyCFunction)(void (*)(void))matrix_rows, METH_FASTCALL, NULL},
                                 {"contiguous_rows", (PyCFunction)(void (*)(void))contiguous_rows, METH_FASTCALL, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_prepared", NULL, -1, methods, NULL, NULL, NULL, NULL};

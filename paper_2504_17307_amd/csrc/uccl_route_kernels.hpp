@@ -13,6 +13,12 @@ namespace {
 template <uint32_t BY>
 __device__ __forceinline__ uint32_t turned(uint32_t v) { return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x120 + BY, 0xF, 0xF, true)); }   // within 16 lanes
 
+// What a wavefront's lanes have left in the LDS is there for its other lanes: its accesses are in order, so that only the compiler has to keep them so.
+__device__ __forceinline__ void left_for_other_lanes() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Reduce over a token's lanes; every lane has the result.
 template <uint32_t LANES, class F>
 __device__ __forceinline__ uint32_t over_lanes(uint32_t v, F f) {
@@ -181,6 +187,7 @@ __global__ __launch_bounds__(SUMS ? kRouteSumThreads : 256) void route_kernel(Ro
       p[v] = expf(s.z[v] - s.most);
       sum += p[v];
     }
+    left_for_other_lanes();
     sum = lanes_sum<LANES>(sum);
     const float per = per_sum(sum);
     if constexpr (SUMS) {
@@ -225,6 +232,7 @@ __global__ __launch_bounds__(SUMS ? kRouteSumThreads : 256) void route_kernel(Ro
           if (mine[k] >= 0) atomicAdd(&counted[mine[k]], 1u);
       }
     }
+    left_for_other_lanes();   // and read, before the next token's
   }
   if constexpr (SUMS) {
     const uint32_t wave = threadIdx.x / 64u;
@@ -376,9 +384,12 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
 #pragma unroll
     for (uint32_t k = 0; k < KEEP; ++k) {
       const uint32_t n = a.slots > k * LANES ? min(a.slots - k * LANES, LANES) : 0u;
-      for (uint32_t j = 0; j < n; ++j)
+      for (uint32_t j = 0; j < n; ++j) {
+        left_for_other_lanes();
         if (lane == j && mine[k] >= 0) chosen_part[mine[k]] += q[k];
+      }
     }
+    left_for_other_lanes();
 #pragma unroll
     for (uint32_t v = 0; v < V; ++v) p[v] += chosen_part[(v / N * LANES + lane) * N + v % N];
   }
@@ -469,6 +480,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     for (uint32_t e = lane; e < a.n_experts; e += 64u) seen[wave][e] = 0u;
 #pragma unroll
     for (uint32_t r = 0; r < ROUNDS; ++r) {
+      left_for_other_lanes();
       uint64_t same = ~0ull;
       for (uint32_t b = 0; b < bits; ++b) {
         const bool set = (expert[r] >> b & 1u) != 0u;
@@ -479,6 +491,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
       rank[r] = before;
       if (expert[r] < a.n_experts) {
         rank[r] += seen[wave][expert[r]];
+        left_for_other_lanes();
         if (before == 0u) seen[wave][expert[r]] = rank[r] + __popcll(same);   // one lane for each expert, when all have read
       }
     }

@@ -10,7 +10,7 @@ import os
 import struct
 
 from . import rows
-from .rows import _count, _find_tables, _rows, _vector
+from .rows import _count, _find_reader, _rows, _vector
 
 EXPERTS_HEADER_PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "uccl_experts.h")
 
@@ -118,9 +118,9 @@ def _matrices(tensors, like=None):
     """The bytes of a HOST array of uccl_rows, and how many there are; a contiguous tensor is one row, or whole rows and what is left.  Tensors are
     cut as those of ``like`` are, if there are any."""
     if type(tensors) is list and (like is None or type(like) is list):
-        tables = _find_tables() if rows._tables is None else rows._tables
-        if tables:
-            made = tables[0].contiguous_rows(tables[1], tensors, tensors if like is None else like, _LONGEST)
+        reader = _find_reader() if rows._reader is None else rows._reader
+        if reader:
+            made = reader.contiguous_rows(tensors, tensors if like is None else like, _LONGEST)
             if made is not None:
                 return made, len(tensors)
     made = []

@@ -54,22 +54,22 @@ def _type(dtype):
     return _types[dtype]
 
 
-_tables = None   # (the extension, DLPack's functions of torch's tensors), or (): not to be had
+_reader = None   # the extension, if it reads tensors; False: it does not
 
 
-def _find_tables():
-    """The extension's functions that read tensors, if they read a matrix and a vector as this module does."""
-    global _tables
+def _find_reader():
+    """The extension, if it reads a matrix and a vector as this module does."""
+    global _reader
     import torch
     from . import _load_extension
     extension, table = _load_extension(), getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
-    _tables = ()
-    if extension and table is not None:
+    _reader = False
+    if extension and table is not None and extension.read_tensors(table, torch.Tensor, torch.nn.Parameter):
         matrix, vector = torch.zeros(3, 8, dtype=torch.bfloat16)[1:, :5], torch.zeros(7, dtype=torch.int32)
         want, address = _rows(matrix), vector.data_ptr()
-        if extension.matrix_rows(table, matrix) == want and extension.vector_address(table, vector, False, 7) == address:
-            _tables = extension, table
-    return _tables
+        if extension.matrix_rows(matrix) == want and extension.vector_address(vector, False, 7) == address:
+            _reader = extension
+    return _reader
 
 
 def _rows(t, scales=None, cols_in_4_bits=None):
@@ -78,9 +78,9 @@ def _rows(t, scales=None, cols_in_4_bits=None):
     if t is None:
         return None
     if scales is None:
-        tables = _find_tables() if _tables is None else _tables
-        if tables:
-            made = tables[0].matrix_rows(tables[1], t)
+        reader = _find_reader() if _reader is None else _reader
+        if reader:
+            made = reader.matrix_rows(t)
             if made is not None:
                 return made
     number, size = _types.get(t.dtype) or _type(t.dtype)
@@ -135,8 +135,8 @@ def _vector(t, kind, n, what):
     """The address of `n` contiguous elements of `kind` (i: int32, f: float32); None for None."""
     if t is None:
         return None
-    if _tables:
-        address = _tables[0].vector_address(_tables[1], t, kind == "f", n)
+    if _reader:
+        address = _reader.vector_address(t, kind == "f", n)
         if address is not None:
             return address
     if t.element_size() != 4 or t.is_floating_point() != (kind == "f") or not t.is_contiguous() or t.numel() != n:

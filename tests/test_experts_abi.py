@@ -225,6 +225,31 @@ def test_the_binding_refuses_what_only_the_tensors_know():
     assert e.value.code == EINVAL
 
 
+def test_tensors_are_read_as_the_interpreter_reads_them(monkeypatch):
+    """By the extension and without it: matrices, vectors and lists, and what neither takes."""
+    import torch
+    from paper_2504_17307_amd import experts, rows as r
+    reader = r._find_reader()
+    assert reader
+    matrices = [torch.zeros(s, dtype=t) for s in ((3, 8), (1, 7), (0, 4), (4, 0), (2, 3, 8), (2, 1, 5), (1, 1, 1)) for t in (torch.float32, torch.bfloat16, torch.float16)]
+    matrices += [torch.zeros(6, 16)[::2, :5], torch.zeros(4, 6, 8)[:, :1], torch.zeros(2, 4, 8)[1:, :2], torch.zeros(9, 1).expand(9, 1), torch.nn.Parameter(torch.zeros(3, 4)), torch.zeros(5, 8).t()[:1].t()]
+    vectors = [torch.zeros(7), torch.zeros(7, dtype=torch.int32), torch.zeros(7, 1), torch.zeros(14)[::2], torch.zeros(7, dtype=torch.float64), torch.zeros(7, dtype=torch.int64), torch.zeros(6), torch.zeros(7, dtype=torch.uint32)]
+    lists = [[torch.zeros(3, 4), torch.zeros(5, dtype=torch.bfloat16)], [torch.zeros(()), torch.zeros(0)], [torch.nn.Parameter(torch.zeros(3)), torch.zeros(3)], [torch.zeros(8, 8)[:, :4]], [torch.zeros(4, dtype=torch.float16)] * 3, []]
+    def answers():
+        got = []
+        for call in [lambda m=m: r._rows(m) for m in matrices] + [lambda v=v, k=k: r._vector(v, k, 7, "v") for v in vectors for k in "if"] + [lambda x=x: experts._matrices(x) for x in lists]:
+            try:
+                got.append(call())
+            except ValueError as e:
+                got.append(str(e))
+        return got
+    fast = answers()
+    monkeypatch.setattr(r, "_reader", False)
+    assert fast == answers()
+    for thing in (None, 3, "x", [1], object()):                              # not taken for tensors
+        assert reader.matrix_rows(thing) is None and reader.vector_address(thing, False, 7) is None and reader.contiguous_rows([thing], [thing], 9) is None
+
+
 def test_kernels_use_no_scratch_memory(tmp_path):
     """The library's code objects of routing and clipping, and of 4 bits."""
     lib, at, blocks = open(pkg.LIB_PATH, "rb").read(), -1, []

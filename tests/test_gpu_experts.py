@@ -193,6 +193,7 @@ def test_route_grad(uccl, dtype, tokens, n, slots):
     experts = choice(scores, torch.randn(n, device="cuda", generator=g), slots).to(torch.int32)
     if tokens > 8:
         experts[7, 0], experts[8, -1] = n, 1 << 30                        # no experts
+        experts[6] = experts[6, 0].item()                                 # the same one in every slot
     dw, ds = torch.randn(tokens, slots, device="cuda", generator=g), torch.randn(n, device="cuda", generator=g)
     for e, d, s, normalise, scale in ((experts, dw, ds, True, 2.5), (experts, dw, None, False, 1.0), (experts, dw, ds, False, -1.5), (experts, dw, None, True, 1.0), (None, None, ds, False, 1.0)):
         out = aligned(tokens, n, t, 2)
@@ -537,6 +538,23 @@ def test_product_of_an_odd_number_of_columns_by_the_struct(uccl, kind):
     assert uccl.load().uccl_group_product(yr, xr, None, rows_of(w, ws, wide), offsets.data_ptr(), 1, torch.cuda.current_stream().cuda_stream) == 0
     want, mag = product_reference(dx, decode(w, ws, cols)[None], None, [0, rows])
     close(y, want, mag, cols, kind)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows", [3, 100, 700])
+def test_product_of_no_columns_and_of_no_rows(uccl, kind, rows):
+    """Empty sums; and rows that an index takes from nothing."""
+    import ctypes as C
+    wide, offsets, index = 300, torch.tensor([0, rows - 1], dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    some = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda").data_ptr()
+    code = {"mx4": uccl.UCCL_MX4, "bf16": uccl.UCCL_BF16, "f16": uccl.UCCL_F16}[kind]
+    for x_rows, cols, take in ((rows, 0, None), (0, 256, index)):
+        y = torch.full((rows, wide), 7.0, device="cuda")
+        yr = C.byref(uccl.uccl_rows(y.data_ptr(), wide * 4, None, 0, rows, wide, uccl.UCCL_F32, 0))
+        xr = C.byref(uccl.uccl_rows(some, 512, some if kind == "mx4" else None, 8, x_rows, cols, code, 0))
+        wr = C.byref(uccl.uccl_rows(some, 128, some, 8, wide, cols, uccl.UCCL_MX4, 0))
+        assert uccl.load().uccl_group_product(yr, xr, None if take is None else take.data_ptr(), wr, offsets.data_ptr(), 1, torch.cuda.current_stream().cuda_stream) == 0
+        assert bool((y[:rows - 1] == 0).all()) and bool((y[rows - 1:] == 7).all())
 
 
 @pytest.mark.parametrize("kind", KINDS)
