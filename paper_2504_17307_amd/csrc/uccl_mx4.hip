@@ -30,6 +30,9 @@ int product_4(const ProductArgs& a, hipStream_t s) {
   const double tiles = fmax(rounds_of(small_tiles, 512.0) * (1.0 + 0.7 * fmin(1.0, small_tiles / 256.0)), used_groups(a) * wide * 3.0e-5);
   if (few < tiles && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 32u) <= 1u << 23)
     return product_tiles<kForward>(mx4_few_kernel<kRows4, 32, 4, 3>, 16, 32, 256, a, s);
+  // 64 x 128 while there is a compute unit for each: 725 rows in 2 of 9 groups, 4839 -> 1929, 22 -> 19 us; 500 rows in 8 groups, 7168 -> 2048, 27.3 -> 26.4; 600 rows in one, 2048 -> 2048, 10.9 -> 8.8;
+  // 1000 rows in 16 groups, where there is not, 44 -> 56
+  if (tiles_down(a, 64u) * blocks_for(a.wide, 128u) <= 256.0) return product_tiles<kForward>(mx4_tile_kernel<64, 128, 2, 4, 2>, 64, 128, 512, a, s);
   const double across = blocks_for(a.wide, 256u), large = rounds_of(tiles_down(a, 256u) * across, 256.0), middle = 0.91 * rounds_of(tiles_down(a, 192u) * across, 256.0);
   const double small = 0.62 * rounds_of(small_tiles, 512.0);
   if (large <= middle && large <= small) return product_tiles<kForward>(mx4_tile_kernel<256, 256, 2, 4, 6>, 256, 256, 512, a, s);
@@ -37,20 +40,24 @@ int product_4(const ProductArgs& a, hipStream_t s) {
   return product_tiles<kForward>(mx4_tile_kernel<128, 128, 2, 4, 3>, 128, 128, 512, a, s);
 }
 
-// Rows of 16 bits, the same.  Few rows by 64 columns: 2.9e-5 for 16 rows of a column, 3.3e-5 for a column's weights; by 16 columns where that would leave most compute units idle; tiles of 128 x 128: 2.4 a
-// round.  Measured in bf16, by 64 columns / 16 columns / 128 x 128 / 128 x 256, 7168 -> 2048, us: one group, 1 / 100 rows, 11.1 / 14.7, 7.4 / 32, - / 61, - / 92; 8 of 32 groups, 16 rows, 15 / 28 / 57 / 73; 32 groups, 128 rows,
-// 65 / 100 / 122 / 93; 8 groups, 300 rows, 40 / 87 / 61 / 79; 16 groups, 1000 rows, 122 / 269 / 74 / 107; 4096 rows 429 / - / 207 / 215; 4000 rows in 4 groups - / - / 142 / 122; 2999 rows in 24 groups, 2043 -> 1003,
-// 80 / - / 45 / 36; 8192^3 3510 / - / 1330 / 1020.
+// Rows of 16 bits, the same.  Few rows by 64 columns: 2.9e-5 for 16 rows of a column, 3.3e-5 for a column's weights; by 16 columns where that would leave most compute units idle.
+// Tiles, in units of a round of 128 x 256 (114 us with a depth of 7168, 4.1 for 256 elements): 128 x 128 costs 0.57, 64 x 128, two on a compute unit, 0.66, and 0.37 while there is one on each.  Measured in bf16, 16 rows at a
+// time / 64 x 128 / 128 x 128 / 128 x 256, 7168 -> 2048, us: one group, 100 rows, 15 / - / 61 / 92; 8 of 32 groups, 16 rows, 15 / - / 57 / 73; 32 groups, 128 rows, 65 / - / 122 / 93; 8 groups, 300 rows, 40 / - / 61 / 79, 500 rows
+// 56 / 40 / 48 / 70; 16 groups, 1000 rows, 121 / 80 / 65 / 100, 4096 rows 428 / 180 / 187 / 200; 4000 rows in 4 groups 415 / 145 / 130 / 114; 8190 rows in 16 groups, 2048 -> 7168, - / 332 / 338 / 275; 2999 rows in 24
+// groups, 2043 -> 1003, 81 / 26 / 42 / 35, in f16 86 / 29 / 52 / 41; 8192^3 in bf16 by 128 x 256 952.  One row by 64 / 16 columns 11.1 / 7.4.
 template <Mx4Rows X>
 int product_16(const ProductArgs& a, hipStream_t s) {
-  const double wide = a.wide, small_tiles = tiles_down(a, 128u) * blocks_for(a.wide, 128u), few_tiles = fmax(tiles_down(a, 16u), used_groups(a));
-  const double few = fmax(tiles_down(a, 16u) * wide * 2.9e-5, used_groups(a) * wide * 3.3e-5);
-  if (few < 2.4 * rounds_of(small_tiles, 256.0) && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 16u) <= 1u << 23) {
+  constexpr bool F16 = X == kRowsF16;
+  const double wide = a.wide, narrow = blocks_for(a.wide, 128u), low_tiles = tiles_down(a, 64u) * narrow, few_tiles = fmax(tiles_down(a, 16u), used_groups(a));
+  const double large = rounds_of(tiles_down(a, 128u) * blocks_for(a.wide, 256u), 256.0), square = 0.57 * rounds_of(tiles_down(a, 128u) * narrow, 256.0);
+  const double low = low_tiles <= 256.0 ? 0.37 : 0.66 * rounds_of(low_tiles, 512.0), few = fmax(tiles_down(a, 16u) * wide * 2.9e-5, used_groups(a) * wide * 3.3e-5);
+  if (few < 4.1 * fmin(fmin(large, square), low) && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 16u) <= 1u << 23) {
     if (few_tiles * blocks_for(a.wide, 64u) <= 64.0) return product_tiles<kForward>(mx4_few_kernel<X, 16, 4, 3>, 16, 16, 256, a, s);
     return product_tiles<kForward>(mx4_few_kernel<X, 64, 4, 2>, 16, 64, 256, a, s);
   }
-  if (rounds_of(tiles_down(a, 128u) * blocks_for(a.wide, 256u), 256.0) <= 0.58 * rounds_of(small_tiles, 256.0)) return product_tiles<kForward>(mx4_wide_kernel<X == kRowsF16, 128, 256, 5>, 128, 256, 512, a, s);
-  return product_tiles<kForward>(mx4_wide_kernel<X == kRowsF16, 128, 128, 5>, 128, 128, 512, a, s);
+  if (low < square && low < large && (static_cast<uint64_t>(a.rows) / 64u + used_groups(a)) * static_cast<uint64_t>(narrow) <= 1u << 23) return product_tiles<kForward>(mx4_wide_kernel<F16, 64, 128, 5>, 64, 128, 512, a, s);
+  if (large <= square) return product_tiles<kForward>(mx4_wide_kernel<F16, 128, 256, 5>, 128, 256, 512, a, s);
+  return product_tiles<kForward>(mx4_wide_kernel<F16, 128, 128, 5>, 128, 128, 512, a, s);
 }
 
 }  // namespace
