@@ -208,39 +208,44 @@ static int read_tensor(PyObject* object, DlTensor* t) {
   return 0;
 }
 
-/* contiguous_rows(tensors, like, most): the bytes of one uccl_rows for every tensor of the list, or None: one of them is not contiguous, of a type
- * without rows, of more than `most` elements, or not of the shape, type and layout of the one beside it in `like`. */
+static int rows_of_contiguous(const DlTensor* t, int64_t most, RowsStruct* out) {
+  int64_t elements;
+  const int f32 = t->dtype.code == 2 && t->dtype.bits == 32, f16 = t->dtype.code == 2 && t->dtype.bits == 16, bf16 = t->dtype.code == 4 && t->dtype.bits == 16;
+  if (!(f32 || f16 || bf16) || t->dtype.lanes != 1 || !contiguous(t, &elements) || elements > most) return 0;
+  *out = (RowsStruct){(uint64_t)(uintptr_t)t->data + t->byte_offset, (uint64_t)(elements == 0 ? 1 : elements) * (t->dtype.bits / 8), 0, 0, 1, (uint32_t)elements, f32 ? 0u : bf16 ? 1u : 2u, 0};
+  return 1;
+}
+
+/* contiguous_rows(tensors, like, most): the bytes of one uccl_rows for every tensor of the first list, and for those of the second (the same list: the same bytes), or None: one
+ * of them is not contiguous, of a type without rows, of more than `most` elements, or not of the shape and type of the one beside it. */
 static PyObject* contiguous_rows(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
   (void)self;
   if (n_args != 3 || !PyList_CheckExact(args[0]) || !PyList_CheckExact(args[1])) Py_RETURN_NONE;
   const long long most = PyLong_AsLongLong(args[2]);
   if (PyErr_Occurred()) return NULL;
   const Py_ssize_t n = PyList_GET_SIZE(args[0]);
+  const int same = args[0] == args[1];
   if (PyList_GET_SIZE(args[1]) != n) Py_RETURN_NONE;
-  PyObject* const bytes = PyBytes_FromStringAndSize(NULL, n * (Py_ssize_t)sizeof(RowsStruct));
-  if (bytes == NULL) return NULL;
-  RowsStruct* const out = (RowsStruct*)PyBytes_AS_STRING(bytes);
-  for (Py_ssize_t i = 0; i < n; ++i) {
-    PyObject *const a = PyList_GET_ITEM(args[0], i), *const b = PyList_GET_ITEM(args[1], i);
+  PyObject* const first = PyBytes_FromStringAndSize(NULL, n * (Py_ssize_t)sizeof(RowsStruct));
+  PyObject* const second = same ? first : PyBytes_FromStringAndSize(NULL, n * (Py_ssize_t)sizeof(RowsStruct));
+  if (same) Py_XINCREF(second);
+  int fits = first != NULL && second != NULL;
+  for (Py_ssize_t i = 0; fits && i < n; ++i) {
     DlTensor t, u;
-    int64_t elements, others;
-    int fits = read_tensor(a, &t);
-    if (fits) {
-      fits = contiguous(&t, &elements) && elements <= most && t.dtype.lanes == 1;
-      const int f32 = t.dtype.code == 2 && t.dtype.bits == 32, f16 = t.dtype.code == 2 && t.dtype.bits == 16, bf16 = t.dtype.code == 4 && t.dtype.bits == 16;
-      fits = fits && (f32 || f16 || bf16);
-      if (fits) out[i] = (RowsStruct){(uint64_t)(uintptr_t)t.data + t.byte_offset, (uint64_t)(elements == 0 ? 1 : elements) * (t.dtype.bits / 8), 0, 0, 1, (uint32_t)elements, f32 ? 0u : bf16 ? 1u : 2u, 0};
-    }
-    if (fits && a != b) {
-      fits = read_tensor(b, &u) && u.ndim == t.ndim && u.dtype.code == t.dtype.code && u.dtype.bits == t.dtype.bits && contiguous(&u, &others);
+    fits = read_tensor(PyList_GET_ITEM(args[0], i), &t) && rows_of_contiguous(&t, most, (RowsStruct*)PyBytes_AS_STRING(first) + i);
+    if (fits && !same) {
+      fits = read_tensor(PyList_GET_ITEM(args[1], i), &u) && rows_of_contiguous(&u, most, (RowsStruct*)PyBytes_AS_STRING(second) + i) && u.ndim == t.ndim && u.dtype.code == t.dtype.code &&
+             u.dtype.bits == t.dtype.bits;
       for (int32_t d = 0; fits && d < t.ndim; ++d) fits = u.shape[d] == t.shape[d];
     }
-    if (!fits) {
-      Py_DECREF(bytes);
-      Py_RETURN_NONE;
-    }
   }
-  return bytes;
+  PyObject* const both = fits ? PyTuple_Pack(2, first, second) : NULL;
+  const int failed = first == NULL || second == NULL || (fits && both == NULL);
+  Py_XDECREF(first);
+  Py_XDECREF(second);
+  if (failed) return NULL;
+  if (both != NULL) return both;
+  Py_RETURN_NONE;
 }
 
 /* vector_address(tensor, whether it is float32 and not int32, elements): where it is, or None: it is not contiguous, of another type or length. */

@@ -115,35 +115,36 @@ _LONGEST = 1 << 30   # columns of a matrix
 
 
 def _matrices(tensors, like=None):
-    """The bytes of a HOST array of uccl_rows, and how many there are; a contiguous tensor is one row, or whole rows and what is left.  Tensors are
-    cut as those of ``like`` are, if there are any."""
-    if type(tensors) is list and (like is None or type(like) is list):
+    """The bytes of a HOST array of uccl_rows for ``tensors``, of another for those of ``like``, which have their shapes and types (by default they themselves), and how many matrices there
+    are: a contiguous tensor is one row, or whole rows and what is left; two tensors are cut alike."""
+    like = tensors if like is None else like
+    if type(tensors) is list and type(like) is list:
         reader = _find_reader() if rows._reader is None else rows._reader
-        if reader:
-            made = reader.contiguous_rows(tensors, tensors if like is None else like, _LONGEST)
-            if made is not None:
-                return made, len(tensors)
-    made = []
-    for i, t in enumerate(tensors):
-        other = t if like is None else like[i]
-        if t.shape != other.shape or t.dtype != other.dtype:
+        made = reader.contiguous_rows(tensors, like, _LONGEST) if reader else None
+        if made is not None:
+            return (*made, len(tensors))
+    made = [], []
+    for pair in zip(tensors, like):
+        if pair[0].shape != pair[1].shape or pair[0].dtype != pair[1].dtype:
             raise ValueError("outputs have the gradients' shapes and types")
-        if not (t.is_contiguous() and other.is_contiguous()):
-            made.append(_rows(t))
-            continue
-        flat = t.view(-1)
-        n = flat.shape[0]
-        if n > _LONGEST:
-            whole = n // _LONGEST * _LONGEST
-            made.append(_rows(flat[:whole].view(-1, _LONGEST)))
-            flat = flat[whole:]
-        made.append(_rows(flat.view(1, -1)))
-    return b"".join(made), len(made)
+        whole = pair[0].is_contiguous() and pair[1].is_contiguous()
+        for to, t in zip(made, pair):
+            if not whole:
+                to.append(_rows(t))
+                continue
+            flat = t.view(-1)
+            n = flat.shape[0]
+            if n > _LONGEST:
+                at = n // _LONGEST * _LONGEST
+                to.append(_rows(flat[:at].view(-1, _LONGEST)))
+                flat = flat[at:]
+            to.append(_rows(flat.view(1, -1)))
+    return b"".join(made[0]), b"".join(made[1]), len(made[0])
 
 
 def uccl_gradient_norm(norm, grads, scratch, stream=None):
     """The root of the sum of the squares of all elements of ``grads``, a list of tensors."""
-    m, n = _matrices(grads)
+    m, _, n = _matrices(grads)
     _call("uccl_gradient_norm", _vector(norm, "f", 1, "norm"), m, n, _ptr(scratch), _nbytes(scratch), _stream(stream))
 
 
@@ -156,8 +157,7 @@ def uccl_gradient_clip(outs, grads, norm, most, stream=None):
     """outs = grads min(1, most / norm), tensor by tensor; ``outs`` may be ``grads``."""
     if len(outs) != len(grads):
         raise ValueError("an output for every gradient")
-    to, n = _matrices(outs, grads)
-    of, _ = (to, n) if outs is grads else _matrices(grads, outs)
+    to, of, n = _matrices(outs, grads)
     _call("uccl_gradient_clip", to, of, n, _vector(norm, "f", 1, "norm"), _pack_clip(most, 0, 0, 0), _stream(stream))
 
 

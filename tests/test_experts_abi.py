@@ -235,9 +235,11 @@ def test_tensors_are_read_as_the_interpreter_reads_them(monkeypatch):
     matrices += [torch.zeros(6, 16)[::2, :5], torch.zeros(4, 6, 8)[:, :1], torch.zeros(2, 4, 8)[1:, :2], torch.zeros(9, 1).expand(9, 1), torch.nn.Parameter(torch.zeros(3, 4)), torch.zeros(5, 8).t()[:1].t()]
     vectors = [torch.zeros(7), torch.zeros(7, dtype=torch.int32), torch.zeros(7, 1), torch.zeros(14)[::2], torch.zeros(7, dtype=torch.float64), torch.zeros(7, dtype=torch.int64), torch.zeros(6), torch.zeros(7, dtype=torch.uint32)]
     lists = [[torch.zeros(3, 4), torch.zeros(5, dtype=torch.bfloat16)], [torch.zeros(()), torch.zeros(0)], [torch.nn.Parameter(torch.zeros(3)), torch.zeros(3)], [torch.zeros(8, 8)[:, :4]], [torch.zeros(4, dtype=torch.float16)] * 3, []]
+    kept = [list(x) for x in lists]
+
     def answers():
         got = []
-        for call in [lambda m=m: r._rows(m) for m in matrices] + [lambda v=v, k=k: r._vector(v, k, 7, "v") for v in vectors for k in "if"] + [lambda x=x: experts._matrices(x) for x in lists]:
+        for call in [lambda m=m: r._rows(m) for m in matrices] + [lambda v=v, k=k: r._vector(v, k, 7, "v") for v in vectors for k in "if"] + [lambda x=x: experts._matrices(x) for x in lists] + [lambda x=x, k=k: experts._matrices(x, [t.detach().clone() for t in kept[k]])[::2] for k, x in enumerate(lists)]:
             try:
                 got.append(call())
             except ValueError as e:
