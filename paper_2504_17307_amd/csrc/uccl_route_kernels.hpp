@@ -54,9 +54,7 @@ __device__ __forceinline__ uint32_t ordered(float key) {
   return key > -INFINITY ? b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u) : 0u;
 }
 // A key and its expert as one binary64, 2^52 and 42 bits: of equal keys the lower expert's is the greater, and the greatest of two is one instruction.
-__device__ __forceinline__ double ranked(uint32_t key, uint32_t expert) {
-  return __builtin_bit_cast(double, 0x4330000000000000ull | static_cast<uint64_t>(key) << 10 | (1023u - expert));
-}
+__device__ __forceinline__ u32x2 ranked(uint32_t key, uint32_t expert) { return u32x2{key << 10 | (1023u - expert), 0x43300000u | key >> 22}; }
 // (fmax would quiet NaNs first, which are none here.)
 __device__ __forceinline__ double greater(double a, double b) {
   double r;
@@ -88,10 +86,10 @@ __device__ __forceinline__ double greatest_of_lanes(double v) {
 }
 // The greatest of N, two by two.
 template <uint32_t N>
-__device__ __forceinline__ double greatest_of(const double (&v)[N]) {
+__device__ __forceinline__ double greatest_of(const u32x2 (&v)[N]) {
   double w[N];
 #pragma unroll
-  for (uint32_t i = 0; i < N; ++i) w[i] = v[i];
+  for (uint32_t i = 0; i < N; ++i) w[i] = __builtin_bit_cast(double, v[i]);
 #pragma unroll
   for (uint32_t n = N / 2u; n != 0u; n /= 2u)
 #pragma unroll
@@ -177,15 +175,25 @@ __global__ __launch_bounds__(SUMS ? kRouteSumThreads : 256) void route_kernel(Ro
     const uint64_t token = min(at, a.tokens - 1u);
     const S s(next, a.cols);
     if constexpr (SUMS) next = S::load(a.scores, min(static_cast<uint64_t>(at) + gridDim.x * EACH, a.tokens - 1ull), a.cols);   // (the last once more, for nothing)
-    double key[V];
+    u32x2 key[V];
     float sum = 0.0f, p[V];
 #pragma unroll
     for (uint32_t v = 0; v < V; ++v) {
       const uint32_t e = (v / N * LANES + lane) * N + v % N;
       scores[threadIdx.x / LANES][e] = s.z[v];
       key[v] = ranked(ordered(s.z[v] + bias[v]), e);
-      p[v] = expf(s.z[v] - s.most);
-      sum += p[v];
+    }
+    if (SUMS || a.normalise == 0u) {
+#pragma unroll
+      for (uint32_t v = 0; v < V; ++v) {
+        p[v] = expf(s.z[v] - s.most);
+        sum += p[v];
+      }
+    } else {   // only whether it is a number
+      bool number = true;
+#pragma unroll
+      for (uint32_t v = 0; v < V; ++v) number = number && s.z[v] < INFINITY;
+      sum = number ? 1.0f : __builtin_nanf("");
     }
     left_for_other_lanes();
     sum = lanes_sum<LANES>(sum);
@@ -201,7 +209,7 @@ __global__ __launch_bounds__(SUMS ? kRouteSumThreads : 256) void route_kernel(Ro
       const uint64_t found = __builtin_bit_cast(uint64_t, greatest_of_lanes<LANES>(greatest_of(key)));
       const uint32_t low = static_cast<uint32_t>(found);   // the expert's number is in it, so no other key has it
 #pragma unroll
-      for (uint32_t v = 0; v < V; ++v) key[v] = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, key[v])) == low ? 0.0 : key[v];
+      for (uint32_t v = 0; v < V; ++v) key[v][1] = key[v][0] == low ? 0u : key[v][1];   // below all others then
 #pragma unroll
       for (uint32_t k = 0; k < KEEP; ++k)
         if (j == k * LANES + lane && found >= 0x4330000000000400ull) mine[k] = static_cast<int32_t>(1023u - (low & 1023u));
