@@ -92,7 +92,8 @@ __device__ __forceinline__ double wave_sum_64(double v) {
   return v;
 }
 
-// Squares in binary64, which has them exactly and does not overflow.
+// Squares in binary64, which has them exactly and does not overflow; a workgroup's sum has its place, and they are added in a fixed order.  Bound by memory: three matrices of
+// together 1.88 GB f32 312 us, 6.0 TB/s; 300 of 9.5 MB bf16 together, two launches by the arguments' size, 6.7 and 5.5, which is latency.
 template <bool FLAT>
 __global__ __launch_bounds__(kGradientThreads) void square_sum_kernel(GradientArgs<FLAT> a) {
   __shared__ double buffer[kGradientThreads / 64u];
@@ -137,6 +138,7 @@ __device__ __forceinline__ void scale_pieces(const Matrix& m, uint64_t begin, ui
     });
 }
 
+// out = grad min(1, most / norm), the product in binary32, rounded once more to the type.  Bound by memory: 1.88 GB f32 709 us, 5.3 TB/s read and written.
 // The last workgroups' pieces first: they are what the norm has read last, and the caches have.
 template <bool FLAT, bool ONCE>
 __global__ __launch_bounds__(kGradientThreads) void gradient_clip_kernel(GradientArgs<FLAT> a) {

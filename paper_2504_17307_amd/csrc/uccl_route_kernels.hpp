@@ -143,8 +143,11 @@ struct Scores {
 // 1 / (sum of exp(z - most)); 0 for a token whose scores are all -infinity.
 __device__ __forceinline__ float per_sum(float sum) { return sum == 0.0f ? 0.0f : 1.0f / sum; }
 
-// The `slots` greatest keys one after the other: the greatest of the lane's own, then of the token's lanes'.
-// SUMS: workgroups take tokens in turn, and add up counts and probabilities in their order.
+// p = softmax(z), the `slots` experts of greatest z + bias, and of those p or the softmax over themselves, times scale.  The greatest keys come one after the other: the
+// greatest of the lane's own, then of the token's lanes'.  Few tokens are bound by that chain, many by the instructions (for f32, 256 experts and 8 slots with the sums about
+// 1200 a wavefront's four tokens, half of them in the choice), in neither case by memory.  Measured without sums, 8 slots, bf16, us: one token of 256 experts 4.0, 4096 of 256 6.6.
+// SUMS: workgroups take tokens in turn, and add up counts and probabilities in their order; no atomics between workgroups, so that the sums are the same from call to
+// call.  32768 x 256 f32 24 us and 4.5 for the workgroups' sums, of which reading takes 6.5; twice as many workgroups, of which a compute unit holds no more at once, 27 and 4.7.
 constexpr uint32_t kRouteSumThreads = 512;
 
 template <class T, uint32_t LANES, uint32_t K, bool SUMS>
@@ -314,7 +317,8 @@ struct RouteGradArgs {
 };
 
 // With g_j = scale dw_j: weights that are p themselves make dz_e = p_e (g_e - sum of g p), normalised ones dz_e = q_e (g_e - sum of g q), where q is the
-// softmax over the chosen; and the sums of probabilities add p_e (d_e - sum of d p).
+// softmax over the chosen; and the sums of probabilities add p_e (d_e - sum of d p).  p is made again from the scores, which are less to read than p kept in binary32 would be.
+// Measured: 32768 x 256 f32, 8 slots, 17.7 us, 3.9 TB/s; 456 x 64 f16 4.8, which is the chain of sums over lanes.
 template <class T, uint32_t LANES, uint32_t K>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
   using S = Scores<T, LANES, K>;
@@ -420,6 +424,7 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
+// loss = coef n / (slots tokens^2) sum of counts_e sums_e, whose gradient along sums_e is what counts_e is multiplied by.  One workgroup and a fixed order: 1.8 us, a launch.
 __global__ __launch_bounds__(256) void balance_kernel(float* loss, float* dsums, const int32_t* counts, const float* sums, uint32_t n, double factor) {
   __shared__ double parts[4];
   double v = 0.0;
@@ -438,7 +443,8 @@ __global__ __launch_bounds__(256) void balance_kernel(float* loss, float* dsums,
 //
 // A stable counting sort.  A workgroup has a share of the choices and goes through it by tiles, a wavefront a run of a tile's choices: a choice's place among its
 // expert's is the workgroup's first one, what earlier tiles, earlier wavefronts and earlier lanes of the same expert have.  Where there
-// are several workgroups, each has counted its share before.
+// are several workgroups, each has counted its share before.  Lanes of the same expert are found bit by bit of its number, by a ballot each: a chain, and what bounds this
+// (memory does not: 32768 choices are 0.4 MB).  Measured: 8 choices 3.2 us, 32768 of 256 experts 3.3 for the counts and 8.8 for the order.
 
 constexpr uint32_t kPlanThreads = 512, kPlanWaves = kPlanThreads / 64u, kMostExperts = 1024;
 

@@ -3,6 +3,7 @@
 Tolerances as in tests/test_gpu_expert_layer.py: every stage is computed from the stage before it as that was rounded.
 """
 import os
+import re
 import sys
 
 import pytest
@@ -97,3 +98,19 @@ def test_gradients_of_the_routed_layer_are_its_derivative(layer):
     by = torch.tensor(0.5, device="cuda") / got["norm"]
     assert all(torch.equal(c, g * by) for c, g in zip(got["clipped"].values(), grads))
     assert abs(float(torch.sqrt(sum((g.double() ** 2).sum() for g in got["clipped"].values()))) - 0.5) <= 1e-6
+
+
+def test_readme_example_of_routing_and_4_bits_runs(gpu_lib):
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    ns = {"torch": torch, "uccl": gpu_lib}
+    for code in re.findall(r"```python\n(.*?)```", text, re.S)[1:]:
+        exec(compile(code, "README.md", "exec"), ns)
+    chosen = choice(ns["scores"], None, 2)
+    assert torch.equal(ns["chosen"].long(), chosen)
+    assert bool(((ns["weight"].sum(1) - 1).abs() <= 4 * torch.finfo(torch.float32).eps).all())
+    first = ns["first"].tolist()
+    for e, (b, f) in enumerate(zip(first, first[1:])):
+        take = ns["index"][b:f].long()
+        assert torch.equal(take, (chosen == e).nonzero()[:, 0])
+        x, w = ns["x"][take].double(), decode(ns["w4"][e], ns["s4"][e], ns["cols"])
+        close(ns["y"][b:f], x @ w.T, x.abs() @ w.abs().T, ns["cols"], f"expert {e}")

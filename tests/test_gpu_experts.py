@@ -140,6 +140,30 @@ def test_route_of_scores_that_are_not_finite(uccl, n):
             assert bool(sums.isnan().all()) and torch.equal(counts.long(), torch.bincount(want[want >= 0], minlength=n))
 
 
+@pytest.mark.parametrize("tokens", [9, 2500])
+@pytest.mark.parametrize("n", [40, 100, 256, 700])
+@pytest.mark.parametrize("dtype", T)
+def test_route_without_sums_is_route_with_them(uccl, dtype, n, tokens):
+    """Normalised weights without sums are made without the sum over all experts: NaN and infinities of experts that are not chosen still count."""
+    scores = normal(gen(tokens + n), tokens, n, T[dtype])
+    scores[0, n - 1], scores[1, n - 1], scores[2, 0], scores[3, n // 2] = NAN, -INF, INF, NAN
+    scores[4, :], scores[5, :], scores[6, 1:] = -INF, NAN, -INF
+    scores[tokens - 1, n - 2] = NAN
+    bias = torch.zeros(n, device="cuda")
+    bias[n - 1] = -INF
+    for normalise in (False, True):
+        for b in (None, bias):
+            experts, w, alike, v = i32(tokens, 4), f32(tokens, 4), i32(tokens, 4), f32(tokens, 4)
+            uccl.uccl_route_rows(experts, w, scores, bias=b, normalise=normalise)
+            uccl.uccl_route_rows(alike, v, scores, bias=b, normalise=normalise, counts=i32(n), sums=f32(n), scratch=bytes_(uccl.uccl_route_rows_scratch(tokens, n)))
+            assert torch.equal(experts, alike) and torch.equal(w.view(torch.int32) << 1 == 0, v.view(torch.int32) << 1 == 0)
+            assert torch.equal(w.isnan(), v.isnan()) and torch.equal(w.nan_to_num(), v.nan_to_num())
+            for row in (0, 2, 3, 5, tokens - 1):
+                assert bool(w[row][experts[row] >= 0].isnan().all()), row
+            for row in (1, 4, 6, 7):
+                assert not bool(w[row].isnan().any()), row
+
+
 def test_route_by_a_bias_to_experts_whose_probability_is_nothing(uccl):
     """Normalised weights are relative to the chosen."""
     scores = aligned(2, 64, torch.float32)
