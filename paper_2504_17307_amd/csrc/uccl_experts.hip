@@ -79,17 +79,21 @@ int check_route(const uccl_rows* scores, const uccl_route_opts* o) {
 
 // ---- the order of rows ------------------------------------------------------------------------------
 
-constexpr uint32_t kPlanGroups = 128;   // workgroups, at most
+// Several workgroups, which have to know what the others' choices are: up to this many, each counts them all, beyond, or where the choices are written over, a launch before
+// has counted every workgroup's.  Measured, 256 experts, all counted by each / a launch before, us: 1280 choices 4.7 / 5.4, 8192 5.2 / 8.3, 32768 7.3 / 10.9,
+// 65536 10.5 / 13.1, of one expert all 11.6 / 13.6, 131072 17.5 / 17.5.
+constexpr uint64_t kPlanCountsAll = 1ull << 16;
+constexpr uint32_t kPlanGroups = 128;   // workgroups with a launch before, at most
 
-// How the choices are shared out.  A workgroup has 1024 or 2048 at a time: more of them at a time are fewer workgroups, each of which reads the others' counts.  Measured, 1024 / 2048 at a
-// time, 256 experts, us: 1024 choices 4.1 / 5.2, 2048 6.6 / 5.5 (one launch), 4096 7.6 / 8.7, 32768 11.6 / 11.2, 131072 26.5 / 18.6.
+// How the choices are shared out.  Where each workgroup counts them all, it has 512 at a time, one of a lane; with a launch before 1024 or 2048: more at a time are fewer workgroups, each of
+// which reads the others' counts.  Measured, 1024 / 2048 at a time, 256 experts, us: 4096 choices 7.6 / 8.7, 32768 11.6 / 11.2, 131072 26.5 / 18.6.
 struct PlanShape {
   uint32_t rounds, groups, share;
 };
-PlanShape plan_shape(uint64_t choices, uint32_t n_experts) {
-  const uint32_t rounds = choices <= 1024u || (choices > 2048u && (choices + 1023u) / 1024u * n_experts <= 4096u) ? 2u : 4u, tile = rounds * kPlanThreads;
-  const uint64_t tiles = (choices + tile - 1u) / tile, each = (tiles + kPlanGroups - 1u) / kPlanGroups;
-  if (each == 0u) return PlanShape{rounds, 1u, tile};
+PlanShape plan_shape(uint64_t choices, uint32_t n_experts, bool counts_all) {
+  const uint32_t rounds = counts_all ? 1u : (choices + 1023u) / 1024u * n_experts <= 4096u ? 2u : 4u, tile = rounds * kPlanThreads;
+  const uint64_t tiles = (choices + tile - 1u) / tile, each = counts_all ? 1u : (tiles + kPlanGroups - 1u) / kPlanGroups;
+  if (tiles == 0u) return PlanShape{rounds, 1u, tile};
   return PlanShape{rounds, static_cast<uint32_t>((tiles + each - 1u) / each), static_cast<uint32_t>(each * tile)};
 }
 
@@ -240,7 +244,7 @@ int uccl_balance_loss(float* loss, float* dsums, const int32_t* counts, const fl
 }
 
 uint64_t uccl_plan_rows_scratch(uint64_t choices, uint32_t n_experts) {
-  const uint32_t groups = plan_shape(choices, n_experts).groups;
+  const uint32_t groups = plan_shape(choices, n_experts, false).groups;
   return groups == 1u ? 0u : (groups * 4ull * n_experts + 15u) / 16u * 16u;
 }
 
@@ -250,19 +254,22 @@ int uccl_plan_rows(int32_t* index, int32_t* offsets, int32_t* pos, const int32_t
   if (choices > kMost || n_experts == 0u || n_experts > UCCL_MOST_EXPERTS || offsets == nullptr || (experts == nullptr && choices != 0u)) return UCCL_EINVAL;
   if (index != nullptr && (index == experts || index == pos)) return UCCL_EINVAL;
   if (misaligned(index, 4) || misaligned(offsets, 4) || misaligned(pos, 4) || misaligned(experts, 4)) return UCCL_EALIGN;
-  const PlanShape shape = plan_shape(choices, n_experts);
-  if (shape.groups > 1u) {
-    if (scratch == nullptr || scratch_bytes < uccl_plan_rows_scratch(choices, n_experts)) return UCCL_EINVAL;
+  const uint64_t needed = uccl_plan_rows_scratch(choices, n_experts);
+  if (needed != 0u) {
+    if (scratch == nullptr || scratch_bytes < needed) return UCCL_EINVAL;
     if (misaligned(scratch, 16)) return UCCL_EALIGN;
   }
+  const bool counts_all = choices <= kPlanCountsAll && pos != experts;
+  const PlanShape shape = plan_shape(choices, n_experts, counts_all);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   Launches go;
-  uint32_t* const counts = shape.groups > 1u ? static_cast<uint32_t*>(scratch) : nullptr;
+  uint32_t* const counts = counts_all || shape.groups == 1u ? nullptr : static_cast<uint32_t*>(scratch);
   const PlanArgs a{index, offsets, pos, experts, counts, static_cast<uint32_t>(choices), slots, n_experts, shape.share};
   if (counts != nullptr) {
     const int e = go(false, plan_count_kernel, shape.groups, kPlanThreads, s, counts, experts, a.choices, n_experts, shape.share);
     if (e != UCCL_OK) return e;
   }
+  if (counts_all) return go(true, plan_kernel<1>, shape.groups, kPlanThreads, s, a);
   return shape.rounds == 2u ? go(true, plan_kernel<2>, shape.groups, kPlanThreads, s, a) : go(true, plan_kernel<4>, shape.groups, kPlanThreads, s, a);
 }
 

@@ -443,17 +443,17 @@ __global__ __launch_bounds__(256) void balance_kernel(float* loss, float* dsums,
 //
 // A stable counting sort.  A workgroup has a share of the choices and goes through it by tiles, a wavefront a run of a tile's choices: a choice's place among its
 // expert's is the workgroup's first one, what earlier tiles, earlier wavefronts and earlier lanes of the same expert have.  Where there
-// are several workgroups, each has counted its share before.  Lanes of the same expert are found bit by bit of its number, by a ballot each: a chain, and what bounds this
-// (memory does not: 32768 choices are 0.4 MB).  Measured: 8 choices 3.2 us, 32768 of 256 experts 3.3 for the counts and 8.8 for the order.
+// are several workgroups, each counts all choices, or each has counted its share before.  Lanes of the same expert are found bit by bit of its number, by a ballot each: a chain, and what bounds this
+// (memory does not: 32768 choices are 0.4 MB).  Measured: 8 choices 3.1 us, 32768 of 256 experts 7.3.
 
-constexpr uint32_t kPlanThreads = 512, kPlanWaves = kPlanThreads / 64u, kMostExperts = 1024;
+constexpr uint32_t kPlanThreads = 512, kPlanWaves = kPlanThreads / 64u, kMostExperts = 1024, kPlanCounts = 2080 + 32;
 
 struct PlanArgs {
   int32_t* index;
   int32_t* offsets;
   int32_t* pos;
   const int32_t* experts;
-  const uint32_t* counts;   // [gridDim.x][n_experts], or nullptr: there is one workgroup
+  const uint32_t* counts;   // [gridDim.x][n_experts], or nullptr: there is one workgroup, or each counts all choices
   uint32_t choices, slots, n_experts, share;   // share: of a workgroup, a multiple of a tile
 };
 
@@ -475,8 +475,8 @@ template <uint32_t ROUNDS>
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   constexpr uint32_t TILE = kPlanThreads * ROUNDS;
   __shared__ uint32_t seen[kPlanWaves][kMostExperts];   // of the tile, by wavefront; then the first place of each wavefront
-  __shared__ uint32_t next[kMostExperts];               // the place of the workgroup's next choice of an expert
-  __shared__ uint32_t totals[kMostExperts];
+  __shared__ uint32_t next[kPlanCounts];               // the place of the workgroup's next choice of an expert
+  __shared__ uint32_t totals[kPlanCounts];
   __shared__ uint32_t sums[kPlanWaves];
   const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
   const uint64_t begin = static_cast<uint64_t>(blockIdx.x) * a.share, end = min(begin + a.share, static_cast<uint64_t>(a.choices));
@@ -514,10 +514,35 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   rank_tile();
   __syncthreads();
   // what the experts have in all, and in earlier workgroups
-  if (a.counts != nullptr) {
-    const uint32_t slices = a.n_experts < kPlanThreads ? kPlanThreads / a.n_experts : 1u;   // threads that share an expert's groups
-    for (uint32_t e = threadIdx.x; e < a.n_experts; e += kPlanThreads) totals[e] = next[e] = 0u;
+  uint32_t copies = 1u;
+  const uint32_t stride = a.n_experts | 1u;   // of copies: a count of an expert and its copies are in different banks
+  const bool counts_all = gridDim.x > 1u && a.counts == nullptr;
+  if (counts_all)
+    while (copies < 32u && copies * 2u * stride <= kPlanCounts - 32u) copies *= 2u;
+  if (gridDim.x > 1u) {
+    for (uint32_t i = threadIdx.x; i < copies * stride; i += kPlanThreads) totals[i] = next[i] = 0u;
     __syncthreads();
+  }
+  if (counts_all) {
+    // Copies of the counts for neighbouring lanes, as many as there is room for: 65536 choices of one expert 59 us without, 11.6 with 8 of them.  What is no expert lies behind them.
+    constexpr uint32_t AT_ONCE = 8, EACH = kPlanThreads * AT_ONCE;
+    const uint32_t mine = lane % copies * stride, none = copies * stride + lane % 32u;
+    auto count = [&](uint32_t first, bool whole) {
+      uint32_t e[AT_ONCE];
+#pragma unroll
+      for (uint32_t r = 0; r < AT_ONCE; ++r) {
+        const uint32_t c = first + r * kPlanThreads + threadIdx.x;
+        e[r] = whole || c < a.choices ? static_cast<uint32_t>(a.experts[c]) : a.n_experts;
+      }
+#pragma unroll
+      for (uint32_t r = 0; r < AT_ONCE; ++r) atomicAdd((first + r * kPlanThreads < begin ? next : totals) + (e[r] < a.n_experts ? mine + e[r] : none), 1u);
+    };
+    uint32_t first = 0;
+    for (; first + EACH <= a.choices; first += EACH) count(first, true);
+    if (first < a.choices) count(first, false);
+    __syncthreads();
+  } else if (a.counts != nullptr) {
+    const uint32_t slices = a.n_experts < kPlanThreads ? kPlanThreads / a.n_experts : 1u;   // threads that share an expert's groups
     for (uint32_t i = threadIdx.x; i < a.n_experts * slices; i += kPlanThreads) {
       const uint32_t slice = i / a.n_experts, e = i - slice * a.n_experts;
       uint32_t all = 0u, earlier = 0u;
@@ -539,9 +564,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     const uint32_t e = threadIdx.x * 2u + i;
     total[i] = before[i] = 0u;
     if (e < a.n_experts) {
-      if (a.counts != nullptr) {
-        total[i] = totals[e];
-        before[i] = next[e];
+      if (gridDim.x > 1u) {
+        for (uint32_t k = 0; k < copies; ++k) {
+          before[i] += next[k * stride + e];
+          total[i] += totals[k * stride + e];
+        }
+        if (counts_all) total[i] += before[i];
       } else {
 #pragma unroll
         for (uint32_t w = 0; w < kPlanWaves; ++w) total[i] += seen[w][e];
