@@ -177,7 +177,7 @@ __global__ __launch_bounds__(SUMS ? kRouteSumThreads : 256) void route_kernel(Ro
     const bool here = at < a.tokens;
     const uint64_t token = min(at, a.tokens - 1u);
     const S s(next, a.cols);
-    if constexpr (SUMS) next = S::load(a.scores, min(static_cast<uint64_t>(at) + gridDim.x * EACH, a.tokens - 1ull), a.cols);   // (the last once more, for nothing)
+    if constexpr (SUMS) next = S::load(a.scores, min(at + gridDim.x * EACH, a.tokens - 1u), a.cols);   // (the last once more, for nothing; tokens are fewer than 2^31)
     u32x2 key[V];
     float sum = 0.0f, p[V];
 #pragma unroll
