@@ -36,7 +36,7 @@ class Launches {
 
 // ---- routing ----------------------------------------------------------------------------------------
 
-constexpr uint32_t kRouteGroups = 256;   // that add up counts and probabilities, at most: one a compute unit
+constexpr uint32_t kRouteGroups = 512;   // that add up counts and probabilities, at most: two a compute unit
 
 // Few tokens: as many lanes for each as it has pieces, up to 64; many, which fill the machine: 16, where what goes over the lanes is done for four tokens at once.  Measured, 16 / as many,
 // 256 experts, with 8 slots, us: f32, 1 / 512 / 4096 / 32768 tokens, 4.8 / 5.2 / 5.5 / 20 against 3.5 / 3.6 / 6.8 / 31; the gradient 4.5 / 4.8 / 5.4 / 16 against 3.2 / 3.6 / 5.6 / 20; bf16, 4096 / 32768, 5.9 / 19.2

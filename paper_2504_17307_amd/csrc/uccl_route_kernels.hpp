@@ -145,46 +145,43 @@ __device__ __forceinline__ float per_sum(float sum) { return sum == 0.0f ? 0.0f 
 
 // p = softmax(z), the `slots` experts of greatest z + bias, and of those p or the softmax over themselves, times scale.  The greatest keys come one after the other: the
 // greatest of the lane's own, then of the token's lanes'.  Few tokens are bound by that chain, many by the instructions (for f32, 256 experts and 8 slots with the sums about
-// 1200 a wavefront's four tokens, half of them in the choice), in neither case by memory.  Measured without sums, 8 slots, bf16, us: one token of 256 experts 4.0, 4096 of 256 6.6.
+// 1200 a wavefront's four tokens, half of them in the choice), in neither case by memory.  Measured without sums, 8 slots, bf16, us: one token of 256 experts 3.6, 4096 of 256 5.3.
+// The biases lie in the LDS: in registers they took a wavefront's place, and each its own look at whether there are any (32768 tokens of 256 in bf16 19.2 us, 13.8 now).
 // SUMS: workgroups take tokens in turn, and add up counts and probabilities in their order; no atomics between workgroups, so that the sums are the same from call to
-// call.  32768 x 256 f32 24 us and 4.5 for the workgroups' sums, of which reading takes 6.5; twice as many workgroups, of which a compute unit holds no more at once, 27 and 4.7.
+// call.  The registers of four wavefronts' quarter, so that two workgroups are on a compute unit: 32768 x 256 f32 21.6 us,
+// and 3.8 for the workgroups' sums, of which reading takes 6.5; one workgroup on each 24 and 4.5.
 constexpr uint32_t kRouteSumThreads = 512;
 
 template <class T, uint32_t LANES, uint32_t K, bool SUMS>
-__global__ __launch_bounds__(SUMS ? kRouteSumThreads : 256) void route_kernel(RouteArgs a) {
+__global__ __launch_bounds__(SUMS ? kRouteSumThreads : 256, SUMS ? 4 : 1) void route_kernel(RouteArgs a) {
   using S = Scores<T, LANES, K>;
   constexpr uint32_t N = S::N, V = S::V, KEEP = 32u / LANES == 0u ? 1u : 32u / LANES, THREADS = SUMS ? kRouteSumThreads : 256u, EACH = THREADS / LANES;
   constexpr uint32_t WAVES = THREADS / 64u, MOST = LANES * V;
   __shared__ uint32_t counted[SUMS ? MOST : 1u];
   __shared__ float added[SUMS ? WAVES : 1u][SUMS ? MOST : 1u];
   __shared__ float scores[EACH][MOST];
+  __shared__ float biases[MOST];
   const uint32_t lane = threadIdx.x % LANES;
-  if constexpr (SUMS) {
-    for (uint32_t e = threadIdx.x; e < MOST; e += THREADS) counted[e] = 0u;
-    __syncthreads();
+  for (uint32_t e = threadIdx.x; e < MOST; e += THREADS) {
+    biases[e] = a.bias != nullptr ? a.bias[min(e, a.cols - 1u)] : 0.0f;
+    if constexpr (SUMS) counted[e] = 0u;
   }
-  float bias[V], total[V];
+  __syncthreads();
+  float total[V];
 #pragma unroll
-  for (uint32_t v = 0; v < V; ++v) {
-    const uint32_t e = (v / N * LANES + lane) * N + v % N;
-    bias[v] = a.bias != nullptr ? a.bias[min(e, a.cols - 1u)] : 0.0f;
-    total[v] = 0.0f;
-  }
-  typename S::Loaded next;
-  if (blockIdx.x * EACH < a.tokens) next = S::load(a.scores, min(blockIdx.x * EACH + threadIdx.x / LANES, a.tokens - 1u), a.cols);
+  for (uint32_t v = 0; v < V; ++v) total[v] = 0.0f;
   for (uint32_t first = blockIdx.x * EACH; first < a.tokens; first += gridDim.x * EACH) {
     const uint32_t at = first + threadIdx.x / LANES;
     const bool here = at < a.tokens;
     const uint64_t token = min(at, a.tokens - 1u);
-    const S s(next, a.cols);
-    if constexpr (SUMS) next = S::load(a.scores, min(at + gridDim.x * EACH, a.tokens - 1u), a.cols);   // (the last once more, for nothing; tokens are fewer than 2^31)
+    const S s(S::load(a.scores, token, a.cols), a.cols);
     u32x2 key[V];
     float sum = 0.0f, p[V];
 #pragma unroll
     for (uint32_t v = 0; v < V; ++v) {
       const uint32_t e = (v / N * LANES + lane) * N + v % N;
       scores[threadIdx.x / LANES][e] = s.z[v];
-      key[v] = ranked(ordered(s.z[v] + bias[v]), e);
+      key[v] = ranked(ordered(s.z[v] + biases[e]), e);
     }
     if (SUMS || a.normalise == 0u) {
 #pragma unroll

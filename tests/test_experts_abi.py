@@ -173,7 +173,7 @@ def test_gradient_clip_refusals(change, code):
 
 def test_scratch_sizes():
     f, g, h = pkg.uccl_route_rows_scratch, pkg.uccl_plan_rows_scratch, pkg.uccl_gradient_norm_scratch
-    assert f(0, 8) == f(32, 8) == 0 and f(33, 8) == 2 * 8 * 8 and f(1 << 31, 1024) == 256 * 8 * 1024
+    assert f(0, 8) == f(32, 8) == 0 and f(33, 8) == 2 * 8 * 8 and f(1 << 31, 1024) == 512 * 8 * 1024
     assert g(0, 8) == 0 and g(1 << 30, 1024) <= 1 << 20 and g(1 << 20, 3) % 16 == 0
     assert h(0) > 0 and h(1000) - h(0) >= 8000 and h(7) % 16 == 0
 
