@@ -39,8 +39,8 @@ class Launches {
 constexpr uint32_t kRouteGroups = 512;   // that add up counts and probabilities, at most: two a compute unit
 
 // Few tokens: as many lanes for each as it has pieces, up to 64; many, which fill the machine: 16, where what goes over the lanes is done for four tokens at once.  Measured, 16 / as many,
-// 256 experts, with 8 slots, us: f32, 1 / 512 / 4096 / 32768 tokens, 4.8 / 5.2 / 5.5 / 20 against 3.5 / 3.6 / 6.8 / 31; the gradient 4.5 / 4.8 / 5.4 / 16 against 3.2 / 3.6 / 5.6 / 20; bf16, 4096 / 32768, 5.9 / 19.2
-// against 5.8 / 19.1, with counts and sums 12.9 / 26.5 against 12.5 / 29.7.
+// 256 experts, with 8 slots, us: f32, 1 / 600 / 4096 / 32768 tokens, 4.3 / 5.2 / 4.9 / 14.7 against 3.3 / 3.7 / 5.6 / 25.7; the gradient 4.5 / 4.9 / 5.4 / 16.1 against 3.1 / 3.6 / 5.4 / 19.7; bf16, 4.4 / 4.5 /
+// 4.6 / 14.2 against 3.6 / 4.1 / 4.6 / 16.5.
 bool takes_16_lanes(uint32_t tokens, uint32_t cols) { return cols <= 256u && tokens > 2048u; }
 
 // Calls f with the lanes of a token and the pieces of a lane, for rows of `cols` elements of T.
