@@ -14,6 +14,7 @@
  * into a graph.  The results of a call on the same inputs are the same bit for bit.  `scratch` is device memory of at least as many bytes
  * as the call's _scratch function says, 16-byte aligned, the call's own until the stream has passed it; what it holds before is of no matter, and no two
  * calls that may run at the same time share it (two captured graphs, say).
+ * What a call writes overlaps nothing else that it reads or writes, but where an entry says that it may be the same.
  *
  * Every call returns UCCL_OK, also where there is nothing to compute; UCCL_EINVAL: a null pointer, shapes or types that do not match, a number
  * out of its range; UCCL_EALIGN; UCCL_ETOOBIG: more workgroups than one launch can have (2^32 threads); UCCL_ELAUNCH: HIP's, the text in
@@ -128,7 +129,7 @@ int uccl_quantise_rows(const uccl_rows* q, const uccl_rows* values, const uccl_r
  * uccl_gradient_clip -- out = grad * min(1, most / norm) for each of n matrices, products in binary32, then rounded to the type.
  *
  *   out      HOST array of n matrices, written: type and shape of the grad beside it, and may be that itself: then nothing is written where the
- *            factor is 1
+ *            factor is 1.  A matrix may be twice among the grads of a norm, and counts twice; among out each is once
  *   norm     read: one float, 4-byte aligned, as uccl_gradient_norm wrote it, or of more than one rank
  *   opts     most: above 0, finite
  * A norm of NaN makes every element NaN; one of infinity makes finite elements 0.
