@@ -20,24 +20,33 @@ double rounds_of(double tiles, double room) {
 
 // Rows of 4 bits, in us for 256 elements of the sum.  Few rows: 2.0e-5 for 16 rows of a column, 2.6e-5 for a column's weights where they are read once;
 // tiles of 128 x 128, two on a compute unit: 1.7 a round, 1 where most of them are idle.  Measured, 16 rows at a time / 128 x 128, 7168 -> 2048, us: one group, 1 / 100 rows, 8.0 / 10.4 against
-// 23 / 28; 8 of 32 groups, 16 rows, 13.3 against 28; 32 groups, 128 rows, 49 against 54; 8 groups, 300 rows, 26 against 29; 16 groups, 1000 rows, 81 against 47.
+// 23 / 28; 8 of 32 groups, 16 rows, 13.3 against 28; 32 groups, 128 rows, 49 against 54; 8 groups, 300 rows, 27 against 27; 16 groups, 1000 rows, 81 against 47.
 // Tiles: in units of one of 256 x 256 (67 us with a depth of 7168, one a compute unit) 192 x 256 costs 0.91, and 128 x 128 0.62, two on a compute unit.  Measured, 256 x 256 / 192 x 256 / 128 x 128, us:
 // 4096 rows in 16 ragged groups, 7168 -> 2048, 83 / 76 / 93; 2048 rows 77 / 73 / 66; 1000 rows 63 / 61 / 44; 4000 rows in 4 groups 67 / 61 / 51; 8192 rows in 8 groups 80 / 135 / 110; 8190 rows in 16 groups,
 // 2048 -> 7168, 131 / 139 / 137; 8192^3 313 / 367 / 429.  (128 x 256, of which one fits a compute unit, takes 52 where 128 x 128 takes 51, and more elsewhere.)
 int product_4(const ProductArgs& a, hipStream_t s) {
   const double wide = a.wide, small_tiles = tiles_down(a, 128u) * blocks_for(a.wide, 128u);
-  const double few = fmax(tiles_down(a, 16u) * wide * 2.0e-5, used_groups(a) * wide * 2.6e-5);
-  const double tiles = fmax(rounds_of(small_tiles, 512.0) * (1.0 + 0.7 * fmin(1.0, small_tiles / 256.0)), used_groups(a) * wide * 3.0e-5);
+  const double few_tiles = fmax(tiles_down(a, 16u), used_groups(a));
+  double few = fmax(tiles_down(a, 16u) * wide * 2.0e-5, used_groups(a) * wide * 2.6e-5);
+  double tiles = fmax(rounds_of(small_tiles, 512.0) * (1.0 + 0.7 * fmin(1.0, small_tiles / 256.0)), used_groups(a) * wide * 3.0e-5);
+  const double low_tiles = tiles_down(a, 64u) * blocks_for(a.wide, 128u), deep = blocks_for(a.cols, 256u);
+  const bool low = low_tiles <= 256.0;
+  // While there is a compute unit for each tile of 64 x 128, in us and with what a call takes at the least.  Measured, 16 rows at a time / 64 x 128, us: 691 rows in 12 groups, 2296 -> 1232, 19.6 / 11.2;
+  // one group, 227 rows, 5387 -> 1960, 16.2 / 16.7, 395 rows, 5152 -> 952, 13.9 / 16.2, 142 rows, 3640 -> 728, 7.0 / 12.2, 614 rows, 3304 -> 1923, 27.7 / 13.2.
+  if (low) {
+    few = 3.5 + fmax(0.65, few_tiles * blocks_for(a.wide, 32u) / 512.0) * (2.0 + 0.85 * ceil(deep / 4.0));
+    tiles = 5.0 + deep * (0.45 + 0.2 * low_tiles / 256.0);
+  }
   if (few < tiles && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 32u) <= 1u << 23)
     return product_tiles<kForward>(mx4_few_kernel<kRows4, 32, 4, 3>, 16, 32, 256, a, s);
   // 64 x 128 while there is a compute unit for each: 725 rows in 2 of 9 groups, 4839 -> 1929, 22 -> 19 us; 500 rows in 8 groups, 7168 -> 2048, 27.3 -> 26.4; 600 rows in one, 2048 -> 2048, 10.9 -> 8.8;
   // 1000 rows in 16 groups, where there is not, 44 -> 56
-  if (tiles_down(a, 64u) * blocks_for(a.wide, 128u) <= 256.0) return product_tiles<kForward>(mx4_tile_kernel<64, 128, 2, 4, 2>, 64, 128, 512, a, s);
+  if (low) return product_tiles<kForward>(mx4_tile_kernel<64, 128, 2, 4, 2, 3>, 64, 128, 512, a, s);
   const double across = blocks_for(a.wide, 256u), large = rounds_of(tiles_down(a, 256u) * across, 256.0), middle = 0.91 * rounds_of(tiles_down(a, 192u) * across, 256.0);
   const double small = 0.62 * rounds_of(small_tiles, 512.0);
-  if (large <= middle && large <= small) return product_tiles<kForward>(mx4_tile_kernel<256, 256, 2, 4, 6>, 256, 256, 512, a, s);
-  if (middle <= small) return product_tiles<kForward>(mx4_tile_kernel<192, 256, 2, 4, 5>, 192, 256, 512, a, s);
-  return product_tiles<kForward>(mx4_tile_kernel<128, 128, 2, 4, 3>, 128, 128, 512, a, s);
+  if (large <= middle && large <= small) return product_tiles<kForward>(mx4_tile_kernel<256, 256, 2, 4, 6, 2>, 256, 256, 512, a, s);
+  if (middle <= small) return product_tiles<kForward>(mx4_tile_kernel<192, 256, 2, 4, 5, 2>, 192, 256, 512, a, s);
+  return product_tiles<kForward>(mx4_tile_kernel<128, 128, 2, 4, 3, 2>, 128, 128, 512, a, s);
 }
 
 // Rows of 16 bits, the same.  Few rows by 64 columns: 2.9e-5 for 16 rows of a column, 3.3e-5 for a column's weights; by 16 columns where that would leave most compute units idle.
@@ -50,8 +59,15 @@ int product_16(const ProductArgs& a, hipStream_t s) {
   constexpr bool F16 = X == kRowsF16;
   const double wide = a.wide, narrow = blocks_for(a.wide, 128u), low_tiles = tiles_down(a, 64u) * narrow, few_tiles = fmax(tiles_down(a, 16u), used_groups(a));
   const double large = rounds_of(tiles_down(a, 128u) * blocks_for(a.wide, 256u), 256.0), square = 0.57 * rounds_of(tiles_down(a, 128u) * narrow, 256.0);
-  const double low = low_tiles <= 256.0 ? 0.37 : 0.66 * rounds_of(low_tiles, 512.0), few = fmax(tiles_down(a, 16u) * wide * 2.9e-5, used_groups(a) * wide * 3.3e-5);
-  if (few < 4.1 * fmin(fmin(large, square), low) && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 16u) <= 1u << 23) {
+  const double low = low_tiles <= 256.0 ? 0.37 : 0.66 * rounds_of(low_tiles, 512.0);
+  double few = fmax(tiles_down(a, 16u) * wide * 2.9e-5, used_groups(a) * wide * 3.3e-5), tiles = 4.1 * fmin(fmin(large, square), low);
+  // As in product_4().  Measured, 16 rows at a time / 64 x 128, us: bf16, 298 rows in 3 groups, 1545 -> 1757, 19.3 / 15.0, 412 in 3, 1176 -> 997, 12.9 / 11.6, 200 in 4, 7168 -> 2048, 27.7 / 37.5; one group,
+  // 385 rows, 4816 -> 1851, 33.4 / 29.3, 595 rows, 5096 -> 623, 24.5 / 30.0; f16, 85 rows in 5 groups, 3863 -> 1545, 13.0 / 28.1, 300 in 8, 7168 -> 2048, 44.4 / 53.6; 400 rows in one, 3000 -> 1900, 28.6 / 26.1.
+  if (low_tiles <= 256.0) {
+    few = 3.0 + ceil(few_tiles * blocks_for(a.wide, 64u) / 256.0 - 0.1) * (3.0 + 1.4 * ceil(blocks_for(a.cols, 256u) / 4.0)) * (F16 ? 1.08 : 1.0);
+    tiles = 7.0 + blocks_for(a.cols, 64u) * (F16 ? 0.33 + 0.14 * low_tiles / 256.0 : 0.25 + 0.07 * low_tiles / 256.0);
+  }
+  if (few < tiles && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 16u) <= 1u << 23) {
     if (few_tiles * blocks_for(a.wide, 64u) <= 64.0) return product_tiles<kForward>(mx4_few_kernel<X, 16, 4, 3>, 16, 16, 256, a, s);
     return product_tiles<kForward>(mx4_few_kernel<X, 64, 4, 2>, 16, 64, 256, a, s);
   }

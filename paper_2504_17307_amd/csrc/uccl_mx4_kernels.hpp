@@ -168,20 +168,22 @@ __device__ __forceinline__ bool exact_in_f16(uint32_t scale) { return scale - (1
 // ---- tiles, rows in 4 bits --------------------------------------------------------------------------
 
 // As product_tile_kernel: a stage is 128 bytes along the sum, 256 elements, and is multiplied in two halves; a half is one matrix instruction for
-// 16 x 16 of the output.  The LDS holds two stages of each operand.  When every wavefront has read its last fragments of a stage, a little into its
-// second half, the stage after the next one is asked for in its place, by loads that SPREAD rows of blocks have between them; the barrier there, which the
+// 16 x 16 of the output.  The LDS holds two stages of each operand, or RING: three where a compute unit has one small tile (64 x 128, 2551 rows, 5208 -> 523, 20.9 us with two and
+// 18.5 with three; five take as long: what is left is a stage's chain of reads, products and addresses).  When every wavefront has read its last fragments of a stage, a little into its
+// second half, the stage RING further is asked for in its place, by loads that SPREAD rows of blocks have between them; the barrier there, which the
 // next stage's arrival is waited for at too, is the only one in a stage.
 // Scales come 32 bytes of a row at a time, for four stages, into one of two places: a load of 64 words touches as few rows as one of 64 pieces does.  (4 bytes of
 // 64 rows at every stage: 8192^3 388 us, 306 without them.)
 // Bound by the loads into the LDS where the sum is long: 8192^3 by 256 x 256 313 to 338 us, 3.5 to 3.3 PFLOP/s, half of what the instruction does out of registers; by the one round
 // of tiles where groups are ragged: 4096 rows in 16 groups, 7168 -> 2048, 69 us by 192 x 256, about 240 tiles, half of them the last rows of a group.
-template <uint32_t BM, uint32_t BN, uint32_t WR, uint32_t WC, uint32_t SPREAD>
+template <uint32_t BM, uint32_t BN, uint32_t WR, uint32_t WC, uint32_t SPREAD, uint32_t RING>
 __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
   constexpr uint32_t THREADS = WR * WC * 64u, SIDE = 16u, NA = BM / WR / SIDE, NB = BN / WC / SIDE, EACH = THREADS / 8u;   // rows of a load
   constexpr uint32_t A_LOADS = BM / EACH, B_LOADS = BN / EACH, LOADS = A_LOADS + B_LOADS, S_LOADS = (LOADS + 1u) / 2u;   // of scales, in the first two of four stages
+  static_assert(RING == 2u || RING == 3u);   // scales of the first two of four stages have come when all but the newest stage's loads have
   constexpr uint32_t A_STAGE = BM * kStageBytes, B_STAGE = BN * kStageBytes, S_STAGE = (BM + BN) * 32u;
   static_assert(BM % EACH == 0u && BN % EACH == 0u);
-  __shared__ __align__(1024) char lds_a[2u * A_STAGE], lds_b[2u * B_STAGE], lds_s[2u * S_STAGE];
+  __shared__ __align__(1024) char lds_a[RING * A_STAGE], lds_b[RING * B_STAGE], lds_s[2u * S_STAGE];
   const char* zeros = reinterpret_cast<const char*>(page_of_zeros);
   asm volatile("" : "+s"(zeros));   // an address in registers: not looked up again at every load
   const uint32_t across = (a.wide + BN - 1u) / BN;
@@ -219,12 +221,12 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
       asm volatile("" : "+v"(r));
       const char* from = x_data + k * static_cast<uint64_t>(kStageBytes) + r * x_stride + own_piece;
       if (behind || r >= x_rows) from = zeros;
-      load_to_lds(from, __builtin_amdgcn_readfirstlane(here_a + k % 2u * A_STAGE + i * THREADS * 16u));
+      load_to_lds(from, __builtin_amdgcn_readfirstlane(here_a + k % RING * A_STAGE + i * THREADS * 16u));
     } else {
       const uint32_t n = i - A_LOADS;
       const char* from = columns >> n & 1u ? lb + n * EACH * w_stride : lb;
       if (behind) from = zeros;
-      load_to_lds(from, __builtin_amdgcn_readfirstlane(here_b + k % 2u * B_STAGE + n * THREADS * 16u));
+      load_to_lds(from, __builtin_amdgcn_readfirstlane(here_b + k % RING * B_STAGE + n * THREADS * 16u));
       if (n + 1u == B_LOADS) lb += kStageBytes;
     }
   };
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
     for (uint32_t r = threadIdx.x; r < BM + BN; r += THREADS) {
       const uint32_t in_operand = r < BM ? r : r - BM;
       if (in != 0u) {
-        uint32_t* piece = reinterpret_cast<uint32_t*>((r < BM ? lds_a + k % 2u * A_STAGE : lds_b + k % 2u * B_STAGE) + in_operand * kStageBytes + ((p ^ (in_operand >> 1 & 7u)) << 4));
+        uint32_t* piece = reinterpret_cast<uint32_t*>((r < BM ? lds_a + k % RING * A_STAGE : lds_b + k % RING * B_STAGE) + in_operand * kStageBytes + ((p ^ (in_operand >> 1 & 7u)) << 4));
 #pragma unroll
         for (uint32_t i = 0; i < 4u; ++i)
           if (in < (i + 1u) * 8u) piece[i] &= in <= i * 8u ? 0u : (1u << (in - i * 8u) * 4u) - 1u;
@@ -276,7 +278,7 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
   };
   auto places = [&](uint32_t k, uint32_t half) {
     const uint32_t piece = in_piece ^ half * 64u;
-    Places p{at_a + k % 2u * A_STAGE + piece, at_b + k % 2u * B_STAGE + piece, at_s + k / 4u % 2u * S_STAGE + ra * 32u + ((k % 4u * 8u + half * 4u) ^ in_word), 0u};
+    Places p{at_a + k % RING * A_STAGE + piece, at_b + k % RING * B_STAGE + piece, at_s + k / 4u % 2u * S_STAGE + ra * 32u + ((k % 4u * 8u + half * 4u) ^ in_word), 0u};
     p.sb = p.sa + (BM + cb - ra) * 32u;
     asm volatile("" : "+v"(p.a), "+v"(p.b), "+v"(p.sa), "+v"(p.sb));   // four registers, and not one for every stage and half
     return p;
@@ -289,11 +291,11 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
     sb[half][n] = *reinterpret_cast<const __attribute__((address_space(3))) uint8_t*>(static_cast<uintptr_t>(p.sb + n * SIDE * 32u));
     fb[half][n] = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(static_cast<uintptr_t>(p.b + n * SIDE * kStageBytes));
   };
-  // STEADY: stage k + 2 is there to be asked for, and is not the last
+  // STEADY: stage k + RING is there to be asked for, and is not the last
   auto work = [&](uint32_t k, auto steady) {
     constexpr bool STEADY = decltype(steady)::value;
     constexpr uint32_t FROM = NA / 4u == 0u ? 1u : NA / 4u, ALL = LOADS + S_LOADS, OVER = SPREAD;
-    const bool more = STEADY || k + 2u < steps, last = !STEADY && k + 3u == steps, scales = k % 4u < 2u && (k / 4u + 1u) * 4u < steps;
+    const bool more = STEADY || k + RING < steps, last = !STEADY && k + RING + 1u == steps, scales = k % 4u < 2u && (k / 4u + 1u) * 4u < steps;
     // the first half's fragments are fa and fb[0]: multiply, and read the second half's
     Places p = places(k, 1);
 #pragma unroll
@@ -316,7 +318,8 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
       __builtin_amdgcn_sched_barrier(0);
       if (m + 1u == FROM) {
         // every wavefront has its last fragments of the stage, and the next stage is there
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (STEADY || k + RING - 1u < steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((RING - 2u) * LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (!STEADY && ragged && k + 2u == steps) trim();
 #pragma unroll
         for (uint32_t n = 0; n < NB; ++n) read_b(p, 0, n);   // behind the last stage: read, and not used
@@ -328,7 +331,7 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
       for (uint32_t i = 0; i < ALL; ++i)
         if (m + 1u >= FROM && i * OVER / ALL == m + 1u - FROM) {
           if (i < LOADS) {
-            if (more) load(k + 2u, i, last);
+            if (more) load(k + RING, i, last);
           } else if (scales) {
             if (k % 4u == 0u) load_scales(k / 4u + 1u, i - LOADS);
             else if (i - LOADS + S_LOADS < LOADS) load_scales(k / 4u + 1u, i - LOADS + S_LOADS);
@@ -341,12 +344,12 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
 #pragma unroll
     for (uint32_t i = 0; i < LOADS; ++i) load_scales(0, i);
 #pragma unroll
-    for (uint32_t k = 0; k < 2u; ++k)
+    for (uint32_t k = 0; k < RING; ++k)
       if (k < steps) {
 #pragma unroll
         for (uint32_t i = 0; i < LOADS; ++i) load(k, i, k + 1u == steps);
       }
-    if (steps >= 2u) wait_for_loads<LOADS>();
+    if (steps >= RING) wait_for_loads<(RING - 1u) * LOADS>();
     else wait_for_loads<0>();
     if (ragged && steps == 1u) trim();
     const Places p = places(0, 0);
@@ -355,7 +358,7 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
 #pragma unroll
     for (uint32_t m = 0; m < NA; ++m) read_a(p, m);
     uint32_t k = 0;
-    for (; k + 3u < steps; ++k) work(k, std::true_type{});
+    for (; k + RING + 1u < steps; ++k) work(k, std::true_type{});
     for (; k < steps; ++k) work(k, std::false_type{});
   }
 #pragma unroll
