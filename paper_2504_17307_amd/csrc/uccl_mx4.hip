@@ -29,18 +29,21 @@ int product_4(const ProductArgs& a, hipStream_t s) {
   const double few_tiles = fmax(tiles_down(a, 16u), used_groups(a));
   double few = fmax(tiles_down(a, 16u) * wide * 2.0e-5, used_groups(a) * wide * 2.6e-5);
   double tiles = fmax(rounds_of(small_tiles, 512.0) * (1.0 + 0.7 * fmin(1.0, small_tiles / 256.0)), used_groups(a) * wide * 3.0e-5);
-  const double low_tiles = tiles_down(a, 64u) * blocks_for(a.wide, 128u), deep = blocks_for(a.cols, 256u);
-  const bool low = low_tiles <= 256.0;
-  // While there is a compute unit for each tile of 64 x 128, in us and with what a call takes at the least.  Measured, 16 rows at a time / 64 x 128, us: 691 rows in 12 groups, 2296 -> 1232, 19.6 / 11.2;
-  // one group, 227 rows, 5387 -> 1960, 16.2 / 16.7, 395 rows, 5152 -> 952, 13.9 / 16.2, 142 rows, 3640 -> 728, 7.0 / 12.2, 614 rows, 3304 -> 1923, 27.7 / 13.2.
-  if (low) {
-    few = 3.5 + fmax(0.65, few_tiles * blocks_for(a.wide, 32u) / 512.0) * (2.0 + 0.85 * ceil(deep / 4.0));
-    tiles = 5.0 + deep * (0.45 + 0.2 * low_tiles / 256.0);
+  // While there is a compute unit for each tile of 64 x 64, or of 64 x 128, in us and with what a call takes at the least; the tiles of ragged groups are fewer than estimated.  Measured, 16 rows at a
+  // time / 64 x 64 / 64 x 128, us: one group, 130 rows, 7168 -> 2048, 14.6 / 16.1 / 19.8, 227 rows, 5387 -> 1960, 16.0 / 14.0 / 16.6, 614 rows, 3304 -> 1923, 27.5 / 14.2 / 12.9; 300 rows in 8 groups,
+  // 7168 -> 2048, 26.4 / 18.0 / 21.0; 691 rows in 12 groups, 2296 -> 1232, 19.6 / 12.1 / 11.2.
+  const double deep = blocks_for(a.cols, 256u), least_tiles = tiles_down(a, 64u) * blocks_for(a.wide, 64u), low_tiles = tiles_down(a, 64u) * blocks_for(a.wide, 128u);
+  const bool least = least_tiles <= 280.0, low = low_tiles <= 256.0;
+  if (least || low) {
+    const double weights = used_groups(a) * wide * a.cols * 1.1e-7;   // from memory
+    few = fmax(weights, 3.5 + fmax(0.65, few_tiles * blocks_for(a.wide, 32u) / 512.0) * (2.0 + 0.85 * ceil(deep / 4.0)));
+    tiles = fmax(weights, least ? 4.8 + deep * (0.38 + 0.08 * least_tiles / 256.0) : 5.0 + deep * (0.45 + 0.2 * low_tiles / 256.0));
   }
-  if (few < tiles && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 32u) <= 1u << 23)
+  if (few <= tiles && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 32u) <= 1u << 23)
     return product_tiles<kForward>(mx4_few_kernel<kRows4, 32, 4, 3>, 16, 32, 256, a, s);
   // 64 x 128 while there is a compute unit for each: 725 rows in 2 of 9 groups, 4839 -> 1929, 22 -> 19 us; 500 rows in 8 groups, 7168 -> 2048, 27.3 -> 26.4; 600 rows in one, 2048 -> 2048, 10.9 -> 8.8;
   // 1000 rows in 16 groups, where there is not, 44 -> 56
+  if (least) return product_tiles<kForward>(mx4_tile_kernel<64, 64, 4, 2, 1, 3>, 64, 64, 512, a, s);
   if (low) return product_tiles<kForward>(mx4_tile_kernel<64, 128, 2, 4, 2, 3>, 64, 128, 512, a, s);
   const double across = blocks_for(a.wide, 256u), large = rounds_of(tiles_down(a, 256u) * across, 256.0), middle = 0.91 * rounds_of(tiles_down(a, 192u) * across, 256.0);
   const double small = 0.62 * rounds_of(small_tiles, 512.0);
@@ -61,19 +64,25 @@ int product_16(const ProductArgs& a, hipStream_t s) {
   const double large = rounds_of(tiles_down(a, 128u) * blocks_for(a.wide, 256u), 256.0), square = 0.57 * rounds_of(tiles_down(a, 128u) * narrow, 256.0);
   const double low = low_tiles <= 256.0 ? 0.37 : 0.66 * rounds_of(low_tiles, 512.0);
   double few = fmax(tiles_down(a, 16u) * wide * 2.9e-5, used_groups(a) * wide * 3.3e-5), tiles = 4.1 * fmin(fmin(large, square), low);
-  // As in product_4().  Measured, 16 rows at a time / 64 x 128, us: bf16, 298 rows in 3 groups, 1545 -> 1757, 19.3 / 15.0, 412 in 3, 1176 -> 997, 12.9 / 11.6, 200 in 4, 7168 -> 2048, 27.7 / 37.5; one group,
-  // 385 rows, 4816 -> 1851, 33.4 / 29.3, 595 rows, 5096 -> 623, 24.5 / 30.0; f16, 85 rows in 5 groups, 3863 -> 1545, 13.0 / 28.1, 300 in 8, 7168 -> 2048, 44.4 / 53.6; 400 rows in one, 3000 -> 1900, 28.6 / 26.1.
-  if (low_tiles <= 256.0) {
-    few = 3.0 + ceil(few_tiles * blocks_for(a.wide, 64u) / 256.0 - 0.1) * (3.0 + 1.4 * ceil(blocks_for(a.cols, 256u) / 4.0)) * (F16 ? 1.08 : 1.0);
-    tiles = 7.0 + blocks_for(a.cols, 64u) * (F16 ? 0.33 + 0.14 * low_tiles / 256.0 : 0.25 + 0.07 * low_tiles / 256.0);
+  // As in product_4().  Measured, 16 rows at a time / 64 x 64 / 64 x 128, us: bf16, one group, 130 rows, 7168 -> 2048, 23.9 / 30.0 / 36.9, 385 rows, 4816 -> 1851, 34.0 / 24.6 / 29.4, 600 rows, 2048 -> 2048,
+  // 33.0 / 18.1 / 16.5; 298 rows in 3 groups, 1545 -> 1757, 19.4 / 12.9 / 15.1; 200 in 8, 7168 -> 2048, 29.2 / - / 35.5; 500 in 8 62.8 / 46.4 / 39.7; f16, 595 rows in one, 5096 -> 623, 26.3 / 31.4 / 40.3,
+  // 385 rows, 4816 -> 1851, 37.2 / 30.6 / 39.1.
+  const double least_tiles = tiles_down(a, 64u) * blocks_for(a.wide, 64u);
+  const bool least = least_tiles <= 280.0;
+  if (least || low_tiles <= 256.0) {
+    const double steps = blocks_for(a.cols, 64u);
+    few = 3.0 + ceil(few_tiles * blocks_for(a.wide, 64u) / 256.0 - 0.1) * (3.0 + 1.4 * ceil(steps / 16.0)) * (F16 ? 1.08 : 1.0);
+    tiles = least ? 5.5 + steps * (F16 ? 0.3 + 0.04 * least_tiles / 256.0 : 0.2 + 0.06 * least_tiles / 256.0)
+                  : 7.0 + steps * (F16 ? 0.33 + 0.14 * low_tiles / 256.0 : 0.25 + 0.07 * low_tiles / 256.0);
   }
   if (few < tiles && (static_cast<uint64_t>(a.rows) / 16u + used_groups(a)) * blocks_for(a.wide, 16u) <= 1u << 23) {
     if (few_tiles * blocks_for(a.wide, 64u) <= 64.0) return product_tiles<kForward>(mx4_few_kernel<X, 16, 4, 3>, 16, 16, 256, a, s);
     return product_tiles<kForward>(mx4_few_kernel<X, 64, 4, 2>, 16, 64, 256, a, s);
   }
-  if (low < square && low < large && (static_cast<uint64_t>(a.rows) / 64u + used_groups(a)) * static_cast<uint64_t>(narrow) <= 1u << 23) return product_tiles<kForward>(mx4_wide_kernel<F16, 64, 128, 5>, 64, 128, 512, a, s);
-  if (large <= square) return product_tiles<kForward>(mx4_wide_kernel<F16, 128, 256, 5>, 128, 256, 512, a, s);
-  return product_tiles<kForward>(mx4_wide_kernel<F16, 128, 128, 5>, 128, 128, 512, a, s);
+  if (least) return product_tiles<kForward>(mx4_wide_kernel<F16, 64, 64, 2, 5>, 64, 64, 512, a, s);
+  if (low < square && low < large && (static_cast<uint64_t>(a.rows) / 64u + used_groups(a)) * static_cast<uint64_t>(narrow) <= 1u << 23) return product_tiles<kForward>(mx4_wide_kernel<F16, 64, 128, 4, 5>, 64, 128, 512, a, s);
+  if (large <= square) return product_tiles<kForward>(mx4_wide_kernel<F16, 128, 256, 4, 5>, 128, 256, 512, a, s);
+  return product_tiles<kForward>(mx4_wide_kernel<F16, 128, 128, 4, 5>, 128, 128, 512, a, s);
 }
 
 }  // namespace

@@ -168,7 +168,7 @@ __device__ __forceinline__ bool exact_in_f16(uint32_t scale) { return scale - (1
 // ---- tiles, rows in 4 bits --------------------------------------------------------------------------
 
 // As product_tile_kernel: a stage is 128 bytes along the sum, 256 elements, and is multiplied in two halves; a half is one matrix instruction for
-// 16 x 16 of the output.  The LDS holds two stages of each operand, or RING: three where a compute unit has one small tile (64 x 128, 2551 rows, 5208 -> 523, 20.9 us with two and
+// 16 x 16 of the output.  The LDS holds two stages of each operand, or RING: three where a compute unit has one small tile (64 x 64 or 64 x 128; of 64 x 128, 2551 rows, 5208 -> 523, 20.9 us with two and
 // 18.5 with three; five take as long: what is left is a stage's chain of reads, products and addresses).  When every wavefront has read its last fragments of a stage, a little into its
 // second half, the stage RING further is asked for in its place, by loads that SPREAD rows of blocks have between them; the barrier there, which the
 // next stage's arrival is waited for at too, is the only one in a stage.
@@ -377,16 +377,16 @@ __global__ __launch_bounds__(WR * WC * 64) void mx4_tile_kernel(ProductArgs a) {
 
 // ---- tiles, rows in 16 bits -------------------------------------------------------------------------
 
-// A workgroup computes BM x BN of the output, 2 x 4 wavefronts a part each, 64 elements of the sum at a time, a step: 128 bytes of x's rows and 32 of w's, which come
+// A workgroup computes BM x BN of the output, 8 / WC x WC wavefronts a part each, 64 elements of the sum at a time, a step: 128 bytes of x's rows and 32 of w's, which come
 // 128 at a time, for four steps.  The LDS holds AHEAD steps of x, and two times four of w with their scales.  A lane has 16 neighbouring elements of a step, half a block: they
 // go into two matrix instructions, whose order of the elements is the same for both operands.  While a step is multiplied, the next one's fragments are read; when every
 // wavefront has had its last fragment of the step, a quarter into its products, the step AHEAD further takes its place.
 // Bound by what prepares the products: a fragment of w is widened in registers, 8 elements an instruction or four, under the matrix instructions of 16 bits: 8192^3 in bf16 952 to 1020 us,
 // 1.15 to 1.08 PFLOP/s of 1.45, in f16 1140 to 1195; 4000 rows in 4 groups, 7168 -> 2048, 119 and 138; 2999 rows in 24 groups, 2043 -> 1003, in f16 28 by 64 x 128: one
 // round of tiles, two on a compute unit, whose 32 steps take twice the products' time, most of them in the barrier and the waits that a step of so few products has too.
-template <bool F16, uint32_t BM, uint32_t BN, uint32_t AHEAD>
+template <bool F16, uint32_t BM, uint32_t BN, uint32_t WC, uint32_t AHEAD>
 __global__ __launch_bounds__(512) void mx4_wide_kernel(ProductArgs a) {
-  constexpr uint32_t SIDE = 16u, NA = BM / 32u, NB = BN / 64u, A_LOADS = BM / 64u, B_LOADS = BN / 64u, FROM = NA / 4u == 0u ? 1u : NA / 4u;
+  constexpr uint32_t SIDE = 16u, WR = 8u / WC, NA = BM / WR / SIDE, NB = BN / WC / SIDE, A_LOADS = BM / 64u, B_LOADS = BN / 64u, FROM = NA / 4u == 0u ? 1u : NA / 4u;
   constexpr uint32_t A_STEP = BM * 128u, B_STAGE = BN * 128u, S_STAGE = 2048u;   // scales: 8 bytes of 256 rows
   static_assert(AHEAD >= 3u && AHEAD <= 5u);
   __shared__ __align__(1024) char lds_a[AHEAD * A_STEP], lds_b[2u * B_STAGE], lds_s[2u * S_STAGE];
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(512) void mx4_wide_kernel(ProductArgs a) {
   };
 
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), lane = threadIdx.x & 63u, quarter = lane / 16u, r16 = lane % 16u;
-  const uint32_t ra = wave / 4u * (BM / 2u), cb = wave % 4u * (BN / 4u);
+  const uint32_t ra = wave / WC * (BM / WR), cb = wave % WC * (BN / WC);
   const uint32_t high = __builtin_amdgcn_readfirstlane(r0 + ra < g.end ? min((g.end - r0 - ra + SIDE - 1u) / SIDE, NA) : 0u);
   f32x4 acc[NB][NA] = {};
   u32x4 fa[NA][2];

@@ -295,12 +295,14 @@ def product(rt, kind, n, groups, wide, cols):
 
 def product_kernels(rt):
     """Rows of a tile, or columns of one of 16 rows, by what is multiplied; the shapes of the GPU's tests and those that were measured."""
-    few, least, small, middle, large, wide = ("few", "32", "4"), ("tile", "64", "128"), ("tile", "128", "128"), ("tile", "192", "256"), ("tile", "256", "256"), ("wide", "128", "256")
-    few16, few64, low, square = ("few", "16", "4"), ("few", "64", "4"), ("wide", "64", "128"), ("wide", "128", "128")
-    for shape, four, sixteen in zip(SHAPES, (least, few, middle, few, small, least, large, middle), (low, few64, square, few16, wide, low, wide, square)):
+    few, least, lower, small, middle, large, wide = ("few", "32", "4"), ("tile", "64", "64"), ("tile", "64", "128"), ("tile", "128", "128"), ("tile", "192", "256"), ("tile", "256", "256"), ("wide", "128", "256")
+    few16, few64, least16, low, square = ("few", "16", "4"), ("few", "64", "4"), ("wide", "64", "64"), ("wide", "64", "128"), ("wide", "128", "128")
+    for shape, four, bf16, f16 in zip(SHAPES, (lower, least, middle, few, small, least, large, middle), (low, least16, square, few16, wide, least16, wide, square), (low, few64, square, few16, wide, least16, wide, square)):
+        assert [product(rt, kind, *shape) for kind in ("mx4", "bf16", "f16")] == [four, bf16, f16], shape
+    for shape, four, sixteen in (((500, 1, 520, 600), least, least16), ((1500, 2, 1030, 600), lower, low), ((150, 8, 1000, 2600), few, few64)):
         assert [product(rt, kind, *shape) for kind in ("mx4", "bf16", "f16")] == [four, sixteen, sixteen], shape
-    for shape, four, sixteen in (((16, 32, 2048, 7168), few, few64), ((128, 32, 2048, 7168), few, few64), ((1, 1, 2048, 7168), few, few16), ((300, 8, 2048, 7168), least, low), ((1000, 16, 2048, 7168), small, square),
-                                 ((4096, 16, 2048, 7168), middle, square), ((4000, 4, 2048, 7168), small, wide), ((8190, 16, 7168, 2048), large, wide), ((2999, 24, 1003, 2044), small, low), ((500, 8, 2048, 7168), least, low), ((8192, 1, 8192, 8192), large, wide)):
+    for shape, four, sixteen in (((16, 32, 2048, 7168), few, few64), ((128, 32, 2048, 7168), few, few64), ((1, 1, 2048, 7168), few, few16), ((300, 8, 2048, 7168), least, least16), ((1000, 16, 2048, 7168), small, square),
+                                 ((4096, 16, 2048, 7168), middle, square), ((4000, 4, 2048, 7168), small, wide), ((8190, 16, 7168, 2048), large, wide), ((2999, 24, 1003, 2044), small, low), ((500, 8, 2048, 7168), lower, low), ((8192, 1, 8192, 8192), large, wide)):
         assert [product(rt, kind, *shape) for kind in ("mx4", "bf16")] == [four, sixteen], (shape, product(rt, "mx4", *shape), product(rt, "bf16", *shape))
     # narrow outputs of very many rows: by 16 rows while that fits a launch, by tiles where these do, refused where nothing does
     for n, kind in ((1 << 26, "few"), ((1 << 29) - 1024, None)):

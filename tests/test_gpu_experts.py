@@ -549,6 +549,14 @@ def test_product_of_long_sums(uccl, kind, rows, groups, wide, cols):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,groups,wide", [(500, 1, 520), (1500, 2, 1030), (150, 8, 1000)])
+@pytest.mark.parametrize("cols", [32, 96, 250, 300, 514, 600, 900, 1100, 1358, 1410, 2600])
+def test_product_by_small_tiles_of_short_sums(uccl, kind, rows, groups, wide, cols):
+    """Of one stage of a ring, two, three and so on, whole ones and not."""
+    test_product_of_long_sums(uccl, kind, rows, groups, wide, cols)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_product_of_an_odd_number_of_columns_by_the_struct(uccl, kind):
     """The half byte behind the last element holds anything."""
     import ctypes as C
