@@ -138,11 +138,11 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 enum Mx4Rows : uint32_t { kRows4, kRowsBf16, kRowsF16 };
 
 // f16 has 11 bits, which are two bf16 exactly: the first 8 of them and what is left, with the same sign.  (The nearest bf16 of the greatest f16 is above them all, and its product may
-// be past binary32 where theirs is not.)
+// be past binary32 where theirs is not.)  What an infinity leaves is any number, for the difference, NaN, would make every sum of the row NaN.
 __device__ __forceinline__ void split_f16(u32x4 v, u32x4& high, u32x4& low) {
   const f16x8 f = __builtin_bit_cast(f16x8, v);
   auto upper_halves = [](float x, float y) { return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u); };   // two bf16
-  auto left = [](float x) { return x - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xFFFF0000u); };
+  auto left = [](float x) { return fminf(x - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xFFFF0000u), 1024.0f); };   // (the lesser of NaN and a number is the number; 224 is the greatest other)
 #pragma unroll
   for (uint32_t i = 0; i < 4u; ++i) {
     const float x = static_cast<float>(f[2u * i]), y = static_cast<float>(f[2u * i + 1u]);

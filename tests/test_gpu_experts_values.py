@@ -5,8 +5,8 @@ Tolerances as in tests/test_gpu_experts.py.
 import pytest
 import torch
 
-from test_gpu_experts import E2M1, E8M0, gen, random_mx4
-from test_gpu_rows import aligned
+from test_gpu_experts import DEEP, E2M1, E8M0, INF, decode, gen, product_reference, random_mx4
+from test_gpu_rows import T, aligned, close, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,32 @@ def test_product_of_the_greatest_f16_by_large_weights(uccl, rows):
     want = torch.full((rows, wide), 65504.0 * 2.0 ** 112, dtype=torch.float64, device="cuda")
     want[1::2] *= -1
     assert torch.equal(y.double(), want)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("more", [0, 17, 40, 64, 100])
+@pytest.mark.parametrize("rows,groups,wide,cols", DEEP)
+def test_product_of_infinities(uccl, kind, rows, groups, wide, cols, more):
+    """A row with an infinity, and every weight beside it another number than 0: an infinity with the sign of the product in every column, also where a column of the same
+    wavefront has scales that f16 does not hold, and where the sum ends within a block.  By every kernel (tests/test_experts_abi.py has which)."""
+    g, cols = gen(rows + cols + more), cols + more + more % 2
+    w, ws = random_mx4(g, groups * wide, cols)
+    w.view(torch.uint8).bitwise_or_(0x11)                                   # no zeros
+    ws.view(torch.uint8)[3::16, ::3] = 0
+    ws.view(torch.uint8)[9::16, -1] = 200
+    x = normal(g, rows, cols, T[kind], pad=1)
+    broken = torch.arange(0, rows, 3, device="cuda")
+    at = torch.randint(0, cols, (len(broken),), device="cuda", generator=g)
+    at[0], at[-1] = cols - 1, 0
+    sign = torch.where(torch.rand(len(broken), device="cuda", generator=g) < 0.5, -1.0, 1.0)
+    x[broken, at] = (INF * sign).to(T[kind])
+    ends = [rows * k // groups for k in range(groups + 1)]
+    y = aligned(rows, wide, torch.float32)
+    uccl.uccl_group_product(y, x, grouped(w, groups).view(E2M1), torch.tensor(ends, dtype=torch.int32, device="cuda"), w_scales=grouped(ws, groups).view(E8M0))
+    dw = decode(w, ws, cols).view(groups, wide, cols)
+    want, mag = product_reference(torch.where(x.isinf(), 0.0, x.double()), dw, None, ends)
+    of = torch.bucketize(broken, torch.tensor(ends[1:], device="cuda"), right=True)
+    want[broken] = INF * sign[:, None].double() * dw[of, :, at].sign()
+    mag[broken] = 0.0
+    close(y, want, mag, cols, kind)
+    assert torch.equal(y[broken].double(), want[broken])
