@@ -321,7 +321,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
   using S = Scores<T, LANES, K>;
   constexpr uint32_t N = S::N, V = S::V, KEEP = 32u / LANES == 0u ? 1u : 32u / LANES, EACH = 256u / LANES;
   __shared__ float part[EACH][LANES * V], of_sums[LANES * V];
-  for (uint32_t e = threadIdx.x; e < LANES * V; e += 256u) of_sums[e] = a.dsums != nullptr ? a.dsums[min(e, a.cols - 1u)] : 0.0f;   // (behind the last expert p is 0)
+  for (uint32_t e = threadIdx.x; e < LANES * V; e += 256u) of_sums[e] = a.dsums != nullptr && e < a.cols ? a.dsums[e] : 0.0f;   // (behind the last expert p is 0, which an infinity would make NaN)
   __syncthreads();
   const uint32_t lane = threadIdx.x % LANES, at = blockIdx.x * EACH + threadIdx.x / LANES;
   const bool here = at < a.tokens;

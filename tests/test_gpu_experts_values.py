@@ -5,7 +5,7 @@ Tolerances as in tests/test_gpu_experts.py.
 import pytest
 import torch
 
-from test_gpu_experts import DEEP, E2M1, E8M0, INF, decode, gen, product_reference, random_mx4
+from test_gpu_experts import DEEP, E2M1, E8M0, INF, decode, f32, gen, i32, product_reference, random_mx4, softmax
 from test_gpu_rows import T, aligned, close, normal
 
 pytestmark = pytest.mark.gpu
@@ -75,3 +75,25 @@ def test_product_of_infinities(uccl, kind, rows, groups, wide, cols, more):
     mag[broken] = 0.0
     close(y, want, mag, cols, kind)
     assert torch.equal(y[broken].double(), want[broken])
+
+
+# ---- routing --------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("normalise", [False, True])
+@pytest.mark.parametrize("tokens", [5, 3000])
+@pytest.mark.parametrize("n", [3, 61, 64, 100, 250, 700])
+@pytest.mark.parametrize("dtype", list(T))
+def test_route_grad_of_infinite_gradients_of_the_sums(uccl, dtype, n, tokens, normalise):
+    """An infinity for one expert's sum: its probability's share is an infinity for every other expert, and what lies behind a row's last expert is not in it."""
+    scores = normal(gen(n), tokens, n, T[dtype])
+    experts, dw = i32(tokens, 2, fill=0), f32(tokens, 2, fill=0.0)
+    for at in (0, n - 1):
+        ds = torch.randn(n, device="cuda", generator=gen(1))
+        ds[at] = INF
+        out = aligned(tokens, n, T[dtype])
+        uccl.uccl_route_rows_grad(out, scores, experts, dw, dsums=ds, normalise=normalise)
+        p = softmax(scores)
+        want = p * (ds.double() - (p * ds.double()).sum(1, keepdim=True))     # infinity less infinity for the expert itself
+        assert bool(want[:, at].isnan().all()) and bool((want[:, torch.arange(n, device="cuda") != at] == -INF).all())
+        assert torch.equal(out.double().nan_to_num(nan=7.0), want.nan_to_num(nan=7.0))
