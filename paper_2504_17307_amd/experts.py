@@ -118,6 +118,8 @@ def _matrices(tensors, like=None):
     """The bytes of a HOST array of uccl_rows for ``tensors``, of another for those of ``like``, which have their shapes and types (by default they themselves), and how many matrices there
     are: a contiguous tensor is one row, or whole rows and what is left; two tensors are cut alike."""
     like = tensors if like is None else like
+    if hasattr(tensors, "__next__") or hasattr(like, "__next__"):   # gone through once, and nothing of it is left for a prepared call to hold
+        raise ValueError("a list of tensors is wanted, not an iterator")
     if type(tensors) is list and type(like) is list:
         reader = _find_reader() if rows._reader is None else rows._reader
         made = reader.contiguous_rows(tensors, like, _LONGEST) if reader else None

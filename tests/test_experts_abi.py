@@ -252,6 +252,30 @@ def test_tensors_are_read_as_the_interpreter_reads_them(monkeypatch):
         assert reader.matrix_rows(thing) is None and reader.vector_address(thing, False, 7) is None and reader.contiguous_rows([thing], [thing], 9) is None
 
 
+@pytest.mark.parametrize("reads", [True, False])
+def test_lists_of_tensors_are_no_iterators(monkeypatch, reads):
+    """Whatever can be gone through again is taken whole; an iterator, which cannot, and of which a prepared call would hold nothing, is refused."""
+    import torch
+    from paper_2504_17307_amd import experts, rows as r
+    r._find_reader()
+    if not reads:
+        monkeypatch.setattr(r, "_reader", False)
+    grads = [torch.ones(5) * k for k in range(5)]
+    want = experts._matrices(grads)
+    assert want[2] == 5
+    for again in (tuple(grads), dict(enumerate(grads)).values(), torch.nn.ParameterList(grads)):
+        assert experts._matrices(again)[2] == 5 and (again.__class__ is torch.nn.ParameterList or experts._matrices(again) == want)
+    f = torch.zeros
+    for once in (lambda: iter(grads), lambda: (g for g in grads), lambda: map(torch.clone, grads), lambda: iter([])):
+        for call in (lambda: pkg.uccl_gradient_norm(f(1), once(), f(100), stream=0), lambda: pkg.uccl_prepare(pkg.uccl_gradient_norm, f(1), once(), f(100), stream=0),
+                     lambda: experts._matrices(grads, once()), lambda: experts._matrices(once(), grads)):
+            with pytest.raises(ValueError):
+                call()
+        for outs, of in ((grads, once()), (once(), grads), (once(), once())):
+            with pytest.raises((ValueError, TypeError)):
+                pkg.uccl_gradient_clip(outs, of, f(1), 1.0, stream=0)
+
+
 def test_kernels_use_no_scratch_memory(tmp_path):
     """The library's code objects of routing and clipping, and of 4 bits."""
     lib, at, blocks = open(pkg.LIB_PATH, "rb").read(), -1, []
