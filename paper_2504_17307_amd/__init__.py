@@ -214,25 +214,28 @@ def uccl_prepare(func, *args, **kwargs):
     uccl_chunk_scatter*, uccl_chunk_reduce_gather, uccl_chunk_segment, uccl_dedup_reset,
     uccl_dedup_report, uccl_message_status); the result is a zero-argument callable that makes that
     C call with the same pointers, sizes and stream handle every time: the stream is the one given,
-    or torch's current one, WHEN THE CALL WAS PREPARED.  The callable keeps the arguments alive."""
+    or torch's current one, WHEN THE CALL WAS PREPARED.  The callable keeps the arguments alive, and what lists among
+    them held then."""
     _tls.pending = []
     try:
         func(*args, **kwargs)
         (typed, cargs, name), = _tls.pending
     finally:
         _tls.pending = None
+    # a list may hold other tensors later: those that it holds now are kept too
+    lists = [list(a) for a in (*args, *kwargs.values()) if hasattr(a, "__iter__") and not hasattr(a, "data_ptr")]
     extension = _extension if _extension is not None else _load_extension()
     if not extension:
-        return _prepared_by_ctypes(typed, cargs, name, (args, kwargs))
+        return _prepared_by_ctypes(typed, cargs, name, (args, kwargs), lists)
     # the arguments are converted to C here, once
-    return extension.Prepared(_address(name), tuple(map(_c_value, typed.argtypes, cargs)), functools.partial(_raise, name), (args, kwargs), (cargs, _lib), name)
+    return extension.Prepared(_address(name), tuple(map(_c_value, typed.argtypes, cargs)), functools.partial(_raise, name), (args, kwargs), (cargs, _lib, lists), name)
 
 
 def _raise(name, code):
     raise UcclError(code, name)
 
 
-def _prepared_by_ctypes(typed, cargs, name, keeps):
+def _prepared_by_ctypes(typed, cargs, name, keeps, lists):
     """The same without the extension: a function object of its own without argument types takes C values as they are."""
     fn = _lib[name]
     fn.restype = typed.restype
@@ -243,7 +246,7 @@ def _prepared_by_ctypes(typed, cargs, name, keeps):
         if code != UCCL_OK:
             raise UcclError(code, name)
 
-    enqueue.keeps, enqueue.__name__ = keeps, name
+    enqueue.keeps, enqueue.lists, enqueue.__name__ = keeps, lists, name
     return enqueue
 
 

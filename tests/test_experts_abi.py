@@ -276,6 +276,28 @@ def test_lists_of_tensors_are_no_iterators(monkeypatch, reads):
                 pkg.uccl_gradient_clip(outs, of, f(1), 1.0, stream=0)
 
 
+@pytest.mark.parametrize("extension", [True, False])
+def test_a_prepared_call_keeps_the_tensors_of_its_lists(monkeypatch, extension):
+    """Also when the lists hold others by then: the call has the addresses of those that it was prepared with."""
+    import gc
+    import weakref
+    import torch
+    if not extension:
+        monkeypatch.setattr(pkg, "_extension", False)
+    make = lambda: [torch.zeros(64) for _ in range(3)]  # noqa: E731
+    outs, grads, norm = make(), make(), torch.zeros(1)
+    for prepare in (lambda: pkg.uccl_prepare(pkg.uccl_gradient_clip, outs, grads, norm, 1.0, stream=0), lambda: pkg.uccl_prepare(pkg.uccl_gradient_norm, norm, grads=grads, scratch=torch.zeros(1 << 16), stream=0)):
+        outs[:], grads[:] = make(), make()
+        call = prepare()
+        there = [weakref.ref(t) for t in (grads + outs if "clip" in call.__name__ else grads)]
+        outs.clear(), grads.clear()
+        gc.collect()
+        assert all(t() is not None for t in there)
+        del call
+        gc.collect()
+        assert all(t() is None for t in there)
+
+
 def test_kernels_use_no_scratch_memory(tmp_path):
     """The library's code objects of routing and clipping, and of 4 bits."""
     lib, at, blocks = open(pkg.LIB_PATH, "rb").read(), -1, []
