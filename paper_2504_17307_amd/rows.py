@@ -48,7 +48,10 @@ def _type(dtype):
         import torch
         from . import UCCL_BF16, UCCL_F16, UCCL_F32
         _types.update({torch.float32: (UCCL_F32, 4), torch.bfloat16: (UCCL_BF16, 2), torch.float16: (UCCL_F16, 2),
-                       torch.float8_e4m3fn: (UCCL_E4M3, 1), torch.float4_e2m1fn_x2: (UCCL_MX4, 1), "scale": torch.float32, "block": torch.float8_e8m0fnu})
+                       torch.float8_e4m3fn: (UCCL_E4M3, 1), "scale": torch.float32})
+        four, block = getattr(torch, "float4_e2m1fn_x2", None), getattr(torch, "float8_e8m0fnu", None)
+        if four is not None and block is not None:   # a torch without them has no tensors of 4 bits, and all others
+            _types.update({four: (UCCL_MX4, 1), "block": block})
     if dtype not in _types:
         raise ValueError(f"rows of {dtype} are not supported")
     return _types[dtype]

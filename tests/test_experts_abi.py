@@ -276,6 +276,22 @@ def test_lists_of_tensors_are_no_iterators(monkeypatch, reads):
                 pkg.uccl_gradient_clip(outs, of, f(1), 1.0, stream=0)
 
 
+@pytest.mark.parametrize("missing", [("float4_e2m1fn_x2", "float8_e8m0fnu"), ("float4_e2m1fn_x2",), ("float8_e8m0fnu",)])
+def test_rows_of_other_types_need_no_torch_with_4_bits(monkeypatch, missing):
+    import torch
+    from paper_2504_17307_amd import rows as r
+    tensors = [torch.zeros(4, 32, dtype=t) for t in (torch.float32, torch.bfloat16, torch.float16)]
+    eight, four = torch.zeros(4, 32, dtype=torch.uint8).view(torch.float8_e4m3fn), torch.zeros(4, 16, dtype=torch.uint8).view(torch.float4_e2m1fn_x2)
+    want = [r._rows(t) for t in tensors] + [r._rows(eight, torch.zeros(4))[4 * 8:]]
+    monkeypatch.setattr(r, "_types", {})
+    monkeypatch.setattr(r, "_reader", False)
+    for name in missing:
+        monkeypatch.delattr(torch, name)
+    assert [r._rows(t) for t in tensors] + [r._rows(eight, torch.zeros(4))[4 * 8:]] == want
+    with pytest.raises(ValueError):
+        r._rows(four, torch.zeros(4, 1, dtype=torch.uint8))
+
+
 @pytest.mark.parametrize("extension", [True, False])
 def test_a_prepared_call_keeps_the_tensors_of_its_lists(monkeypatch, extension):
     """Also when the lists hold others by then: the call has the addresses of those that it was prepared with."""
