@@ -153,11 +153,24 @@ class Router:
         """The gradient of the rows, for ``dweights`` of the weights and the balance loss; the weight's stays here."""
         dscores = self._rows(torch.float32)
         uccl.uccl_route_rows_grad(dscores, self.scores, self.experts, dweights, dsums=self.dsums, normalise=True)
-        self.dscores = self._rows(self.y.dtype).copy_(dscores)   # products are of 16 bits
-        dy, self.dweight = torch.empty_like(self.y), torch.empty(self.weight.shape, dtype=torch.float32, device=self.y.device)
-        uccl.uccl_group_product_grad_x(dy, self.dscores, self.weight[None], self.all)
-        uccl.uccl_group_product_grad_w(self.dweight[None], self.dscores, self.y, self.all)
-        return dy
+        if self.y.dtype == torch.bfloat16:
+            dy, self.dweight = self._products(self._rows(torch.bfloat16).copy_(dscores), torch.bfloat16)   # products are of 16 bits
+            return dy
+        # f16 has nothing below 2^-24, which the balance loss's part of a score is below already with some thousand tokens: the greatest is brought to 1 by a power of two,
+        # and what the first 11 bits leave, 2^24 times as large, is multiplied by itself
+        by = torch.exp2(-torch.frexp(dscores.abs().amax())[1].clamp(min=-100).float())
+        dscores *= by
+        first = self._rows(torch.float16).copy_(dscores)
+        (dy, dweight), (dy2, dweight2) = self._products(first, torch.float32), self._products(self._rows(torch.float16).copy_((dscores - first) * 2.0 ** 24), torch.float32)
+        self.dweight = (dweight + dweight2 * 2.0 ** -24) / by
+        return ((dy + dy2 * 2.0 ** -24) / by).to(torch.float16)
+
+    def _products(self, dscores, dtype):
+        """The gradients of the rows, in that type, and of the weight."""
+        dy, dweight = torch.empty(self.y.shape, dtype=dtype, device=self.y.device), torch.empty(self.weight.shape, dtype=torch.float32, device=self.y.device)
+        uccl.uccl_group_product_grad_x(dy, dscores, self.weight[None], self.all)
+        uccl.uccl_group_product_grad_w(dweight[None], dscores, self.y, self.all)
+        return dy, dweight
 
 
 def serve_in_4_bits(x, norm_weight, router, up, up_scales, down, down_scales, arrival_order):

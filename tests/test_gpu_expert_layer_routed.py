@@ -100,6 +100,33 @@ def test_gradients_of_the_routed_layer_are_its_derivative(layer):
     assert abs(float(torch.sqrt(sum((g.double() ** 2).sum() for g in got["clipped"].values()))) - 0.5) <= 1e-6
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("size", [0.0, 1e-6, 1.0, 300.0])
+def test_gradient_of_the_router_has_the_balance_loss_of_many_tokens(layer, dtype, size):
+    """Whose part of a score is about 1e-7, beside gradients of the weights of any size.  Each score's gradient is rounded to bf16, half of finfo.eps of itself (2^-8), or to two f16: the first is off
+    by 2^-11 of itself at most, and the second by 2^-11 of that, or, where it is subnormal, by half of 2^-24 by 2^-24 where the greatest is 1/2 or more: 2^-48 of it.
+    Products as elsewhere."""
+    import paper_2504_17307_amd as uccl
+    tokens, cols, n, slots = 4096, 64, 32, 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    given = {"up": torch.empty(n, 1, cols), "x": torch.empty(1, cols, dtype=dtype)}
+    router, y = router_of(layer, given, slots, coef=0.01), torch.randn(tokens, cols, device="cuda", generator=g).to(dtype)
+    _, weights = router.forward(y)
+    dweights = size * torch.randn(tokens, slots, device="cuda", generator=g)
+    dy = router.backward(dweights)
+    dscores = torch.empty(tokens, n, device="cuda")
+    uccl.uccl_route_rows_grad(dscores, router.scores, router.experts, dweights, dsums=router.dsums, normalise=True)
+    d, yd, wd = dscores.double(), y.double(), router.weight.double()
+    off = d.abs() * 2.0 ** -8 if dtype == torch.bfloat16 else d.abs() * 2.0 ** -22 + d.abs().amax() * 2.0 ** -48
+    want, mag = d.T @ yd, d.abs().T @ yd.abs()
+    sums = (tokens + 8) * 2.0 ** -24
+    assert bool(((router.dweight.double() - want).abs() <= off.T @ yd.abs() + mag * sums).all())
+    assert bool((router.dweight != 0).all())
+    want, mag = d @ wd, d.abs() @ wd.abs()
+    info = torch.finfo(dtype)
+    assert bool(((dy.double() - want).abs() <= want.abs() * info.eps / 2 + info.smallest_normal * info.eps + off @ wd.abs() * (1 + info.eps) + mag * (n + 8) * 2.0 ** -24).all())
+
+
 def test_readme_example_of_routing_and_4_bits_runs(gpu_lib):
     text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
     ns = {"torch": torch, "uccl": gpu_lib}
