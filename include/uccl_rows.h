@@ -103,7 +103,7 @@ uint64_t uccl_norm_rows_scratch(uint32_t rows, uint32_t cols);
  *            that, below 0 as 0, above the rows of y as these
  * Sums are held in binary32 and rounded once; 8-bit operands are multiplied as they are, exactly, and the sum by both scales.  Operands in 4 bits stand
  * for their values with their blocks' scales: of two of them a block's 32 products are added exactly; beside rows in 16 bits they are what
- * bf16 holds exactly, or f16.
+ * bf16 holds exactly, or f16; one of 2^128 and above (4 and 6 by the scale 2^126, 2 and above by 2^127: no uccl_quantise_rows makes them) makes its sums there infinities or NaN.
  * What a call is cut into depends on its sizes alone, never on the offsets' values.
  */
 int uccl_group_product(const uccl_rows* y, const uccl_rows* x, const int32_t* index, const uccl_rows* w,

@@ -7,7 +7,7 @@ namespace {
 
 constexpr uint32_t kMx4Block = 32;
 
-// Four bytes, two elements each, times 2^(byte - 127) as eight bf16: exact, for bf16 has all these powers.
+// Four bytes, two elements each, times 2^(byte - 127) as eight bf16: exact below 2^128, for bf16 has all these powers; an infinity from there on.
 __device__ __forceinline__ u32x4 widen_e2m1(uint32_t eight, float scale) {
   return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 1)),
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(eight, scale, 3))};
