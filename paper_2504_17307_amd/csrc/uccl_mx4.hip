@@ -18,6 +18,10 @@ double rounds_of(double tiles, double room) {
   return rounds <= 1.05 ? 1.0 : rounds <= 2.0 ? 2.0 : rounds + 0.5;
 }
 
+// Tiles of 64 x 64 while there is a compute unit for each: the tiles of ragged groups are fewer than estimated, one group's are not.  Measured, one group, 260 to 280 of them / half as many of 64 x 128, us:
+// rows in 4 bits, depth 512 5.7 to 6.0 / 5.5 to 5.7, 5000 16.9 to 19.2 / 15.1 to 15.5; bf16, 512 8.2 to 8.6 / 7.2 to 7.5, 5000 33 to 48 / 28 to 30; f16, 5000 42 to 50 / 40; 256 of them, 5000, 12.8, 25 and 31.
+bool takes_least(const ProductArgs& a, double least_tiles) { return least_tiles <= (a.groups == 1u ? 256.0 : 280.0); }
+
 // Rows of 4 bits, in us for 256 elements of the sum.  Few rows: 2.0e-5 for 16 rows of a column, 2.6e-5 for a column's weights where they are read once;
 // tiles of 128 x 128, two on a compute unit: 1.7 a round, 1 where most of them are idle.  Measured, 16 rows at a time / 128 x 128, 7168 -> 2048, us: one group, 1 / 100 rows, 8.0 / 10.4 against
 // 23 / 28; 8 of 32 groups, 16 rows, 13.3 against 28; 32 groups, 128 rows, 49 against 54; 8 groups, 300 rows, 27 against 27; 16 groups, 1000 rows, 81 against 47.
@@ -29,11 +33,11 @@ int product_4(const ProductArgs& a, hipStream_t s) {
   const double few_tiles = fmax(tiles_down(a, 16u), used_groups(a));
   double few = fmax(tiles_down(a, 16u) * wide * 2.0e-5, used_groups(a) * wide * 2.6e-5);
   double tiles = fmax(rounds_of(small_tiles, 512.0) * (1.0 + 0.7 * fmin(1.0, small_tiles / 256.0)), used_groups(a) * wide * 3.0e-5);
-  // While there is a compute unit for each tile of 64 x 64, or of 64 x 128, in us and with what a call takes at the least; the tiles of ragged groups are fewer than estimated.  Measured, 16 rows at a
+  // While there is a compute unit for each tile of 64 x 64, or of 64 x 128, in us and with what a call takes at the least.  Measured, 16 rows at a
   // time / 64 x 64 / 64 x 128, us: one group, 130 rows, 7168 -> 2048, 14.6 / 16.1 / 19.8, 227 rows, 5387 -> 1960, 16.0 / 14.0 / 16.6, 614 rows, 3304 -> 1923, 27.5 / 14.2 / 12.9; 300 rows in 8 groups,
   // 7168 -> 2048, 26.4 / 18.0 / 21.0; 691 rows in 12 groups, 2296 -> 1232, 19.6 / 12.1 / 11.2.
   const double deep = blocks_for(a.cols, 256u), least_tiles = tiles_down(a, 64u) * blocks_for(a.wide, 64u), low_tiles = tiles_down(a, 64u) * blocks_for(a.wide, 128u);
-  const bool least = least_tiles <= 280.0, low = low_tiles <= 256.0;
+  const bool least = takes_least(a, least_tiles), low = low_tiles <= 256.0;
   if (least || low) {
     const double weights = used_groups(a) * wide * a.cols * 1.1e-7;   // from memory
     few = fmax(weights, 3.5 + fmax(0.65, few_tiles * blocks_for(a.wide, 32u) / 512.0) * (2.0 + 0.85 * ceil(deep / 4.0)));
@@ -68,7 +72,7 @@ int product_16(const ProductArgs& a, hipStream_t s) {
   // 33.0 / 18.1 / 16.5; 298 rows in 3 groups, 1545 -> 1757, 19.4 / 12.9 / 15.1; 200 in 8, 7168 -> 2048, 29.2 / - / 35.5; 500 in 8 62.8 / 46.4 / 39.7; f16, 595 rows in one, 5096 -> 623, 26.3 / 31.4 / 40.3,
   // 385 rows, 4816 -> 1851, 37.2 / 30.6 / 39.1.
   const double least_tiles = tiles_down(a, 64u) * blocks_for(a.wide, 64u);
-  const bool least = least_tiles <= 280.0;
+  const bool least = takes_least(a, least_tiles);
   if (least || low_tiles <= 256.0) {
     const double steps = blocks_for(a.cols, 64u);
     few = 3.0 + ceil(few_tiles * blocks_for(a.wide, 64u) / 256.0 - 0.1) * (3.0 + 1.4 * ceil(steps / 16.0)) * (F16 ? 1.08 : 1.0);

@@ -379,6 +379,18 @@ def test_which_kernel_a_product_is_launched_as(tmp_path):
     in_process("product_kernels", tmp_path)
 
 
+def one_round_of_small_tiles(rt):
+    """64 x 64 while every tile of one group has a compute unit."""
+    for rows, wide, small in ((1024, 1024, True), (1024, 1088, False), (832, 1280, False), (256, 4224, False), (256, 4096, True)):
+        for cols in (512, 2048, 5000):
+            for kind in ("mx4", "bf16", "f16"):
+                assert (product(rt, kind, rows, 1, wide, cols)[1:] == ("64", "64")) == small, (kind, rows, wide, cols)
+
+
+def test_one_round_of_small_tiles(tmp_path):
+    in_process("one_round_of_small_tiles", tmp_path)
+
+
 def timing_events(rt):
     """A call's start event is on its first launch and its stop on its last; what HIP refuses comes back."""
     events = []
