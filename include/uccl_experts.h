@@ -37,6 +37,7 @@ extern "C" {
  * uccl_route_rows -- with z a token's scores and p = softmax(z) over its experts:
  *     key_e = z_e + bias_e in binary32;  the token's experts are the `slots` with the greatest keys, in that order, of equal keys the lowest
  *     expert first;  weight = scale p_e, or, normalised, scale p_e / (sum of p over the token's experts).
+ * (The bias is the score's, not p's: a router that adds it to a probability, or whose probabilities are sigmoids, is another.)
  *
  *   experts  written: tokens x slots int32, 4-byte aligned.  An expert whose key is -infinity or NaN is never chosen; where too few are left, -1
  *   weights  written: tokens x slots floats, 4-byte aligned; 0 beside a -1
